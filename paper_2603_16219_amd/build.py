@@ -11,6 +11,8 @@ _ROOT = os.path.dirname(_PKG)
 SOURCES = [os.path.join(_PKG, "csrc", n) for n in ("specsteer.hip", "split.hip")]
 INCLUDE = os.path.join(_ROOT, "include")
 LIBRARY = os.path.join(_PKG, "libspecsteer.so")
+LOSS_SOURCES = [os.path.join(_PKG, "csrc", "loss", "loss.hip")]
+LOSS_LIBRARY = os.path.join(_PKG, "libspecsteer_loss.so")
 CALLS_SOURCES = [os.path.join(_PKG, "csrc", "calls.cpp"), os.path.join(_PKG, "csrc", "unbound.h"), os.path.join(INCLUDE, "specsteer.h")]
 
 HIPCC_FLAGS = [
@@ -36,6 +38,7 @@ def _run(cmd: list, verbose: bool) -> None:
 
 def build(verbose: bool = False) -> str:
     build_library(verbose)
+    build_loss_library(verbose)
     build_calls(verbose)
     return LIBRARY
 
@@ -44,6 +47,13 @@ def build_library(verbose: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     _run([hipcc, *HIPCC_FLAGS, "-I", INCLUDE, "-o", LIBRARY, *SOURCES], verbose)
     return LIBRARY
+
+
+def build_loss_library(verbose: bool = False) -> str:
+    """The losses, a library of their own: who only verifies loads none of their kernels."""
+    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+    _run([hipcc, *HIPCC_FLAGS, "-I", INCLUDE, "-o", LOSS_LIBRARY, *LOSS_SOURCES], verbose)
+    return LOSS_LIBRARY
 
 
 def calls_path() -> str:

@@ -1,0 +1,898 @@
+// The losses over full-vocabulary logits for MI355X (gfx950); include/specsteer_loss.h says what they compute.
+//
+// Every one of them is passes over rows of V logits.  With c = log2(e) / tau, a whole number E near the largest h_v c, and
+//     s = sum_v 2^(h_v c - E),
+// a token's log-prob is (h_y c - E - log2 s) ln 2 and every gradient of a loss of log-probs is, in the row's logits,
+//     dL/dh_v = (g / tau) (1[v = y] - 2^(h_v c - E) / s),    g = dL/dlp.
+// A whole-vocabulary KL to a reference with logits z takes, in the same pass, sum_v 2^(h_v c - E) (h_v - z_v) and the
+// reference's own (E', s'):  KL = E[h - z] / tau - D with D = log-sum-exp(h) - log-sum-exp(z), and adds
+//     (k / tau) P(v) ((h_v - z_v) / tau - D - KL)     to the gradient.
+// A whole E makes moving a sum to another reference exact.  Terms and a lane's sums are fp32; what is formed once a row (log-probs, KL,
+// weights, losses) is double.  Sums of hundreds of log-probs with either sign are small beside their terms, so an error that all rows
+// share counts: c goes into the sums' exponents in two parts, rounded to one it left 6e-8 a token, 1e-5 of a margin over 16 pairs of 1024.
+//
+// Rows whose largest |h c| is beyond 2^20, rows of the type's lowest value among them, take a sweep of their own that subtracts
+// the maximum first (far_row).
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+#include <cstdint>
+#include <type_traits>
+
+#include "../device_common.h"
+#include "loss_plan.h"
+#include "specsteer_loss.h"
+
+namespace {
+
+// E lies this far under the largest h c, rounded up: an exponent is rounded to 2^-24 of itself, and the terms that carry a sum, mostly within 8 of
+// the largest, have small ones then.
+constexpr float kBelow = 4.f;
+constexpr float kFar = 1048576.f;  // |E| up to which a row is summed by exponents
+constexpr double kLn2 = 0.6931471805599453;
+
+template <int DT> struct Row;
+template <> struct Row<SS_BF16> { static constexpr int kVec = 8; using Raw = uint4; };
+template <> struct Row<SS_F32> { static constexpr int kVec = 4; using Raw = float4; };
+
+// A row as whole vectors between the elements before the first 16-byte boundary and those behind the last: vectors are
+// aligned in `aligned_to` (the gradient's row where there is one, since stores pay more for it than loads), and a lane has at most one
+// of the other elements.
+template <int DT>
+struct Layout {
+    int head, vecs, extra;  // extra: the lane's element outside of the vectors, or -1
+    __device__ __forceinline__ Layout(const void* aligned_to, int V, int tid) {
+        constexpr int kVec = Row<DT>::kVec, kElem = DT == SS_BF16 ? 2 : 4;
+        const int off = (int)(reinterpret_cast<uintptr_t>(aligned_to) & 15);
+        head = min(V, ((16 - off) & 15) / kElem);
+        vecs = (V - head) / kVec;
+        const int tail = V - head - vecs * kVec;
+        extra = tid < head ? tid : tid >= 8 && tid < 8 + tail ? V - tail + tid - 8 : -1;
+    }
+};
+
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+
+template <int DT>
+__device__ __forceinline__ typename Row<DT>::Raw ld_vec(const void* p, long vec) {
+    if constexpr (DT == SS_BF16) {
+        const u32x4 t = reinterpret_cast<const u32x4*>(p)[vec];
+        return make_uint4(t.x, t.y, t.z, t.w);
+    } else {
+        const f32x4 t = reinterpret_cast<const f32x4*>(p)[vec];
+        return make_float4(t.x, t.y, t.z, t.w);
+    }
+}
+
+__device__ __forceinline__ unsigned bf16_bits(float x) {
+    const __bf16 b = (__bf16)x;  // to nearest, ties to even
+    return __builtin_bit_cast(unsigned short, b);
+}
+template <int DT>
+__device__ __forceinline__ void st_elem(void* row, long e, float x) {
+    if constexpr (DT == SS_BF16) reinterpret_cast<unsigned short*>(row)[e] = (unsigned short)bf16_bits(x);
+    else reinterpret_cast<float*>(row)[e] = x;
+}
+template <int DT>
+__device__ __forceinline__ void st_vec(void* p, long vec, const float (&h)[Row<DT>::kVec]) {
+    if constexpr (DT == SS_BF16) {
+        typedef unsigned int out_t __attribute__((ext_vector_type(4)));
+        out_t r;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r[i] = bf16_bits(h[2 * i]) | bf16_bits(h[2 * i + 1]) << 16;
+        reinterpret_cast<out_t*>(p)[vec] = r;
+    } else {
+        typedef float out_t __attribute__((ext_vector_type(4)));
+        out_t r = {h[0], h[1], h[2], h[3]};
+        reinterpret_cast<out_t*>(p)[vec] = r;
+    }
+}
+
+// ------------------------------------------------------------------ statistics of a row
+
+// c = log2(e) / tau in two fp32 parts, the first of 16 bits, so that a bf16 logit's product with it is exact; as one fp32 number and the
+// rest; and 1 / tau.
+struct Factor {
+    float hi, lo, whole, rest, inv_tau;
+};
+// 2^(h c - E)
+__device__ __forceinline__ float term(float h, float E, Factor c) { return exp2_hw(fmaf(h, c.lo, fmaf(h, c.hi, -E))); }
+
+// A running sum: the reference E and sum 2^(h c - E).
+struct Sum {
+    float E, s;
+};
+// The same with the cross term sum 2^(h c - E) (h - z) and the reference's own sum.
+struct SumRef {
+    float E, s, x, Ez, sz;
+};
+__device__ __forceinline__ void clear(Sum& a) { a.E = -kFar; a.s = 0.f; }
+__device__ __forceinline__ void clear(SumRef& a) { a.E = a.Ez = -kFar; a.s = a.x = a.sz = 0.f; }
+__device__ __forceinline__ float moved(float s, float from, float to) { return __builtin_ldexpf(s, (int)(from - to)); }
+
+template <int N>
+__device__ __forceinline__ void raise(float& E, float& s, float& x, const float (&h)[N], Factor c) {
+    float top = h[0];
+#pragma unroll
+    for (int i = 1; i < N; ++i) top = fmaxf(top, h[i]);
+    top = fmaf(top, c.hi, -kBelow);
+    if (top > E) {
+        const float to = fminf(ceilf(top), 2.f * kFar);
+        s = moved(s, E, to);
+        x = moved(x, E, to);
+        E = to;
+    }
+}
+template <int N>
+__device__ __forceinline__ float tree_sum(float (&e)[N]) {
+#pragma unroll
+    for (int w = N / 2; w > 0; w /= 2)
+#pragma unroll
+        for (int i = 0; i < w; ++i) e[i] += e[i + w];
+    return e[0];
+}
+template <int N>
+__device__ __forceinline__ void add(Sum& a, const float (&h)[N], Factor c) {
+    float none = 0.f, e[N];
+    raise(a.E, a.s, none, h, c);
+#pragma unroll
+    for (int i = 0; i < N; ++i) e[i] = term(h[i], a.E, c);
+    a.s += tree_sum(e);
+}
+template <int N>
+__device__ __forceinline__ void add(SumRef& a, const float (&h)[N], const float (&z)[N], Factor c) {
+    float none = 0.f, e[N], ez[N], x[N];
+    raise(a.E, a.s, a.x, h, c);
+    raise(a.Ez, a.sz, none, z, c);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        e[i] = term(h[i], a.E, c);
+        x[i] = e[i] > 0.f ? e[i] * (h[i] - z[i]) : 0.f;  // a token that the policy masks counts nothing, -inf - -inf among them
+        ez[i] = term(z[i], a.Ez, c);
+    }
+    a.s += tree_sum(e);
+    a.x += tree_sum(x);
+    a.sz += tree_sum(ez);
+}
+
+// The sums of a whole row.  Lanes' sums are added in double: their last few additions are not averaged over many, and were most of the
+// error of a log-sum (5e-8 by fp32 to the end).
+template <typename S> struct Total;
+template <> struct Total<Sum> {
+    float E;
+    double s;
+};
+template <> struct Total<SumRef> {
+    float E, Ez;
+    double s, x, sz;
+};
+// Whether sums by exponents hold for a row.  Lanes whose logits all lie further down (masked ones) have nothing in their sums.
+__device__ __forceinline__ bool is_far(float E) { return !(E > 256.f - kFar && E < kFar); }
+__device__ __forceinline__ bool is_far(const Total<Sum>& a) { return is_far(a.E); }
+__device__ __forceinline__ bool is_far(const Total<SumRef>& a) { return is_far(a.E) || is_far(a.Ez); }
+
+__device__ __forceinline__ double wave_sum_f64(double x) { return wave_last_f64(wave_incl_scan_f64(x)); }
+__device__ __forceinline__ double moved(double s, float from, float to) { return ldexp(s, (int)(from - to)); }
+
+__device__ __forceinline__ Total<Sum> wave_total(const Sum& a) {
+    Total<Sum> r;
+    r.E = (float)wave_max_i32((int)a.E);
+    r.s = wave_sum_f64((double)moved(a.s, a.E, r.E));
+    return r;
+}
+__device__ __forceinline__ Total<SumRef> wave_total(const SumRef& a) {
+    Total<SumRef> r;
+    r.E = (float)wave_max_i32((int)a.E);
+    r.Ez = (float)wave_max_i32((int)a.Ez);
+    r.s = wave_sum_f64((double)moved(a.s, a.E, r.E));
+    r.x = wave_sum_f64((double)moved(a.x, a.E, r.E));
+    r.sz = wave_sum_f64((double)moved(a.sz, a.Ez, r.Ez));
+    return r;
+}
+// n totals to one: lane i has the i-th if i < n (and any of them otherwise), n <= 64.  Every lane has the result.
+__device__ __forceinline__ Total<Sum> join(const Total<Sum>& a, int n) {
+    const bool has = (int)(threadIdx.x & 63) < n;
+    Total<Sum> r;
+    r.E = (float)wave_max_i32((int)a.E);
+    r.s = wave_sum_f64(has ? moved(a.s, a.E, r.E) : 0.0);
+    return r;
+}
+__device__ __forceinline__ Total<SumRef> join(const Total<SumRef>& a, int n) {
+    const bool has = (int)(threadIdx.x & 63) < n;
+    Total<SumRef> r;
+    r.E = (float)wave_max_i32((int)a.E);
+    r.Ez = (float)wave_max_i32((int)a.Ez);
+    r.s = wave_sum_f64(has ? moved(a.s, a.E, r.E) : 0.0);
+    r.x = wave_sum_f64(has ? moved(a.x, a.E, r.E) : 0.0);
+    r.sz = wave_sum_f64(has ? moved(a.sz, a.Ez, r.Ez) : 0.0);
+    return r;
+}
+// Over a workgroup; `part` is free again behind the next barrier.
+template <int THREADS, typename S>
+__device__ __forceinline__ Total<S> block_total(const S& a, Total<S>* part) {
+    constexpr int kWaves = THREADS / kWave;
+    const int lane = threadIdx.x & 63;
+    const Total<S> mine = wave_total(a);
+    if (lane == 0) part[threadIdx.x >> 6] = mine;
+    __syncthreads();
+    return join(part[lane & (kWaves - 1)], kWaves);
+}
+
+// ------------------------------------------------------------------ rows of a call
+
+struct Rows {
+    const void* logits;
+    const void* ref;       // or NULL
+    void* grad;            // or NULL
+    const int32_t* tokens;
+    const uint8_t* mask;   // or NULL
+    long rows, sb, st, gsb, gst;
+    int T, V;
+    Factor c;              // log2(e) / tau
+    double c64;
+    double inv_tau, scale; // 1 / tau, the gradient's factor
+};
+
+__device__ __forceinline__ bool counts(const Rows& a, long row) { return !a.mask || a.mask[row] != 0; }
+__device__ __forceinline__ void place(const Rows& a, long row, long& at, long& grad_at) {
+    const long b = (unsigned)row / (unsigned)a.T, t = row - b * a.T;
+    at = b * a.sb + t * a.st;
+    grad_at = b * a.gsb + t * a.gst;
+}
+
+template <int DT, int THREADS>
+__device__ __forceinline__ void zero_row(void* g, int V) {
+    const Layout<DT> lay(g, V, threadIdx.x);
+    const float none[Row<DT>::kVec] = {};
+    char* const base = static_cast<char*>(g) + (long)lay.head * (DT == SS_BF16 ? 2 : 4);
+    for (int i = threadIdx.x; i < lay.vecs; i += THREADS) st_vec<DT>(base, i, none);
+    if (lay.extra >= 0) st_elem<DT>(g, lay.extra, 0.f);
+}
+
+// One lane's share of a row: vectors [first, end) by step, and its extra element if `extra`.
+template <int DT, typename S>
+__device__ __forceinline__ S lane_sum(const void* h, const void* z, const Layout<DT>& lay, int first, int end, int step, bool extra, Factor c) {
+    constexpr int kVec = Row<DT>::kVec, kUnroll = 4, kElem = DT == SS_BF16 ? 2 : 4;
+    constexpr bool kRef = std::is_same<S, SumRef>::value;
+    S a;
+    clear(a);
+    const char* const hv = static_cast<const char*>(h) + (long)lay.head * kElem;
+    const char* const zv = kRef ? static_cast<const char*>(z) + (long)lay.head * kElem : nullptr;
+    const auto one = [&](const typename Row<DT>::Raw& r, const typename Row<DT>::Raw& rz) {
+        float x[kVec];
+        unpack(r, x);
+        if constexpr (kRef) {
+            float y[kVec];
+            unpack(rz, y);
+            add(a, x, y, c);
+        } else {
+            add(a, x, c);
+        }
+    };
+    int i = first;
+    for (; i + (kUnroll - 1) * step < end; i += kUnroll * step) {
+        typename Row<DT>::Raw r[kUnroll], rz[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            r[u] = ld_vec<DT>(hv, i + u * step);
+            if constexpr (kRef) rz[u] = ld_vec<DT>(zv, i + u * step);
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) one(r[u], rz[u]);
+    }
+    for (; i < end; i += step) {
+        typename Row<DT>::Raw r = ld_vec<DT>(hv, i), rz = r;
+        if constexpr (kRef) rz = ld_vec<DT>(zv, i);
+        one(r, rz);
+    }
+    if (extra && lay.extra >= 0) {
+        const float x[1] = {ld_elem<DT>(h, lay.extra)};
+        if constexpr (kRef) {
+            const float y[1] = {ld_elem<DT>(z, lay.extra)};
+            add(a, x, y, c);
+        } else {
+            add(a, x, c);
+        }
+    }
+    return a;
+}
+
+// ------------------------------------------------------------------ rows far from zero
+
+// The sums of a row with its largest logit m for a reference: E = m and s = sum 2^((h - m) c), element by element over a workgroup.
+// Differences are exact where they matter, so that this holds for any finite row (of lowest values only: a uniform one).
+template <int DT, int THREADS, typename S>
+__device__ __forceinline__ Total<S> far_sum(const void* h, const void* z, int V, Factor c, Total<S>* part) {
+    constexpr bool kRef = std::is_same<S, SumRef>::value;
+    constexpr int kWaves = THREADS / kWave;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    float m = -__builtin_huge_valf(), mz = m;
+    for (int i = threadIdx.x; i < V; i += THREADS) {
+        m = fmaxf(m, ld_elem<DT>(h, i));
+        if constexpr (kRef) mz = fmaxf(mz, ld_elem<DT>(z, i));
+    }
+    const auto all_max = [&](float v) {
+        for (int d = 1; d < kWave; d <<= 1) v = fmaxf(v, __shfl_xor(v, d, kWave));
+        __syncthreads();
+        if (lane == 0) part[wave].E = v;
+        __syncthreads();
+        v = part[lane & (kWaves - 1)].E;
+        for (int d = 1; d < kWaves; d <<= 1) v = fmaxf(v, __shfl_xor(v, d, kWave));
+        return v;
+    };
+    Total<S> a;
+    a.E = m = all_max(m);
+    if constexpr (kRef) a.Ez = mz = all_max(mz);
+    double s = 0.0, x = 0.0, sz = 0.0;
+    for (int i = threadIdx.x; i < V; i += THREADS) {
+        const float hv = ld_elem<DT>(h, i), e = exp2_hw((hv - m) * c.whole);
+        s += (double)e;
+        if constexpr (kRef) {
+            const float zv = ld_elem<DT>(z, i);
+            x += e > 0.f ? (double)e * ((double)hv - (double)zv) : 0.0;
+            sz += (double)exp2_hw((zv - mz) * c.whole);
+        }
+    }
+    const auto all_sum = [&](double v) {
+        v = wave_sum_f64(v);
+        __syncthreads();
+        if (lane == 0) part[wave].s = v;
+        __syncthreads();
+        return wave_sum_f64(lane < kWaves ? part[lane].s : 0.0);
+    };
+    a.s = all_sum(s);
+    if constexpr (kRef) {
+        a.x = all_sum(x);
+        a.sz = all_sum(sz);
+    }
+    __syncthreads();
+    return a;
+}
+
+// What the gradient of a row needs: dL/dh_v = e (scale + cross (h_v - z_v) / tau) + at_token 1[v = y], e = 2^(h_v c - E), or 2^((h_v - m) c) with
+// the maximum m in E for a row far from zero
+struct RowGrad {
+    float E, scale, cross, at_token;
+};
+
+// g = weight of the row's log-prob, k that of its KL, both with the call's factor; diff = D, the difference of the log-sum-exps.
+// bf16 gradients are formed with c as one number: what its rest adds at the reference goes into the factor here, and the rest is below
+// 2^-24 of |h c - E|, which half a step of the result is thousands of times.
+template <int DT, bool REF>
+__device__ __forceinline__ RowGrad row_grad(const Rows& a, bool far, float E, double s, double g, double k, double diff, double kl) {
+    RowGrad r;
+    double f = a.inv_tau / s;
+    if (DT == SS_BF16 && !far) f *= (double)exp2_hw(E * (a.c.rest / a.c.whole));
+    r.E = E;
+    r.scale = (float)((REF ? -g - k * (diff + kl) : -g) * f);
+    r.cross = REF ? (float)(k * f) : 0.f;
+    r.at_token = (float)(g * a.inv_tau);
+    return r;
+}
+
+template <bool REF>
+__device__ __forceinline__ float grad_of_term(const RowGrad& r, float e, float h, float z, Factor c) {
+    if constexpr (REF) return e > 0.f ? e * fmaf(r.cross, (h - z) * c.inv_tau, r.scale) : 0.f * r.scale;
+    return e * r.scale;
+}
+template <int DT, bool REF>
+__device__ __forceinline__ float grad_of(const RowGrad& r, float h, float z, Factor c) {
+    return grad_of_term<REF>(r, DT == SS_BF16 ? exp2_hw(fmaf(h, c.whole, -r.E)) : term(h, r.E, c), h, z, c);
+}
+
+// The gradient of a row far from zero, element by element over a workgroup.
+template <int DT, bool REF, int THREADS>
+__device__ __forceinline__ void far_grad(const void* h, const void* z, void* g, int V, const RowGrad& r, int token, Factor c) {
+    for (int i = threadIdx.x; i < V; i += THREADS) {
+        const float hv = ld_elem<DT>(h, i), zv = REF ? ld_elem<DT>(z, i) : 0.f;
+        st_elem<DT>(g, i, grad_of_term<REF>(r, exp2_hw((hv - r.E) * c.whole), hv, zv, c) + (i == token ? r.at_token : 0.f));
+    }
+}
+
+// Vectors [first, end) by step, and the lane's extra element if `extra`, of a row's gradient.  The lane that owns the token's element
+// writes it again: its logit is read before anything of the row is overwritten.
+template <int DT, bool REF>
+__device__ __forceinline__ void write_grad(const void* h, const void* z, void* g, const Layout<DT>& lay, const RowGrad& r, int token, int first,
+                                           int end, int step, bool extra, Factor c) {
+    constexpr int kVec = Row<DT>::kVec, kElem = DT == SS_BF16 ? 2 : 4, kUnroll = 4;
+    const char* const hv = static_cast<const char*>(h) + (long)lay.head * kElem;
+    const char* const zv = REF ? static_cast<const char*>(z) + (long)lay.head * kElem : nullptr;
+    char* const gv = static_cast<char*>(g) + (long)lay.head * kElem;
+    const int at = token - lay.head, vec = at >= 0 && at < lay.vecs * kVec ? at / kVec : -1;
+    // lanes without an extra element have -1 there, which a token outside of the vocabulary may be too
+    const bool mine = vec >= 0 ? vec >= first && vec < end && (vec - first) % step == 0 : extra && token >= 0 && lay.extra == token;
+    float mine_h = 0.f, mine_z = 0.f;
+    if (mine) {
+        mine_h = ld_elem<DT>(h, token);
+        if constexpr (REF) mine_z = ld_elem<DT>(z, token);
+    }
+    const auto one = [&](const typename Row<DT>::Raw& raw, const typename Row<DT>::Raw& rawz, int i) {
+        float x[kVec], y[kVec];
+        unpack(raw, x);
+        if constexpr (REF) unpack(rawz, y);
+#pragma unroll
+        for (int j = 0; j < kVec; ++j) x[j] = grad_of<DT, REF>(r, x[j], REF ? y[j] : 0.f, c);
+        st_vec<DT>(gv, i, x);
+    };
+    int i = first;
+    for (; i + (kUnroll - 1) * step < end; i += kUnroll * step) {
+        typename Row<DT>::Raw raw[kUnroll], rawz[kUnroll];
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            raw[u] = ld_vec<DT>(hv, i + u * step);
+            if constexpr (REF) rawz[u] = ld_vec<DT>(zv, i + u * step);
+        }
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) one(raw[u], rawz[u], i + u * step);
+    }
+    for (; i < end; i += step) {
+        const typename Row<DT>::Raw raw = ld_vec<DT>(hv, i);
+        if constexpr (REF) one(raw, ld_vec<DT>(zv, i), i);
+        else one(raw, raw, i);
+    }
+    if (extra && lay.extra >= 0)
+        st_elem<DT>(g, lay.extra, grad_of<DT, REF>(r, ld_elem<DT>(h, lay.extra), REF ? ld_elem<DT>(z, lay.extra) : 0.f, c));
+    if (mine) {
+        asm volatile("" ::: "memory");  // behind the stores above, which cover this element too
+        st_elem<DT>(g, token, r.at_token + grad_of<DT, REF>(r, mine_h, mine_z, c));
+    }
+}
+
+__device__ __forceinline__ double nan64() { return __longlong_as_double(0x7FF8000000000000ll); }
+// log P(y) of a row's token with logit h, from the row's sums
+__device__ __forceinline__ double token_logprob(const Rows& a, bool far, int token, float h, float E, double s) {
+    if (token < 0 || token >= a.V) return nan64();
+    if (far) return ((double)h - (double)E) * a.inv_tau - log(s);
+    return ((double)h * a.c64 - (double)E - log2(s)) * kLn2;
+}
+// log-sum-exp of the policy's row less that of the reference's
+__device__ __forceinline__ double lse_difference(const Rows& a, bool far, const Total<SumRef>& s) {
+    const double sums = log2(s.s) - log2(s.sz), by = (double)s.E - (double)s.Ez;
+    return far ? by * a.inv_tau + sums * kLn2 : (by + sums) * kLn2;
+}
+
+// ------------------------------------------------------------------ token log-probs
+
+constexpr int kRowThreads = 512;
+
+struct ScoreArgs {
+    Rows r;
+    float* logprobs;    // or NULL
+    float* stats;       // or NULL
+    double* logprob64;  // or NULL
+};
+
+// One workgroup a row.  In the statistics a row far from zero has the negative of its sum.
+template <int DT>
+__global__ __launch_bounds__(kRowThreads) void score_kernel(const ScoreArgs a) {
+    __shared__ Total<Sum> part[kRowThreads / kWave];
+    for (long row = blockIdx.x; row < a.r.rows; row += gridDim.x) {
+        double lp = 0.0;
+        Total<Sum> s = {0.f, 1.0};
+        if (counts(a.r, row)) {
+            long at, grad_at;
+            place(a.r, row, at, grad_at);
+            const void* const h = row_ptr<DT>(a.r.logits, at);
+            const Layout<DT> lay(h, a.r.V, threadIdx.x);
+            s = block_total<kRowThreads>(lane_sum<DT, Sum>(h, nullptr, lay, threadIdx.x, lay.vecs, kRowThreads, true, a.r.c), part);
+            const bool far = is_far(s);
+            if (far) s = far_sum<DT, kRowThreads, Sum>(h, nullptr, a.r.V, a.r.c, part);
+            if (threadIdx.x == 0) {
+                const int y = a.r.tokens[row];
+                lp = token_logprob(a.r, far, y, y >= 0 && y < a.r.V ? ld_elem<DT>(h, y) : 0.f, s.E, s.s);
+                if (far) s.s = -s.s;
+            }
+        }
+        if (threadIdx.x == 0) {
+            if (a.logprobs) a.logprobs[row] = (float)lp;
+            if (a.logprob64) a.logprob64[row] = lp;
+            if (a.stats) {
+                a.stats[2 * row] = s.E;
+                a.stats[2 * row + 1] = (float)s.s;
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// ------------------------------------------------------------------ gradient from known statistics
+
+struct GradArgs {
+    Rows r;
+    const float* stats;
+    const float* weight;      // of every row's log-prob, or NULL:
+    const double* seq_weight; // of the first P sequences' log-probs, the other P have the negative
+    int pairs;
+};
+
+template <int DT>
+__global__ __launch_bounds__(kRowThreads) void grad_kernel(const GradArgs a) {
+    for (long row = blockIdx.x; row < a.r.rows; row += gridDim.x) {
+        long at, grad_at;
+        place(a.r, row, at, grad_at);
+        void* const g = const_cast<void*>(row_ptr<DT>(a.r.grad, grad_at));
+        if (!counts(a.r, row)) {
+            zero_row<DT, kRowThreads>(g, a.r.V);
+            continue;
+        }
+        const void* const h = row_ptr<DT>(a.r.logits, at);
+        const int y = a.r.tokens[row], b = (int)((unsigned)row / (unsigned)a.r.T);
+        double w = a.weight ? (double)a.weight[row] : b < a.pairs ? a.seq_weight[b] : -a.seq_weight[b - a.pairs];
+        w *= a.r.scale;
+        if (y < 0 || y >= a.r.V) w = nan64();
+        const float s = a.stats[2 * row + 1];
+        const bool far = s < 0.f;
+        const RowGrad rg = row_grad<DT, false>(a.r, far, a.stats[2 * row], fabsf(s), w, 0.0, 0.0, 0.0);
+        if (far) {
+            far_grad<DT, false, kRowThreads>(h, nullptr, g, a.r.V, rg, y, a.r.c);
+            continue;
+        }
+        const Layout<DT> lay(g, a.r.V, threadIdx.x);
+        write_grad<DT, false>(h, nullptr, g, lay, rg, y, threadIdx.x, lay.vecs, kRowThreads, true, a.r.c);
+    }
+}
+
+// ------------------------------------------------------------------ policy loss
+
+struct PolicyArgs {
+    Rows r;
+    const float* old_logprobs;
+    const float* ref_logprobs;  // or NULL
+    const float* advantages;
+    const double* norm;  // what a token of each sequence counts, or NULL: norm_all
+    double norm_all;
+    double clip_lo, clip_hi, kl_coef;
+    int seq_advantages;
+    float* logprobs;  // or NULL
+    float* kl;        // or NULL
+    double* terms;    // every row's share of the loss
+};
+
+struct RowLoss {
+    double lp, kl, term, g, k, diff;
+};
+
+template <bool REF, typename S>
+__device__ __forceinline__ RowLoss row_loss(const PolicyArgs& a, bool far, long row, int y, float hy, const Total<S>& s) {
+    RowLoss o;
+    const int b = (int)((unsigned)row / (unsigned)a.r.T);
+    const double adv = a.advantages[a.seq_advantages ? b : row], n = a.norm ? a.norm[b] : a.norm_all;
+    o.lp = token_logprob(a.r, far, y, hy, s.E, s.s);
+    o.kl = o.k = o.diff = 0.0;
+    const double ratio = exp(o.lp - (double)a.old_logprobs[row]);
+    const double plain = ratio * adv, bound = fmin(fmax(ratio, a.clip_lo), a.clip_hi) * adv;
+    const bool clipped = plain > bound;  // NaN: not clipped, and NaN below
+    o.term = clipped ? -bound : -plain;
+    o.g = clipped ? 0.0 : -plain;
+    if constexpr (REF) {
+        o.diff = lse_difference(a.r, far, s);
+        o.kl = s.x / s.s * a.r.inv_tau - o.diff;
+        if (o.kl < 0.0) o.kl = 0.0;  // by rounding only
+        o.k = a.kl_coef;
+    } else if (a.ref_logprobs) {
+        const double d = (double)a.ref_logprobs[row] - o.lp, e = expm1(d);
+        o.kl = e - d;
+        if (a.kl_coef != 0.0) o.g -= a.kl_coef * e;
+    }
+    if (a.kl_coef != 0.0) o.term += a.kl_coef * o.kl;
+    o.term *= n;
+    o.g *= n * a.r.scale;
+    o.k *= n * a.r.scale;
+    return o;
+}
+
+template <int DT, bool REF>
+__global__ __launch_bounds__(kRowThreads) void policy_kernel(const PolicyArgs a) {
+    using S = typename std::conditional<REF, SumRef, Sum>::type;
+    __shared__ Total<S> part[kRowThreads / kWave];
+    __shared__ RowGrad shared_grad;
+    for (long row = blockIdx.x; row < a.r.rows; row += gridDim.x) {
+        long at, grad_at;
+        place(a.r, row, at, grad_at);
+        void* const g = a.r.grad ? const_cast<void*>(row_ptr<DT>(a.r.grad, grad_at)) : nullptr;
+        if (!counts(a.r, row)) {
+            if (g) zero_row<DT, kRowThreads>(g, a.r.V);
+            if (threadIdx.x == 0) {
+                if (a.logprobs) a.logprobs[row] = 0.f;
+                if (a.kl) a.kl[row] = 0.f;
+                a.terms[row] = 0.0;
+            }
+            continue;
+        }
+        const void* const h = row_ptr<DT>(a.r.logits, at);
+        const void* const z = REF ? row_ptr<DT>(a.r.ref, at) : nullptr;
+        const Layout<DT> lay(g ? g : h, a.r.V, threadIdx.x);
+        const int y = a.r.tokens[row];
+        Total<S> s = block_total<kRowThreads>(lane_sum<DT, S>(h, z, lay, threadIdx.x, lay.vecs, kRowThreads, true, a.r.c), part);
+        const bool far = is_far(s);
+        if (far) s = far_sum<DT, kRowThreads, S>(h, z, a.r.V, a.r.c, part);
+        if (threadIdx.x == 0) {
+            const RowLoss o = row_loss<REF>(a, far, row, y, y >= 0 && y < a.r.V ? ld_elem<DT>(h, y) : 0.f, s);
+            if (a.logprobs) a.logprobs[row] = (float)o.lp;
+            if (a.kl) a.kl[row] = (float)o.kl;
+            a.terms[row] = o.term;
+            shared_grad = row_grad<DT, REF>(a.r, far, s.E, s.s, o.g, o.k, o.diff, o.kl);
+        }
+        __syncthreads();
+        if (g) {
+            const RowGrad rg = shared_grad;
+            if (far) far_grad<DT, REF, kRowThreads>(h, z, g, a.r.V, rg, y, a.r.c);
+            else write_grad<DT, REF>(h, z, g, lay, rg, y, threadIdx.x, lay.vecs, kRowThreads, true, a.r.c);
+        }
+        __syncthreads();
+    }
+}
+
+// ------------------------------------------------------------------ what is formed once a call
+
+constexpr int kOneThreads = 1024;
+
+// The sum of x over the workgroup, in every lane of wave 0.  The order is fixed.
+__device__ __forceinline__ double block_sum(double x, double* part) {
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) x += __shfl_xor(x, d, kWave);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (lane == 0) part[wave] = x;
+    __syncthreads();
+    x = lane < (int)blockDim.x / kWave ? part[lane] : 0.0;
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) x += __shfl_xor(x, d, kWave);
+    __syncthreads();
+    return x;
+}
+
+// What a token of each sequence counts for the mean over tokens or over sequences: one workgroup, a wave a sequence.
+__global__ __launch_bounds__(kOneThreads) void norm_kernel(const uint8_t* mask, int B, int T, int seq_mean, double* norm) {
+    __shared__ double part[kOneThreads / kWave];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    double all = 0.0;  // tokens, or sequences that have any
+    for (int b = wave; b < B; b += kOneThreads / kWave) {
+        int n = 0;
+        for (int t = lane; t < T; t += kWave) n += mask[(long)b * T + t] != 0 ? 1 : 0;
+        n = wave_sum_i32(n);
+        if (lane == 0) {
+            norm[b] = (double)n;
+            all += seq_mean ? (n > 0 ? 1.0 : 0.0) : (double)n;
+        }
+    }
+    all = block_sum(all, part);
+    for (int b = threadIdx.x; b < B; b += kOneThreads) {
+        const double n = norm[b];
+        norm[b] = n == 0.0 ? 0.0 : seq_mean ? 1.0 / (n * all) : 1.0 / all;
+    }
+}
+
+__global__ __launch_bounds__(kOneThreads) void sum_kernel(const double* terms, long n, double factor, float* loss) {
+    __shared__ double part[kOneThreads / kWave];
+    double x = 0.0;
+    for (long i = threadIdx.x; i < n; i += kOneThreads) x += terms[i];
+    x = block_sum(x, part);
+    if (threadIdx.x == 0) *loss = (float)(x * factor);
+}
+
+struct PairArgs {
+    const double* logprob64;
+    const float* ref_logprobs;  // or NULL
+    const uint8_t* mask;        // or NULL
+    int pairs, T;
+    double beta, smoothing, factor;  // factor: what a pair counts
+    double* weight;  // [P] out: of the preferred sequence's log-probs
+    double* loss64;  // [P] out
+    float* loss;     // [P] out, or NULL
+    float* margin;   // [P] out, or NULL
+};
+
+__device__ __forceinline__ double softplus(double x) { return fmax(x, 0.0) + log1p(exp(-fabs(x))); }
+
+constexpr int kPairThreads = 256;
+
+__global__ __launch_bounds__(kPairThreads) void pair_kernel(const PairArgs a) {
+    __shared__ double part[kPairThreads / kWave];
+    const long p = blockIdx.x;
+    double x = 0.0;
+    for (int side = 0; side < 2; ++side) {
+        const long at = (p + (side ? a.pairs : 0)) * (long)a.T;
+        for (int t = threadIdx.x; t < a.T; t += kPairThreads) {
+            if (a.mask && a.mask[at + t] == 0) continue;
+            const double d = a.logprob64[at + t] - (a.ref_logprobs ? (double)a.ref_logprobs[at + t] : 0.0);
+            x += side ? -d : d;
+        }
+    }
+    x = block_sum(x, part);
+    if (threadIdx.x == 0) {
+        const double h = a.beta * x, e = a.smoothing;
+        const double loss = (1.0 - e) * softplus(-h) + e * softplus(h);
+        const double dh = (e - 1.0) / (1.0 + exp(h)) + e / (1.0 + exp(-h));
+        a.weight[p] = a.beta * a.factor * dh;
+        a.loss64[p] = loss;
+        if (a.loss) a.loss[p] = (float)loss;
+        if (a.margin) a.margin[p] = (float)h;
+    }
+}
+
+__global__ void zero_loss_kernel(float* loss) { *loss = 0.f; }
+
+// ------------------------------------------------------------------ launches
+
+constexpr long kMaxGrid = 1 << 20;
+
+unsigned row_grid(long rows) { return (unsigned)(rows < kMaxGrid ? rows : kMaxGrid); }
+
+Rows make_rows(const void* logits, const void* ref, void* grad, const int32_t* tokens, const uint8_t* mask, const ss_loss_params& p,
+               const LossShape& s) {
+    Rows r;
+    r.logits = logits;
+    r.ref = ref;
+    r.grad = grad;
+    r.tokens = tokens;
+    r.mask = mask;
+    r.rows = s.rows;
+    r.sb = s.sb;
+    r.st = s.st;
+    r.gsb = s.gsb;
+    r.gst = s.gst;
+    r.T = p.length;
+    r.V = p.vocab;
+    r.c64 = 1.4426950408889634 / (double)p.temperature;
+    int e;
+    const double frac = std::frexp(r.c64, &e);  // 0.5 .. 1
+    r.c.hi = (float)std::ldexp(std::nearbyint(std::ldexp(frac, 16)), e - 16);
+    r.c.lo = (float)(r.c64 - (double)r.c.hi);
+    r.c.whole = (float)r.c64;
+    r.c.rest = (float)(r.c64 - (double)r.c.whole);
+    r.c.inv_tau = (float)(1.0 / (double)p.temperature);
+    r.inv_tau = 1.0 / (double)p.temperature;
+    r.scale = (double)p.grad_scale;
+    return r;
+}
+
+bool off_element(const void* p, const ss_loss_params& q) { return (reinterpret_cast<uintptr_t>(p) & (q.dtype == SS_BF16 ? 1 : 3)) != 0; }
+
+ss_status check_workspace(const void* workspace, size_t bytes, size_t need) {
+    return workspace && (reinterpret_cast<uintptr_t>(workspace) & 255) == 0 && bytes >= need ? SS_OK : SS_ERR_WORKSPACE;
+}
+
+ss_status launched() { return hipGetLastError() == hipSuccess ? SS_OK : SS_ERR_DEVICE; }
+
+template <typename A>
+void launch_rows(void (*bf16)(A), void (*f32)(A), const ss_loss_params& p, const A& a, hipStream_t s) {
+    launch(p.dtype == SS_BF16 ? bf16 : f32, dim3(row_grid(a.r.rows)), dim3(kRowThreads), 0, s, a);
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t specsteer_loss_workspace_bytes(const ss_loss_params* params) {
+    LossShape s;
+    return loss_shape(params, s) == SS_OK ? loss_scratch(*params).bytes : 0;
+}
+
+ss_status specsteer_token_logprobs(const void* logits, const int32_t* tokens, const uint8_t* mask, const ss_loss_params* params,
+                                   float* logprobs, float* stats, void* workspace, size_t workspace_bytes, void* stream) {
+    LossShape s;
+    const ss_status chk = loss_shape(params, s);
+    if (chk != SS_OK) return chk;
+    if (s.rows == 0) return SS_OK;
+    if (!logits || !tokens || !logprobs) return SS_ERR_NULL;
+    if (off_element(logits, *params)) return SS_ERR_STRIDE;
+    if (check_workspace(workspace, workspace_bytes, loss_scratch(*params).bytes) != SS_OK) return SS_ERR_WORKSPACE;
+    ScoreArgs a{make_rows(logits, nullptr, nullptr, tokens, mask, *params, s), logprobs, stats, nullptr};
+    launch_rows(score_kernel<SS_BF16>, score_kernel<SS_F32>, *params, a, static_cast<hipStream_t>(stream));
+    return launched();
+}
+
+ss_status specsteer_token_logprobs_grad(const void* logits, const int32_t* tokens, const uint8_t* mask, const float* stats,
+                                        const float* grad_logprobs, const ss_loss_params* params, void* grad_logits, void* stream) {
+    LossShape s;
+    const ss_status chk = loss_shape(params, s);
+    if (chk != SS_OK) return chk;
+    if (s.rows == 0) return SS_OK;
+    if (!logits || !tokens || !stats || !grad_logprobs || !grad_logits) return SS_ERR_NULL;
+    if (off_element(logits, *params) || off_element(grad_logits, *params)) return SS_ERR_STRIDE;
+    GradArgs a{make_rows(logits, nullptr, grad_logits, tokens, mask, *params, s), stats, grad_logprobs, nullptr, 0};
+    launch_rows(grad_kernel<SS_BF16>, grad_kernel<SS_F32>, *params, a, static_cast<hipStream_t>(stream));
+    return launched();
+}
+
+ss_status specsteer_policy_loss(const void* logits, const void* ref_logits, const int32_t* tokens, const uint8_t* mask,
+                                const float* old_logprobs, const float* ref_logprobs, const float* advantages,
+                                const ss_loss_params* params, const ss_policy_params* policy, float* loss, float* logprobs, float* kl,
+                                void* grad_logits, void* workspace, size_t workspace_bytes, void* stream) {
+    LossShape s;
+    ss_status chk = loss_shape(params, s);
+    if (chk == SS_OK) chk = check_policy(policy);
+    if (chk != SS_OK) return chk;
+    if (!loss || (s.rows > 0 && (!logits || !tokens || !old_logprobs || !advantages))) return SS_ERR_NULL;
+    if (ref_logits && ref_logprobs) return SS_ERR_PARAM;
+    if (s.rows > 0 && (policy->kl_coef > 0.f || kl) && !ref_logits && !ref_logprobs) return SS_ERR_NULL;
+    if (off_element(logits, *params) || off_element(ref_logits, *params) || off_element(grad_logits, *params)) return SS_ERR_STRIDE;
+    const LossScratch w = loss_scratch(*params);
+    if (check_workspace(workspace, workspace_bytes, w.bytes) != SS_OK) return SS_ERR_WORKSPACE;
+    hipStream_t q = static_cast<hipStream_t>(stream);
+    if (s.rows == 0) {
+        launch(zero_loss_kernel, dim3(1), dim3(1), 0, q, loss);
+        return launched();
+    }
+    PolicyArgs a;
+    a.r = make_rows(logits, ref_logits, grad_logits, tokens, mask, *params, s);
+    a.old_logprobs = old_logprobs;
+    a.ref_logprobs = ref_logprobs;
+    a.advantages = advantages;
+    a.norm = nullptr;
+    a.norm_all = (policy->flags & SS_LOSS_SUM) ? 1.0 : 1.0 / (double)s.rows;  // without a mask both means are this one
+    a.clip_lo = 1.0 - (double)policy->clip_low;
+    a.clip_hi = 1.0 + (double)policy->clip_high;
+    a.kl_coef = (double)policy->kl_coef;
+    a.seq_advantages = (policy->flags & SS_LOSS_SEQ_ADVANTAGES) ? 1 : 0;
+    a.logprobs = logprobs;
+    a.kl = kl;
+    char* const base = static_cast<char*>(workspace);
+    a.terms = reinterpret_cast<double*>(base + w.row_value);
+    if (mask && !(policy->flags & SS_LOSS_SUM)) {
+        double* const norm = reinterpret_cast<double*>(base + w.seq);
+        launch(norm_kernel, dim3(1), dim3(kOneThreads), 0, q, mask, (int)params->batch, (int)params->length,
+               (policy->flags & SS_LOSS_SEQ_MEAN) ? 1 : 0, norm);
+        a.norm = norm;
+    }
+    if (ref_logits) launch_rows(policy_kernel<SS_BF16, true>, policy_kernel<SS_F32, true>, *params, a, q);
+    else launch_rows(policy_kernel<SS_BF16, false>, policy_kernel<SS_F32, false>, *params, a, q);
+    launch(sum_kernel, dim3(1), dim3(kOneThreads), 0, q, static_cast<const double*>(a.terms), s.rows, 1.0, loss);
+    return launched();
+}
+
+ss_status specsteer_preference_loss(const void* logits, const int32_t* tokens, const uint8_t* mask, const float* ref_logprobs,
+                                    const ss_loss_params* params, const ss_preference_params* preference, float* loss, float* pair_loss,
+                                    float* margin, float* logprobs, void* grad_logits, void* workspace, size_t workspace_bytes,
+                                    void* stream) {
+    LossShape s;
+    ss_status chk = loss_shape(params, s);
+    if (chk == SS_OK) chk = check_preference(preference);
+    if (chk != SS_OK) return chk;
+    if (params->batch & 1) return SS_ERR_SHAPE;
+    if (!loss || (s.rows > 0 && (!logits || !tokens))) return SS_ERR_NULL;
+    if (off_element(logits, *params) || off_element(grad_logits, *params)) return SS_ERR_STRIDE;
+    const LossScratch w = loss_scratch(*params);
+    if (check_workspace(workspace, workspace_bytes, w.bytes) != SS_OK) return SS_ERR_WORKSPACE;
+    hipStream_t q = static_cast<hipStream_t>(stream);
+    const int pairs = params->batch / 2;
+    if (pairs == 0) {
+        launch(zero_loss_kernel, dim3(1), dim3(1), 0, q, loss);
+        return launched();
+    }
+    char* const base = static_cast<char*>(workspace);
+    double* const lp64 = reinterpret_cast<double*>(base + w.row_value);
+    float* const stats = reinterpret_cast<float*>(base + w.stats);
+    double *const weight = reinterpret_cast<double*>(base + w.seq), *const loss64 = weight + pairs;
+    const Rows r = make_rows(logits, nullptr, grad_logits, tokens, mask, *params, s);
+    if (s.rows > 0) {
+        ScoreArgs a{r, logprobs, stats, lp64};
+        launch_rows(score_kernel<SS_BF16>, score_kernel<SS_F32>, *params, a, q);
+    }
+    const double factor = (preference->flags & SS_LOSS_SUM) ? 1.0 : 1.0 / (double)pairs;
+    PairArgs pa{lp64, ref_logprobs, mask, pairs, params->length, (double)preference->beta, (double)preference->label_smoothing, factor,
+                weight, loss64, pair_loss, margin};
+    launch(pair_kernel, dim3((unsigned)pairs), dim3(kPairThreads), 0, q, pa);
+    if (grad_logits && s.rows > 0) {
+        GradArgs a{r, stats, nullptr, weight, pairs};
+        launch_rows(grad_kernel<SS_BF16>, grad_kernel<SS_F32>, *params, a, q);
+    }
+    launch(sum_kernel, dim3(1), dim3(kOneThreads), 0, q, static_cast<const double*>(loss64), (long)pairs, factor, loss);
+    return launched();
+}
+
+const char* specsteer_loss_status_string(int status) {
+    switch (status) {
+        case SS_OK: return "ok";
+        case SS_ERR_NULL: return "a required pointer is NULL";
+        case SS_ERR_SHAPE: return "batch, length or vocab out of range, or an odd batch of pairs";
+        case SS_ERR_DTYPE: return "unknown logits dtype";
+        case SS_ERR_PARAM: return "temperature, coefficients or flags out of range, or two references";
+        case SS_ERR_STRIDE: return "strides negative, rows overlap, or a pointer off its element";
+        case SS_ERR_WORKSPACE: return "workspace missing, misaligned or too small";
+        case SS_ERR_DEVICE: return "HIP launch failed";
+        default: return "unknown status";
+    }
+}
+
+}  // extern "C"
