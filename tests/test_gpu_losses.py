@@ -279,7 +279,8 @@ def test_masked_vocabulary(losses, dtype, low):
     x[3, 3] = value
     whole = torch.zeros(4, 6, dtype=torch.bool, device="cuda")
     whole[3, 3] = True
-    check_score(losses, {"logits": x, "tokens": y}, mask=None if low == "lowest" else ~whole)
+    for tau in (1.0, 0.6, 0.7, 0.9, 1.3):
+        check_score(losses, {"logits": x, "tokens": y}, mask=None if low == "lowest" else ~whole, tau=tau)
     if low == "-inf":
         out = losses.token_logprobs(x, y, want_stats=True)
         assert out["logprobs"].isnan().sum() == 1 and out["logprobs"][3, 3].isnan()
@@ -287,7 +288,8 @@ def test_masked_vocabulary(losses, dtype, low):
         assert grad[3, 3].isnan().all() and not grad[~whole].isnan().any()
     z[1, 2, 17], z[3, 3] = 0.25, 0.0  # the reference's own masks differ in these rows
     for kl in ("none", "sampled", "full"):
-        check_policy(losses, {"logits": x, "tokens": y, "ref_logits": z}, g, kl=kl, mask=~whole)
+        for tau in (1.0, 0.6, 0.9, 1.3):
+            check_policy(losses, {"logits": x, "tokens": y, "ref_logits": z}, g, kl=kl, mask=~whole, tau=tau)
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])

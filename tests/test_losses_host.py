@@ -185,3 +185,17 @@ def test_the_reference_s_gradients_are_those_of_its_losses():
         got = R.preference(rows, mask, ref, beta=0.4, label_smoothing=0.1, reduction=reduction)
         assert got["loss"].item() == pytest.approx(loss.item(), abs=1e-13)
         assert torch.allclose(rows.gradient(got["w"]), want, atol=1e-13)
+
+
+def test_waves_that_hold_a_row(tmp_path):
+    """csrc/loss/loss_plan.h: a workgroup holds all of a row that fits, and no other number of waves would hold more on a compute unit."""
+    src = tmp_path / "waves.cpp"
+    src.write_text('#include <cstdio>\n#include <initializer_list>\n#include "loss_plan.h"\nint main() { for (int held : {kHeldVecs, kHeldPairs}) for (int n = 0; n < 140000; n = n < 4000 ? n + 1 : n * 17 / 16)'
+                   ' std::printf("%d %d %d\\n", held, n, row_waves(n, held)); }\n')
+    exe = tmp_path / "waves"
+    subprocess.run(["g++", "-std=c++17", "-Wall", "-Wextra", "-Werror", "-Wno-unused-function", "-I", os.path.join(ROOT, "include"),
+                    "-I", os.path.join(ROOT, "paper_2603_16219_amd", "csrc", "loss"), "-o", exe, src], check=True)
+    for line in subprocess.run([exe], check=True, capture_output=True, text=True).stdout.splitlines():
+        held, n, got = map(int, line.split())
+        on_unit = lambda w: (16 // w) * min((w - 1) * 64 * held, n)
+        assert 2 <= got <= 16 and on_unit(got) == max(on_unit(w) for w in range(2, 17)), (held, n)
