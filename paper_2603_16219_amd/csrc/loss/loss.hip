@@ -280,7 +280,7 @@ __device__ __forceinline__ void zero_row(void* g, int V, int threads) {
 }
 
 // One lane's share of a row: vectors [first, end) by step, and its extra element if `extra`.
-template <int DT, typename S>
+template <int DT, typename S, bool ONCE = false>
 __device__ __forceinline__ S lane_sum(const void* h, const void* z, const Layout<DT>& lay, int first, int end, int step, bool extra, Factor c) {
     constexpr int kVec = Row<DT>::kVec, kUnroll = 4, kElem = DT == SS_BF16 ? 2 : 4;
     constexpr bool kRef = std::is_same<S, SumRef>::value;
@@ -304,14 +304,14 @@ __device__ __forceinline__ S lane_sum(const void* h, const void* z, const Layout
         typename Row<DT>::Raw r[kUnroll], rz[kUnroll];
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
-            r[u] = ld_vec<DT>(hv, i + u * step);
+            r[u] = ONCE ? ld_once<DT>(hv, i + u * step) : ld_vec<DT>(hv, i + u * step);
             if constexpr (kRef) rz[u] = ld_vec<DT>(zv, i + u * step);
         }
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) one(r[u], rz[u]);
     }
     for (; i < end; i += step) {
-        typename Row<DT>::Raw r = ld_vec<DT>(hv, i), rz = r;
+        typename Row<DT>::Raw r = ONCE ? ld_once<DT>(hv, i) : ld_vec<DT>(hv, i), rz = r;
         if constexpr (kRef) rz = ld_vec<DT>(zv, i);
         one(r, rz);
     }
@@ -422,7 +422,7 @@ __device__ __forceinline__ void far_grad(const void* h, const void* z, void* g, 
 
 // Vectors [first, end) by step, and the lane's extra element if `extra`, of a row's gradient.  The lane that owns the token's element
 // writes it again: its logit is read before anything of the row is overwritten.
-template <int DT, bool REF>
+template <int DT, bool REF, bool ONCE = false>
 __device__ __forceinline__ void write_grad(const void* h, const void* z, void* g, const Layout<DT>& lay, const RowGrad& r, int token, int first,
                                            int end, int step, bool extra, Factor c) {
     constexpr int kVec = Row<DT>::kVec, kElem = DT == SS_BF16 ? 2 : 4, kUnroll = 4;
@@ -450,14 +450,14 @@ __device__ __forceinline__ void write_grad(const void* h, const void* z, void* g
         typename Row<DT>::Raw raw[kUnroll], rawz[kUnroll];
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
-            raw[u] = ld_vec<DT>(hv, i + u * step);
+            raw[u] = ONCE ? ld_once<DT>(hv, i + u * step) : ld_vec<DT>(hv, i + u * step);
             if constexpr (REF) rawz[u] = ld_vec<DT>(zv, i + u * step);
         }
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) one(raw[u], rawz[u], i + u * step);
     }
     for (; i < end; i += step) {
-        const typename Row<DT>::Raw raw = ld_vec<DT>(hv, i);
+        const typename Row<DT>::Raw raw = ONCE ? ld_once<DT>(hv, i) : ld_vec<DT>(hv, i);
         if constexpr (REF) one(raw, ld_vec<DT>(zv, i), i);
         else one(raw, raw, i);
     }
@@ -494,7 +494,8 @@ struct ScoreArgs {
     double* logprob64;  // or NULL
 };
 
-// One workgroup a row.  In the statistics a row far from zero has the negative of its sum.
+// One workgroup a row, past the caches: 1024 rows of V = 151936 bf16 50 us (6.2 TB/s), 56 through them; fp32 6.6 TB/s.  bf16 rows have half the
+// arithmetic units' time for the exponentials.  In the statistics a row far from zero has the negative of its sum.
 template <int DT>
 __global__ __launch_bounds__(kRowThreads) void score_kernel(const ScoreArgs a) {
     __shared__ Total<Sum> part[kRowThreads / kWave];
@@ -507,7 +508,7 @@ __global__ __launch_bounds__(kRowThreads) void score_kernel(const ScoreArgs a) {
         place(a.r, row, at, grad_at);
         const void* const h = row_ptr<DT>(a.r.logits, at);
         const Layout<DT> lay(h, a.r.V, threadIdx.x);
-        s = block_total(lane_sum<DT, Sum>(h, nullptr, lay, threadIdx.x, lay.vecs, kRowThreads, true, a.r.c), kRowThreads, part);
+        s = block_total(lane_sum<DT, Sum, true>(h, nullptr, lay, threadIdx.x, lay.vecs, kRowThreads, true, a.r.c), kRowThreads, part);
         const bool far = is_far(s);
         if (far) s = far_sum<DT, Sum>(h, nullptr, a.r.V, a.r.c, kRowThreads, part);
         if (threadIdx.x == 0) {
@@ -534,17 +535,29 @@ struct GradArgs {
     const float* weight;      // of every row's log-prob, or NULL:
     const double* seq_weight; // of the first P sequences' log-probs, the other P have the negative
     int pairs;
+    int slices;               // workgroups a row
 };
+// A workgroup takes this much of a row, four vectors a lane, all in flight at once, and is gone: stores of one workgroup and loads of the next
+// overlap better than in longer ones.  2048 rows of V = 128256 bf16 169 us in these (6.2 TB/s), 178 in halves, 181 in twice as much, 203 a
+// workgroup of 512 a row; of V = 50257 fp32, 4096 rows, 281, 281, 320, 361.
+constexpr int kGradThreads = 256, kGradVecs = kGradThreads * 4;
 
 template <int DT>
-__global__ __launch_bounds__(kRowThreads) void grad_kernel(const GradArgs a) {
-    const long row = this_row();
+__global__ __launch_bounds__(kGradThreads) void grad_kernel(const GradArgs a) {
+    const long id = this_row();
+    const long row = (unsigned)id / (unsigned)a.slices;
+    const int slice = (int)(id - row * a.slices);
     if (row >= a.r.rows) return;
     long at, grad_at;
     place(a.r, row, at, grad_at);
     void* const g = const_cast<void*>(row_ptr<DT>(a.r.grad, grad_at));
+    const Layout<DT> lay(g, a.r.V, threadIdx.x);
+    const int first = slice * kGradVecs + threadIdx.x, end = slice + 1 == a.slices ? lay.vecs : min(lay.vecs, (slice + 1) * kGradVecs);
     if (!counts(a.r, row)) {
-        zero_row<DT>(g, a.r.V, kRowThreads);
+        const float none[Row<DT>::kVec] = {};
+        char* const base = static_cast<char*>(g) + (long)lay.head * (DT == SS_BF16 ? 2 : 4);
+        for (int i = first; i < end; i += kGradThreads) st_vec<DT>(base, i, none);
+        if (slice == 0 && lay.extra >= 0) st_elem<DT>(g, lay.extra, 0.f);
         return;
     }
     const void* const h = row_ptr<DT>(a.r.logits, at);
@@ -556,11 +569,10 @@ __global__ __launch_bounds__(kRowThreads) void grad_kernel(const GradArgs a) {
     const bool far = s < 0.f;
     const RowGrad rg = row_grad<DT, false>(a.r, far, a.stats[2 * row], fabsf(s), w, 0.0, 0.0, 0.0);
     if (far) {
-        far_grad<DT, false>(h, nullptr, g, a.r.V, rg, y, a.r.c, kRowThreads);
+        if (slice == 0) far_grad<DT, false>(h, nullptr, g, a.r.V, rg, y, a.r.c, kGradThreads);
         return;
     }
-    const Layout<DT> lay(g, a.r.V, threadIdx.x);
-    write_grad<DT, false>(h, nullptr, g, lay, rg, y, threadIdx.x, lay.vecs, kRowThreads, true, a.r.c);
+    write_grad<DT, false, true>(h, nullptr, g, lay, rg, y, first, end, kGradThreads, slice == 0, a.r.c);
 }
 
 // ------------------------------------------------------------------ policy loss
@@ -896,6 +908,12 @@ void launch_rows(void (*bf16)(A), void (*f32)(A), const ss_loss_params& p, const
     launch(p.dtype == SS_BF16 ? bf16 : f32, row_grid(a.r.rows), dim3(kRowThreads), 0, s, a);
 }
 
+void launch_grad(const ss_loss_params& p, GradArgs& a, hipStream_t q) {
+    const int vecs = p.vocab / (p.dtype == SS_BF16 ? 8 : 4);
+    a.slices = vecs > kGradVecs ? (vecs + kGradVecs - 1) / kGradVecs : 1;
+    launch(p.dtype == SS_BF16 ? grad_kernel<SS_BF16> : grad_kernel<SS_F32>, row_grid(a.r.rows * a.slices), dim3(kGradThreads), 0, q, a);
+}
+
 template <bool REF>
 void launch_policy(const ss_loss_params& p, const PolicyArgs& a, hipStream_t q) {
     constexpr int kHeld = REF ? kHeldPairs : kHeldVecs;
@@ -934,8 +952,8 @@ ss_status specsteer_token_logprobs_grad(const void* logits, const int32_t* token
     if (s.rows == 0) return SS_OK;
     if (!logits || !tokens || !stats || !grad_logprobs || !grad_logits) return SS_ERR_NULL;
     if (off_element(logits, *params) || off_element(grad_logits, *params)) return SS_ERR_STRIDE;
-    GradArgs a{make_rows(logits, nullptr, grad_logits, tokens, mask, *params, s), stats, grad_logprobs, nullptr, 0};
-    launch_rows(grad_kernel<SS_BF16>, grad_kernel<SS_F32>, *params, a, static_cast<hipStream_t>(stream));
+    GradArgs a{make_rows(logits, nullptr, grad_logits, tokens, mask, *params, s), stats, grad_logprobs, nullptr, 0, 0};
+    launch_grad(*params, a, static_cast<hipStream_t>(stream));
     return launched();
 }
 
@@ -1018,8 +1036,8 @@ ss_status specsteer_preference_loss(const void* logits, const int32_t* tokens, c
                 weight, loss64, pair_loss, margin};
     launch(pair_kernel, dim3((unsigned)pairs), dim3(kPairThreads), 0, q, pa);
     if (grad_logits && s.rows > 0) {
-        GradArgs a{r, stats, nullptr, weight, pairs};
-        launch_rows(grad_kernel<SS_BF16>, grad_kernel<SS_F32>, *params, a, q);
+        GradArgs a{r, stats, nullptr, weight, pairs, 0};
+        launch_grad(*params, a, q);
     }
     launch(sum_kernel, dim3(1), dim3(kOneThreads), 0, q, static_cast<const double*>(loss64), (long)pairs, factor, loss);
     return launched();
