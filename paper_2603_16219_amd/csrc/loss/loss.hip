@@ -270,13 +270,13 @@ __device__ __forceinline__ void place(const Rows& a, long row, long& at, long& g
     grad_at = b * a.gsb + t * a.gst;
 }
 
+// The gradient of a row that does not count, the part that write_grad takes of another.
 template <int DT>
-__device__ __forceinline__ void zero_row(void* g, int V, int threads) {
-    const Layout<DT> lay(g, V, threadIdx.x);
+__device__ __forceinline__ void zero_slice(void* g, const Layout<DT>& lay, int first, int end, int step, bool extra) {
     const float none[Row<DT>::kVec] = {};
     char* const base = static_cast<char*>(g) + (long)lay.head * (DT == SS_BF16 ? 2 : 4);
-    for (int i = threadIdx.x; i < lay.vecs; i += threads) st_vec<DT>(base, i, none);
-    if (lay.extra >= 0) st_elem<DT>(g, lay.extra, 0.f);
+    for (int i = first; i < end; i += step) st_vec<DT>(base, i, none);
+    if (extra && lay.extra >= 0) st_elem<DT>(g, lay.extra, 0.f);
 }
 
 // One lane's share of a row: vectors [first, end) by step, and its extra element if `extra`.
@@ -424,7 +424,8 @@ __device__ __forceinline__ void far_grad(const void* h, const void* z, void* g, 
 // writes it again: its logit is read before anything of the row is overwritten.
 template <int DT, bool REF, bool ONCE = false>
 __device__ __forceinline__ void write_grad(const void* h, const void* z, void* g, const Layout<DT>& lay, const RowGrad& r, int token, int first,
-                                           int end, int step, bool extra, Factor c) {
+                                           int end, int step, bool extra, Factor c, const int ahead = 0, const typename Row<DT>::Raw* r_ahead = nullptr,
+                                           const typename Row<DT>::Raw* rz_ahead = nullptr) {
     constexpr int kVec = Row<DT>::kVec, kElem = DT == SS_BF16 ? 2 : 4, kUnroll = 4;
     const char* const hv = static_cast<const char*>(h) + (long)lay.head * kElem;
     const char* const zv = REF ? static_cast<const char*>(z) + (long)lay.head * kElem : nullptr;
@@ -446,6 +447,9 @@ __device__ __forceinline__ void write_grad(const void* h, const void* z, void* g
         st_vec<DT>(gv, i, x);
     };
     int i = first;
+#pragma unroll
+    for (int u = 0; u < ahead; ++u, i += step)
+        if (i < end) one(r_ahead[u], rz_ahead[u], i);
     for (; i + (kUnroll - 1) * step < end; i += kUnroll * step) {
         typename Row<DT>::Raw raw[kUnroll], rawz[kUnroll];
 #pragma unroll
@@ -482,6 +486,35 @@ __device__ __forceinline__ double lse_difference(const Rows& a, bool far, const 
     return far ? by * a.inv_tau + sums * kLn2 : (by + sums) * kLn2;
 }
 
+// The sum of x over the workgroup, in every lane of wave 0.  The order is fixed.
+__device__ __forceinline__ double block_sum(double x, double* part) {
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) x += __shfl_xor(x, d, kWave);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (lane == 0) part[wave] = x;
+    __syncthreads();
+    x = lane < (int)blockDim.x / kWave ? part[lane] : 0.0;
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) x += __shfl_xor(x, d, kWave);
+    __syncthreads();
+    return x;
+}
+
+// Bytes of m that are not 0, over one wave.
+__device__ __forceinline__ int wave_count(const uint8_t* m, long n) {
+    const int lane = threadIdx.x & 63;
+    const long head = min(n, (long)((16 - (reinterpret_cast<uintptr_t>(m) & 15)) & 15)), vecs = (n - head) / 16, tail = head + vecs * 16;
+    int k = lane < head && m[lane] != 0 ? 1 : 0;
+    if (tail + lane < n && m[tail + lane] != 0) ++k;
+    const auto bytes = [](unsigned w) { return __popc((((w & 0x7F7F7F7Fu) + 0x7F7F7F7Fu) | w) & 0x80808080u); };
+#pragma unroll 4
+    for (long i = lane; i < vecs; i += kWave) {
+        const uint4 w = reinterpret_cast<const uint4*>(m + head)[i];
+        k += bytes(w.x) + bytes(w.y) + bytes(w.z) + bytes(w.w);
+    }
+    return wave_sum_i32(k);
+}
+
 // ------------------------------------------------------------------ token log-probs
 
 constexpr int kRowThreads = 512;
@@ -494,37 +527,121 @@ struct ScoreArgs {
     double* logprob64;  // or NULL
 };
 
-// One workgroup a row, past the caches: 1024 rows of V = 151936 bf16 50 us (6.2 TB/s), 56 through them; fp32 6.6 TB/s.  bf16 rows have half the
-// arithmetic units' time for the exponentials.  In the statistics a row far from zero has the negative of its sum.
+__device__ __forceinline__ void write_score(const ScoreArgs& a, long row, double lp, float E, double s) {
+    if (a.logprobs) a.logprobs[row] = (float)lp;
+    if (a.logprob64) a.logprob64[row] = lp;
+    if (a.stats) {
+        a.stats[2 * row] = E;
+        a.stats[2 * row + 1] = (float)s;
+    }
+}
+// A row far from zero, which has the negative of its sum in the statistics, by the whole workgroup.
 template <int DT>
-__global__ __launch_bounds__(kRowThreads) void score_kernel(const ScoreArgs a) {
-    __shared__ Total<Sum> part[kRowThreads / kWave];
+__device__ __forceinline__ void score_far_row(const ScoreArgs& a, long row, int threads, Total<Sum>* part) {
+    long at, grad_at;
+    place(a.r, row, at, grad_at);
+    const void* const h = row_ptr<DT>(a.r.logits, at);
+    const Total<Sum> s = far_sum<DT, Sum>(h, nullptr, a.r.V, a.r.c, threads, part);
+    if (threadIdx.x == 0) {
+        const int y = a.r.tokens[row];
+        write_score(a, row, token_logprob(a.r, true, y, y >= 0 && y < a.r.V ? ld_elem<DT>(h, y) : 0.f, s.E, s.s), s.E, -s.s);
+    }
+}
+
+// One workgroup a row, past the caches: 1024 rows of V = 151936 bf16 50 us (6.2 TB/s), 56 through them; fp32 6.6 TB/s.  bf16 rows take half the
+// arithmetic units' time for the exponentials.
+template <int DT>
+__global__ __launch_bounds__(kMaxThreads) void score_kernel(const ScoreArgs a) {
+    __shared__ Total<Sum> part[kUnitWaves];
+    const int threads = blockDim.x;
     const long row = this_row();
     if (row >= a.r.rows) return;
-    double lp = 0.0;
-    Total<Sum> s = {0.f, 1.0};
-    if (counts(a.r, row)) {
-        long at, grad_at;
-        place(a.r, row, at, grad_at);
-        const void* const h = row_ptr<DT>(a.r.logits, at);
-        const Layout<DT> lay(h, a.r.V, threadIdx.x);
-        s = block_total(lane_sum<DT, Sum, true>(h, nullptr, lay, threadIdx.x, lay.vecs, kRowThreads, true, a.r.c), kRowThreads, part);
-        const bool far = is_far(s);
-        if (far) s = far_sum<DT, Sum>(h, nullptr, a.r.V, a.r.c, kRowThreads, part);
-        if (threadIdx.x == 0) {
-            const int y = a.r.tokens[row];
-            lp = token_logprob(a.r, far, y, y >= 0 && y < a.r.V ? ld_elem<DT>(h, y) : 0.f, s.E, s.s);
-            if (far) s.s = -s.s;
-        }
+    if (!counts(a.r, row)) {
+        if (threadIdx.x == 0) write_score(a, row, 0.0, 0.f, 1.0);
+        return;
     }
+    long at, grad_at;
+    place(a.r, row, at, grad_at);
+    const void* const h = row_ptr<DT>(a.r.logits, at);
+    const Layout<DT> lay(h, a.r.V, threadIdx.x);
+    const Sum mine = lane_sum<DT, Sum, true>(h, nullptr, lay, threadIdx.x, lay.vecs, threads, true, a.r.c);
+    const Total<Sum> s = block_total(mine, threads, part);
+    if (is_far(s)) {
+        score_far_row<DT>(a, row, threads, part);
+    } else if (threadIdx.x == 0) {
+        const int y = a.r.tokens[row];
+        write_score(a, row, token_logprob(a.r, false, y, y >= 0 && y < a.r.V ? ld_elem<DT>(h, y) : 0.f, s.E, s.s), s.E, s.s);
+    }
+}
+
+// ------------------------------------------------------------------ few rows: several workgroups each
+
+constexpr int kSliceThreads = 256;
+
+struct Slices {
+    void* parts;          // the sums of every row's slices, Total<S> each
+    float* token_logits;  // of every row: the gradient may replace the logits before all workgroups have read them
+    int n, vecs;          // slices a row, vectors a slice
+};
+template <typename S>
+__device__ __forceinline__ Total<S>* parts_of(const Slices& p, long row) { return static_cast<Total<S>*>(p.parts) + row * p.n; }
+
+template <int DT, typename S>
+__global__ __launch_bounds__(kSliceThreads) void slice_kernel(const Rows r, const Slices p) {
+    static_assert(sizeof(Total<S>) <= kPartBytes, "space for a slice's sums");
+    __shared__ Total<S> part[kSliceThreads / kWave];
+    const long row = blockIdx.x / (unsigned)p.n;
+    const int slice = (int)(blockIdx.x - row * p.n);
+    if (!counts(r, row)) return;
+    long at, grad_at;
+    place(r, row, at, grad_at);
+    const void* const h = row_ptr<DT>(r.logits, at);
+    const void* const z = std::is_same<S, SumRef>::value ? row_ptr<DT>(r.ref, at) : nullptr;
+    const Layout<DT> lay(h, r.V, threadIdx.x);
+    const int end = slice + 1 == p.n ? lay.vecs : min(lay.vecs, (slice + 1) * p.vecs);
+    const S mine = lane_sum<DT, S>(h, z, lay, slice * p.vecs + threadIdx.x, end, kSliceThreads, slice == 0, r.c);
+    const Total<S> s = block_total(mine, kSliceThreads, part);
     if (threadIdx.x == 0) {
-        if (a.logprobs) a.logprobs[row] = (float)lp;
-        if (a.logprob64) a.logprob64[row] = lp;
-        if (a.stats) {
-            a.stats[2 * row] = s.E;
-            a.stats[2 * row + 1] = (float)s.s;
+        parts_of<S>(p, row)[slice] = s;
+        if (slice == 0) {
+            const int y = r.tokens[row];
+            p.token_logits[row] = y >= 0 && y < r.V ? ld_elem<DT>(h, y) : 0.f;
         }
     }
+}
+
+template <typename S>
+__device__ __forceinline__ Total<S> join_slices(const Slices& p, long row) {
+    const int lane = threadIdx.x & 63;
+    return join(parts_of<S>(p, row)[lane < p.n ? lane : 0], p.n);
+}
+
+// The log-prob of a row in slices, by one wave; true if the row is far from zero, and has none yet then.
+template <int DT>
+__device__ __forceinline__ bool score_joined(const ScoreArgs& a, const Slices& p, long row) {
+    const bool first = (threadIdx.x & 63) == 0;
+    if (!counts(a.r, row)) {
+        if (first) write_score(a, row, 0.0, 0.f, 1.0);
+        return false;
+    }
+    const Total<Sum> s = join_slices<Sum>(p, row);
+    if (is_far(s)) return true;
+    if (first) write_score(a, row, token_logprob(a.r, false, a.r.tokens[row], p.token_logits[row], s.E, s.s), s.E, s.s);
+    return false;
+}
+
+template <int DT>
+__global__ __launch_bounds__(kSliceThreads) void score_slices_kernel(const ScoreArgs a, const Slices p) {
+    constexpr int kWaves = kSliceThreads / kWave;
+    __shared__ Total<Sum> part[kWaves];
+    __shared__ int far_rows[kWaves];
+    const long first = (long)blockIdx.x * kWaves;
+    const int wave = threadIdx.x >> 6;
+    const bool far = first + wave < a.r.rows && score_joined<DT>(a, p, first + wave);
+    if ((threadIdx.x & 63) == 0) far_rows[wave] = far ? 1 : 0;
+    __syncthreads();
+    for (int w = 0; w < kWaves; ++w)
+        if (far_rows[w]) score_far_row<DT>(a, first + w, kSliceThreads, part);
 }
 
 // ------------------------------------------------------------------ gradient from known statistics
@@ -554,10 +671,7 @@ __global__ __launch_bounds__(kGradThreads) void grad_kernel(const GradArgs a) {
     const Layout<DT> lay(g, a.r.V, threadIdx.x);
     const int first = slice * kGradVecs + threadIdx.x, end = slice + 1 == a.slices ? lay.vecs : min(lay.vecs, (slice + 1) * kGradVecs);
     if (!counts(a.r, row)) {
-        const float none[Row<DT>::kVec] = {};
-        char* const base = static_cast<char*>(g) + (long)lay.head * (DT == SS_BF16 ? 2 : 4);
-        for (int i = first; i < end; i += kGradThreads) st_vec<DT>(base, i, none);
-        if (slice == 0 && lay.extra >= 0) st_elem<DT>(g, lay.extra, 0.f);
+        zero_slice<DT>(g, lay, first, end, kGradThreads, slice == 0);
         return;
     }
     const void* const h = row_ptr<DT>(a.r.logits, at);
@@ -582,8 +696,9 @@ struct PolicyArgs {
     const float* old_logprobs;
     const float* ref_logprobs;  // or NULL
     const float* advantages;
-    const double* norm;  // what a token of each sequence counts, or NULL: norm_all
+    const double* norm;  // what a token of each sequence counts, or NULL: norm_all, or one over the tokens that count
     double norm_all;
+    int count;  // the rows form their number themselves
     double clip_lo, clip_hi, kl_coef;
     int seq_advantages;
     float* logprobs;  // or NULL
@@ -595,12 +710,18 @@ struct RowLoss {
     double lp, kl, term, g, k, diff;
 };
 
+// What a token of the row counts, by any one wave.
+__device__ __forceinline__ double token_norm(const PolicyArgs& a, long row) {
+    if (a.count) return 1.0 / (double)wave_count(a.r.mask, a.r.rows);  // the row itself counts
+    return a.norm ? a.norm[(unsigned)row / (unsigned)a.r.T] : a.norm_all;
+}
+
 // A row's log-prob, KL and share of the loss, and their gradients, from its sums; hy is its token's logit.
 template <bool REF, typename S>
-__device__ __forceinline__ RowLoss row_loss(const PolicyArgs& a, bool far, long row, int y, float hy, float old, float advantage,
+__device__ __forceinline__ RowLoss row_loss(const PolicyArgs& a, bool far, long row, int y, float hy, float old, float advantage, double n,
                                                const Total<S>& s) {
     RowLoss o;
-    const double adv = advantage, n = a.norm ? a.norm[(unsigned)row / (unsigned)a.r.T] : a.norm_all;
+    const double adv = advantage;
     o.lp = token_logprob(a.r, far, y, hy, s.E, s.s);
     o.kl = o.k = o.diff = 0.0;
     const double ratio = exp(o.lp - (double)old);
@@ -625,13 +746,17 @@ __device__ __forceinline__ RowLoss row_loss(const PolicyArgs& a, bool far, long 
     return o;
 }
 
+__device__ __forceinline__ void write_policy(const PolicyArgs& a, long row, double lp, double kl, double term) {
+    if (a.logprobs) a.logprobs[row] = (float)lp;
+    if (a.kl) a.kl[row] = (float)kl;
+    a.terms[row] = term;
+}
 // The same written down, and what the gradient needs.
 template <int DT, bool REF, typename S>
-__device__ __forceinline__ RowGrad finish_row(const PolicyArgs& a, bool far, long row, int y, float hy, float old, float advantage, const Total<S>& s) {
-    const RowLoss o = row_loss<REF>(a, far, row, y, hy, old, advantage, s);
-    if (a.logprobs) a.logprobs[row] = (float)o.lp;
-    if (a.kl) a.kl[row] = (float)o.kl;
-    a.terms[row] = o.term;
+__device__ __forceinline__ RowGrad finish_row(const PolicyArgs& a, bool far, long row, int y, float hy, float old, float advantage, double n,
+                                             const Total<S>& s) {
+    const RowLoss o = row_loss<REF>(a, far, row, y, hy, old, advantage, n, s);
+    write_policy(a, row, o.lp, o.kl, o.term);
     return row_grad<DT, REF>(a.r, far, s.E, s.s, o.g, o.k, o.diff, o.kl);
 }
 
@@ -665,12 +790,11 @@ __global__ __launch_bounds__(kMaxThreads) void policy_kernel(const PolicyArgs a)
     place(a.r, row, at, grad_at);
     void* const g = a.r.grad ? const_cast<void*>(row_ptr<DT>(a.r.grad, grad_at)) : nullptr;
     if (!counts(a.r, row)) {
-        if (g) zero_row<DT>(g, a.r.V, blockDim.x);
-        if (tid == 0) {
-            if (a.logprobs) a.logprobs[row] = 0.f;
-            if (a.kl) a.kl[row] = 0.f;
-            a.terms[row] = 0.0;
+        if (g) {
+            const Layout<DT> lay(g, a.r.V, tid);
+            zero_slice<DT>(g, lay, tid, lay.vecs, blockDim.x, true);
         }
+        if (tid == 0) write_policy(a, row, 0.0, 0.0, 0.0);
         return;
     }
     const void* const h = row_ptr<DT>(a.r.logits, at);
@@ -680,12 +804,13 @@ __global__ __launch_bounds__(kMaxThreads) void policy_kernel(const PolicyArgs a)
     if (helper) {
         const float hy = valid ? ld_elem<DT>(h, y) : 0.f;
         const float old = a.old_logprobs[row], adv = a.advantages[a.seq_advantages ? (unsigned)row / (unsigned)a.r.T : row];
+        const double n = token_norm(a, row);
         __syncthreads();
         const int lane = tid & 63, waves = threads / kWave;
         const Total<S> s = join(part[lane < waves ? lane : 0], waves);
         const bool far = a.r.far || is_far(s);
         if (lane == 0) {
-            if (!far) shared.grad = finish_row<DT, REF>(a, false, row, y, hy, old, adv, s);
+            if (!far) shared.grad = finish_row<DT, REF>(a, false, row, y, hy, old, adv, n, s);
             shared.far = far ? 1 : 0;
         }
         __syncthreads();
@@ -761,32 +886,76 @@ __global__ __launch_bounds__(kMaxThreads) void policy_kernel(const PolicyArgs a)
     }
     if (shared.far) {
         const Total<S> s = far_sum<DT, S>(h, z, a.r.V, a.r.c, blockDim.x, part);
+        const double n = token_norm(a, row);
         if (tid == 0)
             shared.grad = finish_row<DT, REF>(a, true, row, y, valid ? ld_elem<DT>(h, y) : 0.f, a.old_logprobs[row],
-                                              a.advantages[a.seq_advantages ? (unsigned)row / (unsigned)a.r.T : row], s);
+                                              a.advantages[a.seq_advantages ? (unsigned)row / (unsigned)a.r.T : row], n, s);
         __syncthreads();
         const RowGrad rg = shared.grad;
         if (g) far_grad<DT, REF>(h, z, g, a.r.V, rg, y, a.r.c, blockDim.x);
     }
 }
 
+// Rows in slices: every workgroup forms what the row has once for itself, and writes its slice of the gradient.
+template <int DT, bool REF>
+__global__ __launch_bounds__(kSliceThreads) void policy_slices_kernel(const PolicyArgs a, const Slices p) {
+    using S = typename std::conditional<REF, SumRef, Sum>::type;
+    __shared__ Total<S> part[kSliceThreads / kWave];
+    __shared__ RowGrad shared_grad;
+    const long row = blockIdx.x / (unsigned)p.n;
+    const int slice = (int)(blockIdx.x - row * p.n);
+    long at, grad_at;
+    place(a.r, row, at, grad_at);
+    void* const g = a.r.grad ? const_cast<void*>(row_ptr<DT>(a.r.grad, grad_at)) : nullptr;
+    const void* const h = row_ptr<DT>(a.r.logits, at);
+    const void* const z = REF ? row_ptr<DT>(a.r.ref, at) : nullptr;
+    const Layout<DT> lay(g ? g : h, a.r.V, threadIdx.x);
+    const int first = slice * p.vecs + threadIdx.x, end = slice + 1 == p.n ? lay.vecs : min(lay.vecs, (slice + 1) * p.vecs);
+    if (!counts(a.r, row)) {
+        if (g) zero_slice<DT>(g, lay, first, end, kSliceThreads, slice == 0);
+        if (slice == 0 && threadIdx.x == 0) write_policy(a, row, 0.0, 0.0, 0.0);
+        return;
+    }
+    // the first vectors are on their way while the row's sums are joined
+    constexpr int kAhead = REF ? 2 : 4;
+    typename Row<DT>::Raw r[kAhead], rz[kAhead];
+    const char* const hv = static_cast<const char*>(h) + (long)lay.head * (DT == SS_BF16 ? 2 : 4);
+    const char* const zv = REF ? static_cast<const char*>(z) + (long)lay.head * (DT == SS_BF16 ? 2 : 4) : nullptr;
+    if (g && lay.vecs > 0) {
+#pragma unroll
+        for (int u = 0; u < kAhead; ++u) {
+            const int i = min(first + u * kSliceThreads, lay.vecs - 1);
+            r[u] = ld_vec<DT>(hv, i);
+            if constexpr (REF) rz[u] = ld_vec<DT>(zv, i);
+        }
+    }
+    const Total<S> s = join_slices<S>(p, row);
+    const float old = a.old_logprobs[row], adv = a.advantages[a.seq_advantages ? (unsigned)row / (unsigned)a.r.T : row];
+    const int y = a.r.tokens[row];
+    const double n = token_norm(a, row);
+    if (a.r.far || is_far(s)) {  // the row's first workgroup alone
+        if (slice != 0) return;
+        const Total<S> sf = far_sum<DT, S>(h, z, a.r.V, a.r.c, kSliceThreads, part);
+        if (threadIdx.x == 0) {
+            const RowLoss o = row_loss<REF>(a, true, row, y, p.token_logits[row], old, adv, n, sf);
+            write_policy(a, row, o.lp, o.kl, o.term);
+            shared_grad = row_grad<DT, REF>(a.r, true, sf.E, sf.s, o.g, o.k, o.diff, o.kl);
+        }
+        __syncthreads();
+        const RowGrad rg = shared_grad;
+        if (g) far_grad<DT, REF>(h, z, g, a.r.V, rg, y, a.r.c, kSliceThreads);
+        return;
+    }
+    const RowLoss o = row_loss<REF>(a, false, row, y, p.token_logits[row], old, adv, n, s);
+    if (slice == 0 && threadIdx.x == 0) write_policy(a, row, o.lp, o.kl, o.term);
+    if (!g) return;
+    const RowGrad rg = row_grad<DT, REF>(a.r, false, s.E, s.s, o.g, o.k, o.diff, o.kl);
+    write_grad<DT, REF>(h, z, g, lay, rg, y, first, end, kSliceThreads, slice == 0, a.r.c, kAhead, r, rz);
+}
+
 // ------------------------------------------------------------------ what is formed once a call
 
 constexpr int kOneThreads = 1024;
-
-// The sum of x over the workgroup, in every lane of wave 0.  The order is fixed.
-__device__ __forceinline__ double block_sum(double x, double* part) {
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) x += __shfl_xor(x, d, kWave);
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    if (lane == 0) part[wave] = x;
-    __syncthreads();
-    x = lane < (int)blockDim.x / kWave ? part[lane] : 0.0;
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) x += __shfl_xor(x, d, kWave);
-    __syncthreads();
-    return x;
-}
 
 // What a token of each sequence counts for the mean over tokens or over sequences: one workgroup, a wave a sequence.
 __global__ __launch_bounds__(kOneThreads) void norm_kernel(const uint8_t* mask, int B, int T, int seq_mean, double* norm) {
@@ -833,28 +1002,69 @@ __device__ __forceinline__ double softplus(double x) { return fmax(x, 0.0) + log
 
 constexpr int kPairThreads = 256;
 
-__global__ __launch_bounds__(kPairThreads) void pair_kernel(const PairArgs a) {
-    __shared__ double part[kPairThreads / kWave];
-    const long p = blockIdx.x;
+// One lane's share of what a sequence of a pair adds to their difference.
+__device__ __forceinline__ double pair_side(const PairArgs& a, long p, int side, int first, int step) {
+    const long at = (p + (side ? a.pairs : 0)) * (long)a.T;
     double x = 0.0;
-    for (int side = 0; side < 2; ++side) {
-        const long at = (p + (side ? a.pairs : 0)) * (long)a.T;
-        for (int t = threadIdx.x; t < a.T; t += kPairThreads) {
-            if (a.mask && a.mask[at + t] == 0) continue;
-            const double d = a.logprob64[at + t] - (a.ref_logprobs ? (double)a.ref_logprobs[at + t] : 0.0);
-            x += side ? -d : d;
-        }
+#pragma unroll 4
+    for (int t = first; t < a.T; t += step) {
+        if (a.mask && a.mask[at + t] == 0) continue;
+        const double d = a.logprob64[at + t] - (a.ref_logprobs ? (double)a.ref_logprobs[at + t] : 0.0);
+        x += side ? -d : d;
     }
-    x = block_sum(x, part);
-    if (threadIdx.x == 0) {
-        const double h = a.beta * x, e = a.smoothing;
-        const double loss = (1.0 - e) * softplus(-h) + e * softplus(h);
-        const double dh = (e - 1.0) / (1.0 + exp(h)) + e / (1.0 + exp(-h));
+    return x;
+}
+// A pair's loss from the difference of its sequences' log ratios.
+__device__ __forceinline__ double finish_pair(const PairArgs& a, long p, double x, bool write) {
+    const double h = a.beta * x, e = a.smoothing;
+    const double loss = (1.0 - e) * softplus(-h) + e * softplus(h);
+    const double dh = (e - 1.0) / (1.0 + exp(h)) + e / (1.0 + exp(-h));
+    if (write) {
         a.weight[p] = a.beta * a.factor * dh;
         a.loss64[p] = loss;
         if (a.loss) a.loss[p] = (float)loss;
         if (a.margin) a.margin[p] = (float)h;
     }
+    return loss;
+}
+
+__global__ __launch_bounds__(kPairThreads) void pair_kernel(const PairArgs a) {
+    __shared__ double part[kPairThreads / kWave];
+    const long p = blockIdx.x;
+    double x = 0.0;
+    for (int side = 0; side < 2; ++side) x += pair_side(a, p, side, threadIdx.x, kPairThreads);
+    x = block_sum(x, part);
+    if (threadIdx.x < kWave) finish_pair(a, p, x, threadIdx.x == 0);
+}
+
+// One workgroup for all pairs, a wave each, and the loss; rows in slices it joins first.
+template <int DT>
+__global__ __launch_bounds__(kOneThreads) void pairs_kernel(const ScoreArgs r, const Slices c, const PairArgs a, float* total) {
+    constexpr int kWaves = kOneThreads / kWave;
+    __shared__ Total<Sum> far_part[kWaves];
+    __shared__ double part[kWaves];
+    __shared__ int far_rows[kJoinRows];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (c.n > 1) {
+        for (int row = wave; row < (int)r.r.rows; row += kWaves) {
+            const bool far = score_joined<DT>(r, c, row);
+            if (lane == 0) far_rows[row] = far ? 1 : 0;
+        }
+        __syncthreads();
+        for (int row = 0; row < (int)r.r.rows; ++row)
+            if (far_rows[row]) score_far_row<DT>(r, row, kOneThreads, far_part);
+        __syncthreads();
+    }
+    double loss = 0.0;
+    for (int p = wave; p < a.pairs; p += kWaves) {
+        double x = 0.0;
+        for (int side = 0; side < 2; ++side) x += pair_side(a, p, side, lane, kWave);
+        x = wave_sum_f64(x);
+        const double one = finish_pair(a, p, x, lane == 0);
+        if (lane == 0) loss += one;
+    }
+    loss = block_sum(loss, part);
+    if (threadIdx.x == 0) *total = (float)(loss * a.factor);
 }
 
 __global__ void zero_loss_kernel(float* loss) { *loss = 0.f; }
@@ -903,22 +1113,47 @@ ss_status check_workspace(const void* workspace, size_t bytes, size_t need) {
 
 ss_status launched() { return hipGetLastError() == hipSuccess ? SS_OK : SS_ERR_DEVICE; }
 
-template <typename A>
-void launch_rows(void (*bf16)(A), void (*f32)(A), const ss_loss_params& p, const A& a, hipStream_t s) {
-    launch(p.dtype == SS_BF16 ? bf16 : f32, row_grid(a.r.rows), dim3(kRowThreads), 0, s, a);
+// The sums of the rows' slices; false if there is one a row.
+template <typename S>
+bool launch_slices(const ss_loss_params& p, const Rows& r, const LossScratch& w, void* workspace, int slices, Slices& out, hipStream_t q) {
+    const int vecs = row_vecs(p);
+    out.n = slices;
+    if (slices < 2) return false;
+    out.vecs = (vecs + out.n - 1) / out.n;
+    out.parts = static_cast<char*>(workspace) + w.parts;
+    out.token_logits = reinterpret_cast<float*>(static_cast<char*>(workspace) + w.token_logits);
+    launch(p.dtype == SS_BF16 ? slice_kernel<SS_BF16, S> : slice_kernel<SS_F32, S>, dim3((unsigned)(r.rows * out.n)), dim3(kSliceThreads), 0, q, r, out);
+    return true;
+}
+
+void launch_score(const ss_loss_params& p, const ScoreArgs& a, const LossScratch& w, void* workspace, hipStream_t q) {
+    Slices c;
+    if (launch_slices<Sum>(p, a.r, w, workspace, score_slices(a.r.rows, row_vecs(p)), c, q)) {
+        constexpr long kRowsEach = kSliceThreads / kWave;
+        launch(p.dtype == SS_BF16 ? score_slices_kernel<SS_BF16> : score_slices_kernel<SS_F32>, dim3((unsigned)((a.r.rows + kRowsEach - 1) / kRowsEach)),
+               dim3(kSliceThreads), 0, q, a, c);
+        return;
+    }
+    launch(p.dtype == SS_BF16 ? score_kernel<SS_BF16> : score_kernel<SS_F32>, row_grid(a.r.rows), dim3(a.r.rows <= device_cu_count() ? kMaxThreads : kRowThreads), 0, q, a);
 }
 
 void launch_grad(const ss_loss_params& p, GradArgs& a, hipStream_t q) {
-    const int vecs = p.vocab / (p.dtype == SS_BF16 ? 8 : 4);
+    const int vecs = row_vecs(p);
     a.slices = vecs > kGradVecs ? (vecs + kGradVecs - 1) / kGradVecs : 1;
     launch(p.dtype == SS_BF16 ? grad_kernel<SS_BF16> : grad_kernel<SS_F32>, row_grid(a.r.rows * a.slices), dim3(kGradThreads), 0, q, a);
 }
 
 template <bool REF>
-void launch_policy(const ss_loss_params& p, const PolicyArgs& a, hipStream_t q) {
+void launch_policy(const ss_loss_params& p, const PolicyArgs& a, const LossScratch& w, void* workspace, hipStream_t q) {
     constexpr int kHeld = REF ? kHeldPairs : kHeldVecs;
+    Slices c;
+    if (launch_slices<typename std::conditional<REF, SumRef, Sum>::type>(p, a.r, w, workspace, row_slices(a.r.rows, row_vecs(p)), c, q)) {
+        const unsigned groups = (unsigned)(a.r.rows * c.n);
+        launch(p.dtype == SS_BF16 ? policy_slices_kernel<SS_BF16, REF> : policy_slices_kernel<SS_F32, REF>, dim3(groups), dim3(kSliceThreads), 0, q, a, c);
+        return;
+    }
     void (*const k)(PolicyArgs) = p.dtype == SS_BF16 ? policy_kernel<SS_BF16, REF, kHeld> : policy_kernel<SS_F32, REF, kHeld>;
-    launch(k, row_grid(a.r.rows), dim3((unsigned)(kWave * row_waves(p.vocab / (p.dtype == SS_BF16 ? 8 : 4), kHeld))), 0, q, a);
+    launch(k, row_grid(a.r.rows), dim3((unsigned)(kWave * call_waves(a.r.rows, device_cu_count(), row_vecs(p), kHeld))), 0, q, a);
 }
 
 }  // namespace
@@ -938,9 +1173,10 @@ ss_status specsteer_token_logprobs(const void* logits, const int32_t* tokens, co
     if (s.rows == 0) return SS_OK;
     if (!logits || !tokens || !logprobs) return SS_ERR_NULL;
     if (off_element(logits, *params)) return SS_ERR_STRIDE;
-    if (check_workspace(workspace, workspace_bytes, loss_scratch(*params).bytes) != SS_OK) return SS_ERR_WORKSPACE;
-    ScoreArgs a{make_rows(logits, nullptr, nullptr, tokens, mask, *params, s), logprobs, stats, nullptr};
-    launch_rows(score_kernel<SS_BF16>, score_kernel<SS_F32>, *params, a, static_cast<hipStream_t>(stream));
+    const LossScratch w = loss_scratch(*params);
+    if (check_workspace(workspace, workspace_bytes, w.bytes) != SS_OK) return SS_ERR_WORKSPACE;
+    const ScoreArgs a{make_rows(logits, nullptr, nullptr, tokens, mask, *params, s), logprobs, stats, nullptr};
+    launch_score(*params, a, w, workspace, static_cast<hipStream_t>(stream));
     return launched();
 }
 
@@ -991,14 +1227,16 @@ ss_status specsteer_policy_loss(const void* logits, const void* ref_logits, cons
     a.kl = kl;
     char* const base = static_cast<char*>(workspace);
     a.terms = reinterpret_cast<double*>(base + w.row_value);
-    if (mask && !(policy->flags & SS_LOSS_SUM)) {
+    // the mean over tokens: each row counts them itself, beside its loads, up to 16 bytes of the mask 16 times a lane (a launch of its own 5 us)
+    a.count = mask && !(policy->flags & (SS_LOSS_SUM | SS_LOSS_SEQ_MEAN)) && s.rows <= 16384 ? 1 : 0;
+    if (mask && !(policy->flags & SS_LOSS_SUM) && !a.count) {
         double* const norm = reinterpret_cast<double*>(base + w.seq);
         launch(norm_kernel, dim3(1), dim3(kOneThreads), 0, q, mask, (int)params->batch, (int)params->length,
                (policy->flags & SS_LOSS_SEQ_MEAN) ? 1 : 0, norm);
         a.norm = norm;
     }
-    if (ref_logits) launch_policy<true>(*params, a, q);
-    else launch_policy<false>(*params, a, q);
+    if (ref_logits) launch_policy<true>(*params, a, w, workspace, q);
+    else launch_policy<false>(*params, a, w, workspace, q);
     launch(sum_kernel, dim3(1), dim3(kOneThreads), 0, q, static_cast<const double*>(a.terms), s.rows, 1.0, loss);
     return launched();
 }
@@ -1027,19 +1265,21 @@ ss_status specsteer_preference_loss(const void* logits, const int32_t* tokens, c
     float* const stats = reinterpret_cast<float*>(base + w.stats);
     double *const weight = reinterpret_cast<double*>(base + w.seq), *const loss64 = weight + pairs;
     const Rows r = make_rows(logits, nullptr, grad_logits, tokens, mask, *params, s);
-    if (s.rows > 0) {
-        ScoreArgs a{r, logprobs, stats, lp64};
-        launch_rows(score_kernel<SS_BF16>, score_kernel<SS_F32>, *params, a, q);
-    }
+    const ScoreArgs sa{r, logprobs, stats, lp64};
+    Slices c{nullptr, nullptr, 1, 0};
+    const bool one = pairs_in_one(pairs, params->length), join = one && s.rows > 0 && s.rows <= kJoinRows && score_slices(s.rows, row_vecs(*params)) > 1;
+    if (join) launch_slices<Sum>(*params, r, w, workspace, score_slices(s.rows, row_vecs(*params)), c, q);
+    else if (s.rows > 0) launch_score(*params, sa, w, workspace, q);
     const double factor = (preference->flags & SS_LOSS_SUM) ? 1.0 : 1.0 / (double)pairs;
     PairArgs pa{lp64, ref_logprobs, mask, pairs, params->length, (double)preference->beta, (double)preference->label_smoothing, factor,
                 weight, loss64, pair_loss, margin};
-    launch(pair_kernel, dim3((unsigned)pairs), dim3(kPairThreads), 0, q, pa);
+    if (one) launch(params->dtype == SS_BF16 ? pairs_kernel<SS_BF16> : pairs_kernel<SS_F32>, dim3(1), dim3(kOneThreads), 0, q, sa, c, pa, loss);
+    else launch(pair_kernel, dim3((unsigned)pairs), dim3(kPairThreads), 0, q, pa);
     if (grad_logits && s.rows > 0) {
         GradArgs a{r, stats, nullptr, weight, pairs, 0};
         launch_grad(*params, a, q);
     }
-    launch(sum_kernel, dim3(1), dim3(kOneThreads), 0, q, static_cast<const double*>(loss64), (long)pairs, factor, loss);
+    if (!one) launch(sum_kernel, dim3(1), dim3(kOneThreads), 0, q, static_cast<const double*>(loss64), (long)pairs, factor, loss);
     return launched();
 }
 

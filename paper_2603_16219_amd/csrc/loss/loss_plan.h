@@ -66,9 +66,32 @@ inline ss_status check_preference(const ss_preference_params* q) {
 
 // The scratch: a double a row (its share of the policy loss, or its log-prob for the preference loss), its statistics, and two
 // doubles a sequence (what a token of it counts; a pair's weight and loss).
+//
+// Calls of few rows give each to several workgroups, whose sums over their slices lie behind that.
 struct LossScratch {
-    size_t row_value, stats, seq, bytes;
+    size_t row_value, stats, seq, parts, token_logits, bytes;
 };
+
+// Workgroups that a row of so many vectors takes: about 1024 in all, 512 vectors each at least.  In a third of the compute units and less one
+// workgroup a row leaves most of them idle: the policy loss of one row of V = 128256 bf16 20 us in one workgroup, 8.5 in slices (two launches
+// instead of one), of 16 20.9 and 11, of 64 21.2 and 15.4, of 100 21.4 and 18.9, of 128 21.7 and 23.3; of 32 rows of V = 32000 11 and 9.3.
+// Log-probs alone gain less: of rows up to 8192 vectors, 8 a lane of a workgroup, they are faster in one (4 of V = 32000 fp32 4.5 and 5.2 us; of
+// V = 50257 6.5 and 5.2).
+constexpr int kMaxRowSlices = 64, kPartBytes = 32;
+constexpr long kSliceRows = 100, kSliceGroups = 1024, kSliceVecs = 512;
+constexpr int kScoreVecs = 8192;
+inline int row_slices(long rows, int vecs) {
+    if (rows < 1 || rows > kSliceRows) return 1;
+    const long want = (kSliceGroups + rows - 1) / rows, most = vecs / kSliceVecs;
+    const long n = want < most ? want : most;
+    return (int)(n > kMaxRowSlices ? kMaxRowSlices : n < 1 ? 1 : n);
+}
+inline int score_slices(long rows, int vecs) { return vecs > kScoreVecs ? row_slices(rows, vecs) : 1; }
+// Pairs that one workgroup of 16 waves forms with their loss, a wave a pair: 14 rows 3.2 us, a launch of its own for the loss 2 more.
+inline bool pairs_in_one(int pairs, int length) { return pairs <= 16 && length <= 512; }
+// Rows in slices that the same workgroup joins first.
+constexpr long kJoinRows = 64;
+inline int row_vecs(const ss_loss_params& p) { return p.vocab / (p.dtype == SS_BF16 ? 8 : 4); }
 
 inline LossScratch loss_scratch(const ss_loss_params& p) {
     const auto up = [](size_t n) { return (n + 255) / 256 * 256; };
@@ -77,7 +100,10 @@ inline LossScratch loss_scratch(const ss_loss_params& p) {
     w.row_value = 0;
     w.stats = up(rows * sizeof(double));
     w.seq = w.stats + up(rows * 2 * sizeof(float));
-    w.bytes = w.seq + up((size_t)p.batch * 2 * sizeof(double)) + 256;
+    w.parts = w.seq + up((size_t)p.batch * 2 * sizeof(double)) + 256;
+    const int slices = row_slices((long)rows, row_vecs(p));
+    w.token_logits = w.parts + (slices > 1 ? up(rows * slices * kPartBytes) : 0);
+    w.bytes = w.token_logits + (slices > 1 ? up(rows * sizeof(float)) : 0);
     return w;
 }
 
@@ -98,6 +124,12 @@ inline int row_waves(int vecs, int held) {
         }
     }
     return best;
+}
+// The same for a call of so many rows on so many compute units: where all of them run at once with more waves each, with as many.
+inline int call_waves(long rows, int units, int vecs, int held) {
+    const int most = (int)(kUnitWaves / ((rows + units - 1) / units)), useful = (vecs + 63) / 64 + 1, w = row_waves(vecs, held);
+    const int wide = most < useful ? most : useful;
+    return wide > w ? wide : w;
 }
 
 }  // namespace

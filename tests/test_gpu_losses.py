@@ -212,6 +212,41 @@ def test_policy_loss_of_large_vocabularies(losses, dtype, V, kl):
     check_policy(losses, inp, g, kl=kl, tau=0.8)
 
 
+# More rows than are cut into slices: one workgroup holds a row.  Around what it holds of short and long rows, and rows it holds a part of.
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("kl", ["none", "full"])
+@pytest.mark.parametrize("V", [5, 1023, 4099, 8191, 8193, 16391, 30721, 61447, 122879, 122881, 200003])
+def test_policy_loss_of_rows_held_by_a_workgroup(losses, V, kl, dtype):
+    inp, g = make(2, 52, V, dtype, ref=True)
+    check_policy(losses, inp, g, kl=kl, tau=0.9, mask=ragged_mask(2, 52, g, "lengths"))
+
+
+@pytest.mark.parametrize("kl", ["none", "sampled", "full"])
+def test_policy_loss_over_more_rows_than_units(losses, kl):
+    inp, g = make(3, 300, 6007, "bf16", ref=True)
+    check_policy(losses, inp, g, kl=kl, mask=ragged_mask(3, 300, g, "empty_sequence"), poison=True)
+    inp, g = make(1, 17000, 211, "bf16", ref=True)  # more than count the mask's tokens themselves
+    check_policy(losses, inp, g, kl=kl, mask=ragged_mask(1, 17000, g, "lengths"))
+
+
+@pytest.mark.parametrize("offset", [1, 3, 15])
+@pytest.mark.parametrize("T", [1, 5, 40, 700])
+def test_tokens_counted_from_a_mask_at_any_address(losses, offset, T):
+    inp, g = make(1, T, 67, "f32")
+    store = torch.zeros(T + 64, dtype=torch.uint8, device="cuda")
+    store[offset:offset + T] = (torch.rand(T, generator=g, device="cuda") < 0.5).byte() * torch.randint(1, 256, (T,), generator=g, device="cuda").byte()
+    store[:offset], store[offset + T:] = 1, 1
+    check_policy(losses, inp, g, kl="none", mask=store[offset:offset + T].view(1, T))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [4099, 50257, 70001])
+def test_token_logprobs_of_many_long_rows(losses, V, dtype):
+    inp, g = make(4, 75, V, dtype)
+    check_score(losses, inp, mask=ragged_mask(4, 75, g, "lengths"), tau=0.8)
+    check_score(losses, {k: v[:, :30] for k, v in inp.items()} | {"tokens": inp["tokens"][:, :30].contiguous()})
+
+
 def test_policy_loss_without_gradient(losses):
     for kl in ("none", "sampled", "full"):
         inp, g = make(4, 9, 4099, "bf16", ref=True)
@@ -250,7 +285,7 @@ def test_preference_loss_at_the_edges(losses, V, dtype):
     check_preference(losses, inp, g, mask=ragged_mask(4, 5, g, "empty_sequence"), tau=0.7, reduction="sum", scale=0.25)
 
 
-@pytest.mark.parametrize("B,T", [(2, 1), (2, 2000), (64, 7), (600, 3)])
+@pytest.mark.parametrize("B,T", [(2, 1), (2, 2000), (32, 7), (34, 5), (2, 512), (2, 513), (600, 3)])
 @pytest.mark.parametrize("reference", [True, False])
 def test_preference_loss_of_few_and_many_pairs(losses, B, T, reference):
     inp, g = make(B, T, 403, "bf16")
@@ -292,11 +327,12 @@ def test_masked_vocabulary(losses, dtype, low):
             check_policy(losses, {"logits": x, "tokens": y, "ref_logits": z}, g, kl=kl, mask=~whole, tau=tau)
 
 
+@pytest.mark.parametrize("rows", [(3, 4, 2051), (3, 4, 70003), (2, 60, 1999)])  # one workgroup a row, slices, and the same of many rows
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("shift", [700.0, -7e5, 9e5, 3e7, -1e30])
-def test_rows_far_from_zero(losses, dtype, shift):
+def test_rows_far_from_zero(losses, dtype, shift, rows):
     """Logits around a common offset, on both sides of the limit up to which rows are summed by exponents, some of them masked."""
-    inp, g = make(3, 4, 2051, dtype, sigma=1.0, ref=True)
+    inp, g = make(*rows, dtype, sigma=1.0, ref=True)
     x, z, y = inp["logits"], inp["ref_logits"], inp["tokens"]
     step = max(1.0, abs(shift)) * torch.finfo(x.dtype).eps  # differences of a few steps of the type there
     x.copy_(x.float() * step + shift)
@@ -339,13 +375,17 @@ def test_token_of_probability_zero_and_tokens_outside_the_vocabulary(losses):
     assert pref["grad_logits"][[1, 3]].isnan().all() and not pref["grad_logits"][[0, 2]].isnan().any()
 
 
+@pytest.mark.parametrize("T", [4, 51])
+@pytest.mark.parametrize("far", [False, True])
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("V", [9, 4099, 50257, 128256, 256000])
-def test_gradient_in_place_of_the_logits(losses, V, dtype):
-    inp, g = make(2, 4, V, dtype, ref=True)
+def test_gradient_in_place_of_the_logits(losses, V, dtype, far, T):
+    inp, g = make(2, T, V, dtype, ref=True)
     x, y, z = inp["logits"], inp["tokens"], inp["ref_logits"]
-    zeros, adv = torch.zeros(2, 4, device="cuda") - 5, torch.randn(2, 4, generator=g, device="cuda")
-    mask = torch.tensor([[1, 1, 0, 1], [0, 1, 1, 1]], dtype=torch.bool, device="cuda")
+    if far:
+        x[1, ::2] = 2e6
+    zeros, adv = torch.zeros(2, T, device="cuda") - 5, torch.randn(2, T, generator=g, device="cuda")
+    mask = torch.tensor([[1, 1, 0, 1], [0, 1, 1, 1]], dtype=torch.bool, device="cuda").repeat(1, (T + 3) // 4)[:, :T]
     calls = [lambda t, **k: losses.policy_loss(t, y, zeros, adv, mask=mask, **k),
              lambda t, **k: losses.policy_loss(t, y, zeros, adv, mask=mask, ref_logits=z, kl_coef=0.2, **k),
              lambda t, **k: losses.preference_loss(t, y, mask=mask, beta=0.4, **k)]

@@ -199,3 +199,23 @@ def test_waves_that_hold_a_row(tmp_path):
         held, n, got = map(int, line.split())
         on_unit = lambda w: (16 // w) * min((w - 1) * 64 * held, n)
         assert 2 <= got <= 16 and on_unit(got) == max(on_unit(w) for w in range(2, 17)), (held, n)
+
+
+def test_slices_of_calls_with_few_rows(tmp_path, losses):
+    """csrc/loss/loss_plan.h: slices are as many as a wave joins, none is empty, and the workspace holds them."""
+    src = tmp_path / "slices.cpp"
+    src.write_text('#include <cstdio>\n#include "loss_plan.h"\nint main() { for (long r = 0; r < 300; r += r < 8 ? 1 : 7) for (int n = 0; n < 300000; n = n < 1100 ? n + 37 : n * 5 / 4)'
+                   ' std::printf("%ld %d %d %d\\n", r, n, row_slices(r, n), score_slices(r, n)); }\n')
+    exe = tmp_path / "slices"
+    subprocess.run(["g++", "-std=c++17", "-Wall", "-Wextra", "-Werror", "-Wno-unused-function", "-I", os.path.join(ROOT, "include"),
+                    "-I", os.path.join(ROOT, "paper_2603_16219_amd", "csrc", "loss"), "-o", exe, src], check=True)
+    seen = set()
+    for line in subprocess.run([exe], check=True, capture_output=True, text=True).stdout.splitlines():
+        rows, vecs, n, scored = map(int, line.split())
+        seen.add(n)
+        assert 1 <= n <= 64 and scored in (1, n) and (n == 1 or vecs // n >= 512) and (n == 1 or rows <= 100)
+        if n > 1:
+            p = losses.SSLossParams(1, rows, 8 * vecs, 1, 0, 0, 0, 0, 1.0, 1.0)
+            if p.vocab <= 1 << 20:
+                assert losses.workspace_bytes(p) >= rows * (n * 32 + 4 + 16)
+    assert {1, 2, 64} <= seen
