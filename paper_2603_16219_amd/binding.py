@@ -90,23 +90,26 @@ def library() -> ctypes.CDLL:
 
 
 def _native_wrappers(lib: ctypes.CDLL):
-    """The native wrappers of this library (built only if absent), or None with a warning: the general path answers everything
+    return load_wrappers("_calls", _build.calls_path, _build.build_calls, lambda: (
+        lib.specsteer_workspace_bytes, lib.specsteer_verify_block_unbound, lib.specsteer_cloud_topk, lib.specsteer_edge_resample))
+
+
+def load_wrappers(name: str, where, build, functions):
+    """The native wrappers of a library (built only if absent), or None with a warning: the general path answers everything
     without them, small calls with more host time."""
     try:
-        path = _build.calls_path()
+        path = where()
         if not os.path.exists(path):
             if not os.access(os.path.dirname(path), os.W_OK):
                 raise OSError(f"{path} is not there and cannot be built there")
-            _build.build_calls()
-        spec = importlib.util.spec_from_file_location(__package__ + "._calls", path)
+            build()
+        spec = importlib.util.spec_from_file_location(f"{__package__}.{name}", path)
         calls = importlib.util.module_from_spec(spec)
         spec.loader.exec_module(calls)
-        calls.use(*(ctypes.cast(f, ctypes.c_void_p).value for f in (
-            lib.specsteer_workspace_bytes, lib.specsteer_verify_block_unbound, lib.specsteer_cloud_topk, lib.specsteer_edge_resample)),
-            torch._C._cuda_getCurrentRawStream)
+        calls.use(*(ctypes.cast(f, ctypes.c_void_p).value for f in functions()), torch._C._cuda_getCurrentRawStream)
         return calls
     except Exception as e:  # no compiler or headers, a file that does not load, a library from before the wrappers
-        warnings.warn(f"the binding's native wrappers are not available, small calls take more host time: {e}", RuntimeWarning, stacklevel=3)
+        warnings.warn(f"the binding's native wrappers are not available, small calls take more host time: {e}", RuntimeWarning, stacklevel=4)
         return None
 
 

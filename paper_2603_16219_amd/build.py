@@ -13,7 +13,10 @@ INCLUDE = os.path.join(_ROOT, "include")
 LIBRARY = os.path.join(_PKG, "libspecsteer.so")
 LOSS_SOURCES = [os.path.join(_PKG, "csrc", "loss", "loss.hip")]
 LOSS_LIBRARY = os.path.join(_PKG, "libspecsteer_loss.so")
-CALLS_SOURCES = [os.path.join(_PKG, "csrc", "calls.cpp"), os.path.join(_PKG, "csrc", "unbound.h"), os.path.join(INCLUDE, "specsteer.h")]
+CALLS_SOURCES = [os.path.join(_PKG, "csrc", "calls.cpp"), os.path.join(_PKG, "csrc", "calls_common.hpp"), os.path.join(_PKG, "csrc", "unbound.h"),
+                 os.path.join(INCLUDE, "specsteer.h")]
+LOSS_CALLS_SOURCES = [os.path.join(_PKG, "csrc", "loss", "loss_calls.cpp"), os.path.join(_PKG, "csrc", "calls_common.hpp"),
+                      os.path.join(INCLUDE, "specsteer_loss.h"), os.path.join(INCLUDE, "specsteer.h")]
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950",
@@ -40,6 +43,7 @@ def build(verbose: bool = False) -> str:
     build_library(verbose)
     build_loss_library(verbose)
     build_calls(verbose)
+    build_loss_calls(verbose)
     return LIBRARY
 
 
@@ -59,16 +63,33 @@ def build_loss_library(verbose: bool = False) -> str:
 def calls_path() -> str:
     """Where the native wrappers for this torch and these sources lie: what they are compiled against is in the name, so that one
     built for another torch, whose tensors may be laid out differently, or from other sources is never loaded."""
+    return _calls_path("_calls", CALLS_SOURCES)
+
+
+def loss_calls_path() -> str:
+    """The same for those of the losses."""
+    return _calls_path("_loss_calls", LOSS_CALLS_SOURCES)
+
+
+def _calls_path(name: str, sources: list) -> str:
     import torch
 
     h = hashlib.sha256(repr((torch.__version__, torch.version.git_version, torch._C._GLIBCXX_USE_CXX11_ABI)).encode())
-    for path in CALLS_SOURCES:
+    for path in sources:
         with open(path, "rb") as f:
             h.update(f.read())
-    return os.path.join(_PKG, f"_calls-{h.hexdigest()[:16]}{sysconfig.get_config_var('EXT_SUFFIX')}")
+    return os.path.join(_PKG, f"{name}-{h.hexdigest()[:16]}{sysconfig.get_config_var('EXT_SUFFIX')}")
 
 
 def build_calls(verbose: bool = False) -> str:
+    return _build_calls(calls_path(), CALLS_SOURCES[0], verbose)
+
+
+def build_loss_calls(verbose: bool = False) -> str:
+    return _build_calls(loss_calls_path(), LOSS_CALLS_SOURCES[0], verbose)
+
+
+def _build_calls(path: str, source: str, verbose: bool) -> str:
     """The binding's native wrappers, host code against torch's headers and libraries.  Renamed into place, so that processes that
     build at the same time never load half a file."""
     import torch
@@ -76,11 +97,10 @@ def build_calls(verbose: bool = False) -> str:
 
     lib = os.path.join(os.path.dirname(torch.__file__), "lib")
     includes = [x for d in (INCLUDE, *cpp_extension.include_paths(), sysconfig.get_paths()["include"]) for x in ("-I", d)]
-    path = calls_path()
     part = f"{path}.{os.getpid()}"
     try:
         _run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden",
-              f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *includes, "-o", part, CALLS_SOURCES[0],
+              f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}", *includes, "-o", part, source,
               "-L", lib, "-lc10", "-ltorch_cpu", "-ltorch_python", f"-Wl,-rpath,{lib}"], verbose)
         os.replace(part, path)
     finally:

@@ -1,5 +1,7 @@
 """Binding of the losses over full-vocabulary logits (include/specsteer_loss.h): argument marshalling only.
 
+As in ``binding``, arguments that need nothing done to them go to native code (csrc/loss/loss_calls.cpp), others through ctypes here.
+
 Every sum, loss and gradient is formed inside ``libspecsteer_loss.so`` (hand-written HIP for gfx950) on torch's current
 stream; PyTorch supplies device memory and the stream.  There is no CPU or PyTorch fallback.
 
@@ -17,7 +19,7 @@ from typing import Optional
 import torch  # imported before the library so both share one HIP runtime
 
 from . import build as _build
-from .binding import SpecSteerError, _ptr, _ready, _refuse_repeated_rows, _stream
+from .binding import SpecSteerError, _ptr, _ready, _refuse_repeated_rows, _stream, load_wrappers
 
 SS_LOSS_SUM = 1
 SS_LOSS_SEQ_MEAN = 2
@@ -50,11 +52,12 @@ class SSPreferenceParams(ctypes.Structure):
 
 
 _lib = None
+_calls = None  # the native wrappers, once the library is loaded and if they can be
 
 
 def library() -> ctypes.CDLL:
     """Load libspecsteer_loss.so from the package directory (building it only if absent)."""
-    global _lib
+    global _lib, _calls
     if _lib is None:
         path = _build.LOSS_LIBRARY
         if not os.path.exists(path):
@@ -72,7 +75,22 @@ def library() -> ctypes.CDLL:
         lib.specsteer_loss_status_string.restype = ctypes.c_char_p
         lib.specsteer_loss_status_string.argtypes = [ctypes.c_int]
         _lib = lib
+        _calls = load_wrappers("_loss_calls", _build.loss_calls_path, _build.build_loss_calls, lambda: (
+            lib.specsteer_loss_workspace_bytes, lib.specsteer_token_logprobs, lib.specsteer_token_logprobs_grad, lib.specsteer_policy_loss,
+            lib.specsteer_preference_loss))
     return _lib
+
+
+def _native(name: str, *args):
+    """What the native wrapper of this name returns for arguments that it takes, None for others."""
+    if _lib is None:
+        library()
+    if _calls is None:
+        return None
+    out = getattr(_calls, name)(*args)
+    if type(out) is int:
+        raise SpecSteerError(out, status_string(out))
+    return out
 
 
 def status_string(status: int) -> str:
@@ -182,6 +200,9 @@ def token_logprobs(logits: torch.Tensor, tokens: torch.Tensor, *, mask: Optional
                    want_stats: bool = False, workspace: Optional[torch.Tensor] = None) -> dict:
     """specsteer_token_logprobs on logits [B, T, V] and tokens [B, T]: {"logprobs" [B, T] float32, 0 where `mask` [B, T] is
     false, "stats" [B, T, 2] or None}.  The stats are what token_logprobs_grad takes."""
+    out = _native("token_logprobs", logits, tokens, mask, temperature, want_stats, workspace)
+    if out is not None:
+        return out
     params = _make_params(logits, tokens, temperature)
     dev = logits.device
     mask = _ready_mask(mask, tokens, dev)
@@ -199,6 +220,9 @@ def token_logprobs_grad(logits: torch.Tensor, tokens: torch.Tensor, stats: torch
                         grad_logits: Optional[torch.Tensor] = None) -> torch.Tensor:
     """specsteer_token_logprobs_grad: the gradient [B, T, V] with respect to the logits, in their type, of a loss whose gradient with
     respect to their log-probs is grad_logprobs [B, T].  It goes to `grad_logits` if given, which may be the logits."""
+    out = _native("token_logprobs_grad", logits, tokens, stats, grad_logprobs, mask, temperature, grad_scale, grad_logits)
+    if out is not None:
+        return out
     grad_logits = _gradient(logits, True, grad_logits)
     params = _make_params(logits, tokens, temperature, grad_scale, grad_logits)
     dev = logits.device
@@ -226,6 +250,10 @@ def policy_loss(logits: torch.Tensor, tokens: torch.Tensor, old_logprobs: torch.
     flags = _REDUCTIONS.get(reduction)
     if flags is None:
         raise ValueError(f"reduction must be one of {sorted(_REDUCTIONS)}, got {reduction!r}")
+    out = _native("policy_loss", logits, tokens, old_logprobs, advantages, mask, ref_logits, ref_logprobs, clip_low, clip_high, kl_coef, temperature,
+                  flags, grad_scale, want_grad, grad_logits, workspace)
+    if out is not None:
+        return out
     if ref_logits is not None and ref_logprobs is not None:
         raise ValueError("give the reference by its logits or by its log-probs, not both")
     has_ref = ref_logits is not None or ref_logprobs is not None
@@ -268,6 +296,11 @@ def preference_loss(logits: torch.Tensor, tokens: torch.Tensor, *, mask: Optiona
     the logits' type or None}."""
     if reduction not in ("mean", "sum"):
         raise ValueError(f"reduction must be 'mean' or 'sum', got {reduction!r}")
+    flags = SS_LOSS_SUM if reduction == "sum" else 0
+    out = _native("preference_loss", logits, tokens, mask, ref_logprobs, beta, label_smoothing, temperature, flags, grad_scale, want_grad, grad_logits,
+                  workspace)
+    if out is not None:
+        return out
     grad_logits = _gradient(logits, want_grad, grad_logits)
     params = _make_params(logits, tokens, temperature, grad_scale, grad_logits)
     dev = logits.device
@@ -282,6 +315,6 @@ def preference_loss(logits: torch.Tensor, tokens: torch.Tensor, *, mask: Optiona
     margin = torch.empty_like(pair_loss)
     logprobs = torch.empty(tokens.shape, dtype=torch.float32, device=dev)
     _call(library().specsteer_preference_loss, dev, _ptr(logits), _ptr(tokens), _ptr(mask), _ptr(ref_logprobs), ctypes.byref(params),
-          ctypes.byref(SSPreferenceParams(beta, label_smoothing, SS_LOSS_SUM if reduction == "sum" else 0)), _ptr(loss), _ptr(pair_loss),
+          ctypes.byref(SSPreferenceParams(beta, label_smoothing, flags)), _ptr(loss), _ptr(pair_loss),
           _ptr(margin), _ptr(logprobs), _ptr(grad_logits), _ptr(workspace), _bytes(workspace))
     return {"loss": loss, "pair_loss": pair_loss, "margin": margin, "logprobs": logprobs, "grad_logits": grad_logits}
