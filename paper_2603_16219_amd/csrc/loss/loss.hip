@@ -233,6 +233,32 @@ __device__ __forceinline__ Total<SumRef> join(const Total<SumRef>& a, int n) {
     r.sz = wave_sum_f64(has ? moved(a.sz, a.Ez, r.Ez) : 0.0);
     return r;
 }
+// Totals of aligned groups of lanes, 2 to 64 of them, each its group's.  Cleared ones add nothing.
+__device__ __forceinline__ void clear_total(Total<Sum>& a) { a.E = -kFar; a.s = 0.0; }
+__device__ __forceinline__ void clear_total(Total<SumRef>& a) { a.E = a.Ez = -kFar; a.s = a.x = a.sz = 0.0; }
+__device__ __forceinline__ float group_max(float v, int group) {
+    for (int d = 1; d < group; d <<= 1) v = fmaxf(v, __shfl_xor(v, d, kWave));
+    return v;
+}
+__device__ __forceinline__ double group_sum(double v, int group) {
+    for (int d = 1; d < group; d <<= 1) v += __shfl_xor(v, d, kWave);
+    return v;
+}
+__device__ __forceinline__ Total<Sum> join_group(const Total<Sum>& a, int group) {
+    Total<Sum> r;
+    r.E = group_max(a.E, group);
+    r.s = group_sum(moved(a.s, a.E, r.E), group);
+    return r;
+}
+__device__ __forceinline__ Total<SumRef> join_group(const Total<SumRef>& a, int group) {
+    Total<SumRef> r;
+    r.E = group_max(a.E, group);
+    r.Ez = group_max(a.Ez, group);
+    r.s = group_sum(moved(a.s, a.E, r.E), group);
+    r.x = group_sum(moved(a.x, a.E, r.E), group);
+    r.sz = group_sum(moved(a.sz, a.Ez, r.Ez), group);
+    return r;
+}
 // Over a workgroup; `part` is free again behind the next barrier.
 template <typename S>
 __device__ __forceinline__ Total<S> block_total(const S& a, int threads, Total<S>* part) {
@@ -704,6 +730,7 @@ struct PolicyArgs {
     float* logprobs;  // or NULL
     float* kl;        // or NULL
     double* terms;    // every row's share of the loss
+    float* loss;
 };
 
 struct RowLoss {
@@ -711,9 +738,9 @@ struct RowLoss {
 };
 
 // What a token of the row counts, by any one wave.
+__device__ __forceinline__ double row_norm(const PolicyArgs& a, long row) { return a.norm ? a.norm[(unsigned)row / (unsigned)a.r.T] : a.norm_all; }
 __device__ __forceinline__ double token_norm(const PolicyArgs& a, long row) {
-    if (a.count) return 1.0 / (double)wave_count(a.r.mask, a.r.rows);  // the row itself counts
-    return a.norm ? a.norm[(unsigned)row / (unsigned)a.r.T] : a.norm_all;
+    return a.count ? 1.0 / (double)wave_count(a.r.mask, a.r.rows) : row_norm(a, row);  // the row itself counts
 }
 
 // A row's log-prob, KL and share of the loss, and their gradients, from its sums; hy is its token's logit.
@@ -746,17 +773,20 @@ __device__ __forceinline__ RowLoss row_loss(const PolicyArgs& a, bool far, long 
     return o;
 }
 
-__device__ __forceinline__ void write_policy(const PolicyArgs& a, long row, double lp, double kl, double term) {
+__device__ __forceinline__ float advantage_of(const PolicyArgs& a, long row) {
+    return a.advantages[a.seq_advantages ? (unsigned)row / (unsigned)a.r.T : row];
+}
+__device__ __forceinline__ void write_policy(const PolicyArgs& a, long row, double lp, double kl) {
     if (a.logprobs) a.logprobs[row] = (float)lp;
     if (a.kl) a.kl[row] = (float)kl;
-    a.terms[row] = term;
 }
 // The same written down, and what the gradient needs.
 template <int DT, bool REF, typename S>
 __device__ __forceinline__ RowGrad finish_row(const PolicyArgs& a, bool far, long row, int y, float hy, float old, float advantage, double n,
                                              const Total<S>& s) {
     const RowLoss o = row_loss<REF>(a, far, row, y, hy, old, advantage, n, s);
-    write_policy(a, row, o.lp, o.kl, o.term);
+    write_policy(a, row, o.lp, o.kl);
+    a.terms[row] = o.term;
     return row_grad<DT, REF>(a.r, far, s.E, s.s, o.g, o.k, o.diff, o.kl);
 }
 
@@ -794,7 +824,10 @@ __global__ __launch_bounds__(kMaxThreads) void policy_kernel(const PolicyArgs a)
             const Layout<DT> lay(g, a.r.V, tid);
             zero_slice<DT>(g, lay, tid, lay.vecs, blockDim.x, true);
         }
-        if (tid == 0) write_policy(a, row, 0.0, 0.0, 0.0);
+        if (tid == 0) {
+            write_policy(a, row, 0.0, 0.0);
+            a.terms[row] = 0.0;
+        }
         return;
     }
     const void* const h = row_ptr<DT>(a.r.logits, at);
@@ -803,7 +836,7 @@ __global__ __launch_bounds__(kMaxThreads) void policy_kernel(const PolicyArgs a)
     const bool valid = y >= 0 && y < a.r.V;
     if (helper) {
         const float hy = valid ? ld_elem<DT>(h, y) : 0.f;
-        const float old = a.old_logprobs[row], adv = a.advantages[a.seq_advantages ? (unsigned)row / (unsigned)a.r.T : row];
+        const float old = a.old_logprobs[row], adv = advantage_of(a, row);
         const double n = token_norm(a, row);
         __syncthreads();
         const int lane = tid & 63, waves = threads / kWave;
@@ -889,31 +922,97 @@ __global__ __launch_bounds__(kMaxThreads) void policy_kernel(const PolicyArgs a)
         const double n = token_norm(a, row);
         if (tid == 0)
             shared.grad = finish_row<DT, REF>(a, true, row, y, valid ? ld_elem<DT>(h, y) : 0.f, a.old_logprobs[row],
-                                              a.advantages[a.seq_advantages ? (unsigned)row / (unsigned)a.r.T : row], n, s);
+                                              advantage_of(a, row), n, s);
         __syncthreads();
         const RowGrad rg = shared.grad;
         if (g) far_grad<DT, REF>(h, z, g, a.r.V, rg, y, a.r.c, blockDim.x);
     }
 }
 
-// Rows in slices: every workgroup forms what the row has once for itself, and writes its slice of the gradient.
+// The loss of rows in slices, and what each has once, by one workgroup: a group of lanes a row, a lane a slice.  Rows far from zero it does alone,
+// their gradients among them, one after the other.
+template <int DT, bool REF>
+__device__ __forceinline__ void policy_slices_loss(const PolicyArgs& a, const Slices& p) {
+    using S = typename std::conditional<REF, SumRef, Sum>::type;
+    __shared__ Total<S> part[kSliceThreads / kWave];
+    __shared__ double sums[kSliceThreads / kWave];
+    __shared__ RowGrad shared_grad;
+    __shared__ Total<S> joined[kSliceRows];
+    __shared__ unsigned char far_rows[kSliceRows];
+    static_assert(kSliceRows <= kSliceThreads, "a lane a row");
+    const int tid = threadIdx.x, group = p.n <= 2 ? 2 : 1 << (32 - __clz(p.n - 1)), slice = tid & (group - 1);
+    const double counted = a.count ? 1.0 / (double)wave_count(a.r.mask, a.r.rows) : 0.0;
+#pragma unroll 2
+    for (long first = 0; first < a.r.rows; first += kSliceThreads / group) {
+        const long row = first + tid / group;
+        Total<S> s;
+        clear_total(s);
+        if (row < a.r.rows && slice < p.n && counts(a.r, row)) s = parts_of<S>(p, row)[slice];
+        s = join_group(s, group);
+        if (row < a.r.rows && slice == 0) joined[row] = s;
+    }
+    __syncthreads();
+    double loss = 0.0;
+    bool any_far = false;
+    if (tid < a.r.rows) {
+        const bool kept = counts(a.r, tid);
+        const Total<S> s = joined[tid];
+        any_far = kept && (a.r.far || is_far(s));
+        far_rows[tid] = any_far ? 1 : 0;
+        if (!kept) {
+            write_policy(a, tid, 0.0, 0.0);
+        } else if (!any_far) {
+            const RowLoss o = row_loss<REF>(a, false, tid, a.r.tokens[tid], p.token_logits[tid], a.old_logprobs[tid], advantage_of(a, tid),
+                                            a.count ? counted : row_norm(a, tid), s);
+            write_policy(a, tid, o.lp, o.kl);
+            loss = o.term;
+        }
+    }
+    if (__syncthreads_or(any_far ? 1 : 0)) {
+        for (long row = 0; row < a.r.rows; ++row) {
+            if (!far_rows[row]) continue;
+            long at, grad_at;
+            place(a.r, row, at, grad_at);
+            const void* const h = row_ptr<DT>(a.r.logits, at);
+            const void* const z = REF ? row_ptr<DT>(a.r.ref, at) : nullptr;
+            const int y = a.r.tokens[row];
+            const Total<S> s = far_sum<DT, S>(h, z, a.r.V, a.r.c, kSliceThreads, part);
+            if (tid == 0) {
+                const RowLoss o = row_loss<REF>(a, true, row, y, p.token_logits[row], a.old_logprobs[row], advantage_of(a, row),
+                                                a.count ? counted : row_norm(a, row), s);
+                write_policy(a, row, o.lp, o.kl);
+                loss += o.term;
+                shared_grad = row_grad<DT, REF>(a.r, true, s.E, s.s, o.g, o.k, o.diff, o.kl);
+            }
+            __syncthreads();
+            const RowGrad rg = shared_grad;
+            if (a.r.grad) far_grad<DT, REF>(h, z, const_cast<void*>(row_ptr<DT>(a.r.grad, grad_at)), a.r.V, rg, y, a.r.c, kSliceThreads);
+            __syncthreads();
+        }
+    }
+    loss = block_sum(loss, sums);
+    if (tid == 0) *a.loss = (float)loss;
+}
+
+// Rows in slices: the first workgroup forms the loss, the others, each with what its row has once formed for itself, a slice of the gradient.
 template <int DT, bool REF>
 __global__ __launch_bounds__(kSliceThreads) void policy_slices_kernel(const PolicyArgs a, const Slices p) {
     using S = typename std::conditional<REF, SumRef, Sum>::type;
-    __shared__ Total<S> part[kSliceThreads / kWave];
-    __shared__ RowGrad shared_grad;
-    const long row = blockIdx.x / (unsigned)p.n;
-    const int slice = (int)(blockIdx.x - row * p.n);
+    if (blockIdx.x == 0) {
+        policy_slices_loss<DT, REF>(a, p);
+        return;
+    }
+    const long row = (blockIdx.x - 1) / (unsigned)p.n;
+    const int slice = (int)(blockIdx.x - 1 - row * p.n);
     long at, grad_at;
     place(a.r, row, at, grad_at);
-    void* const g = a.r.grad ? const_cast<void*>(row_ptr<DT>(a.r.grad, grad_at)) : nullptr;
+    void* const g = const_cast<void*>(row_ptr<DT>(a.r.grad, grad_at));
     const void* const h = row_ptr<DT>(a.r.logits, at);
     const void* const z = REF ? row_ptr<DT>(a.r.ref, at) : nullptr;
-    const Layout<DT> lay(g ? g : h, a.r.V, threadIdx.x);
+    const Layout<DT> lay(g, a.r.V, threadIdx.x);
     const int first = slice * p.vecs + threadIdx.x, end = slice + 1 == p.n ? lay.vecs : min(lay.vecs, (slice + 1) * p.vecs);
     if (!counts(a.r, row)) {
-        if (g) zero_slice<DT>(g, lay, first, end, kSliceThreads, slice == 0);
-        if (slice == 0 && threadIdx.x == 0) write_policy(a, row, 0.0, 0.0, 0.0);
+        zero_slice<DT>(g, lay, first, end, kSliceThreads, slice == 0);
         return;
     }
     // the first vectors are on their way while the row's sums are joined
@@ -921,7 +1020,7 @@ __global__ __launch_bounds__(kSliceThreads) void policy_slices_kernel(const Poli
     typename Row<DT>::Raw r[kAhead], rz[kAhead];
     const char* const hv = static_cast<const char*>(h) + (long)lay.head * (DT == SS_BF16 ? 2 : 4);
     const char* const zv = REF ? static_cast<const char*>(z) + (long)lay.head * (DT == SS_BF16 ? 2 : 4) : nullptr;
-    if (g && lay.vecs > 0) {
+    if (lay.vecs > 0) {
 #pragma unroll
         for (int u = 0; u < kAhead; ++u) {
             const int i = min(first + u * kSliceThreads, lay.vecs - 1);
@@ -930,25 +1029,9 @@ __global__ __launch_bounds__(kSliceThreads) void policy_slices_kernel(const Poli
         }
     }
     const Total<S> s = join_slices<S>(p, row);
-    const float old = a.old_logprobs[row], adv = a.advantages[a.seq_advantages ? (unsigned)row / (unsigned)a.r.T : row];
+    if (a.r.far || is_far(s)) return;
     const int y = a.r.tokens[row];
-    const double n = token_norm(a, row);
-    if (a.r.far || is_far(s)) {  // the row's first workgroup alone
-        if (slice != 0) return;
-        const Total<S> sf = far_sum<DT, S>(h, z, a.r.V, a.r.c, kSliceThreads, part);
-        if (threadIdx.x == 0) {
-            const RowLoss o = row_loss<REF>(a, true, row, y, p.token_logits[row], old, adv, n, sf);
-            write_policy(a, row, o.lp, o.kl, o.term);
-            shared_grad = row_grad<DT, REF>(a.r, true, sf.E, sf.s, o.g, o.k, o.diff, o.kl);
-        }
-        __syncthreads();
-        const RowGrad rg = shared_grad;
-        if (g) far_grad<DT, REF>(h, z, g, a.r.V, rg, y, a.r.c, kSliceThreads);
-        return;
-    }
-    const RowLoss o = row_loss<REF>(a, false, row, y, p.token_logits[row], old, adv, n, s);
-    if (slice == 0 && threadIdx.x == 0) write_policy(a, row, o.lp, o.kl, o.term);
-    if (!g) return;
+    const RowLoss o = row_loss<REF>(a, false, row, y, p.token_logits[row], a.old_logprobs[row], advantage_of(a, row), token_norm(a, row), s);
     const RowGrad rg = row_grad<DT, REF>(a.r, false, s.E, s.s, o.g, o.k, o.diff, o.kl);
     write_grad<DT, REF>(h, z, g, lay, rg, y, first, end, kSliceThreads, slice == 0, a.r.c, kAhead, r, rz);
 }
@@ -1143,17 +1226,19 @@ void launch_grad(const ss_loss_params& p, GradArgs& a, hipStream_t q) {
     launch(p.dtype == SS_BF16 ? grad_kernel<SS_BF16> : grad_kernel<SS_F32>, row_grid(a.r.rows * a.slices), dim3(kGradThreads), 0, q, a);
 }
 
+// The loss is left to the caller to sum unless true comes back.
 template <bool REF>
-void launch_policy(const ss_loss_params& p, const PolicyArgs& a, const LossScratch& w, void* workspace, hipStream_t q) {
+bool launch_policy(const ss_loss_params& p, const PolicyArgs& a, const LossScratch& w, void* workspace, hipStream_t q) {
     constexpr int kHeld = REF ? kHeldPairs : kHeldVecs;
     Slices c;
     if (launch_slices<typename std::conditional<REF, SumRef, Sum>::type>(p, a.r, w, workspace, row_slices(a.r.rows, row_vecs(p)), c, q)) {
-        const unsigned groups = (unsigned)(a.r.rows * c.n);
+        const unsigned groups = 1 + (a.r.grad ? (unsigned)(a.r.rows * c.n) : 0u);
         launch(p.dtype == SS_BF16 ? policy_slices_kernel<SS_BF16, REF> : policy_slices_kernel<SS_F32, REF>, dim3(groups), dim3(kSliceThreads), 0, q, a, c);
-        return;
+        return true;
     }
     void (*const k)(PolicyArgs) = p.dtype == SS_BF16 ? policy_kernel<SS_BF16, REF, kHeld> : policy_kernel<SS_F32, REF, kHeld>;
     launch(k, row_grid(a.r.rows), dim3((unsigned)(kWave * call_waves(a.r.rows, device_cu_count(), row_vecs(p), kHeld))), 0, q, a);
+    return false;
 }
 
 }  // namespace
@@ -1235,9 +1320,9 @@ ss_status specsteer_policy_loss(const void* logits, const void* ref_logits, cons
                (policy->flags & SS_LOSS_SEQ_MEAN) ? 1 : 0, norm);
         a.norm = norm;
     }
-    if (ref_logits) launch_policy<true>(*params, a, w, workspace, q);
-    else launch_policy<false>(*params, a, w, workspace, q);
-    launch(sum_kernel, dim3(1), dim3(kOneThreads), 0, q, static_cast<const double*>(a.terms), s.rows, 1.0, loss);
+    a.loss = loss;
+    const bool summed = ref_logits ? launch_policy<true>(*params, a, w, workspace, q) : launch_policy<false>(*params, a, w, workspace, q);
+    if (!summed) launch(sum_kernel, dim3(1), dim3(kOneThreads), 0, q, static_cast<const double*>(a.terms), s.rows, 1.0, loss);
     return launched();
 }
 

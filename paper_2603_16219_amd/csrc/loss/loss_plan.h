@@ -73,8 +73,8 @@ struct LossScratch {
 };
 
 // Workgroups that a row of so many vectors takes: about 1024 in all, 512 vectors each at least.  In a third of the compute units and less one
-// workgroup a row leaves most of them idle: the policy loss of one row of V = 128256 bf16 20 us in one workgroup, 8.5 in slices (two launches
-// instead of one), of 16 20.9 and 11, of 64 21.2 and 15.4, of 100 21.4 and 18.9, of 128 21.7 and 23.3; of 32 rows of V = 32000 11 and 9.3.
+// workgroup a row leaves most of them idle: the policy loss of one row of V = 128256 bf16 20 us in one workgroup, 6.7 in slices, of 16 20.9 and
+// 9.3, of 64 21.2 and 15.1, of 100 21.4 and 19.4, of 128 21.6 and 23.3; of 4 rows of V = 32000 10.4 and 6.4, of 32 11 and 7.9.
 // Log-probs alone gain less: of rows up to 8192 vectors, 8 a lane of a workgroup, they are faster in one (4 of V = 32000 fp32 4.5 and 5.2 us; of
 // V = 50257 6.5 and 5.2).
 constexpr int kMaxRowSlices = 64, kPartBytes = 32;
