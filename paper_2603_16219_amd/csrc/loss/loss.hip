@@ -97,13 +97,15 @@ __device__ __forceinline__ void st_vec(void* p, long vec, const float (&h)[Row<D
 
 // ------------------------------------------------------------------ statistics of a row
 
-// c = log2(e) / tau in two fp32 parts, the first of 16 bits, so that a bf16 logit's product with it is exact; as one fp32 number and the
-// rest; and 1 / tau.
+// c = log2(e) / tau in two fp32 parts, the first of 16 bits, so that a bf16 logit's product with it is exact; as one fp32 number; and 1 / tau.
 struct Factor {
-    float hi, lo, whole, rest, inv_tau;
+    float hi, lo, whole, inv_tau;
 };
-// 2^(h c - E)
-__device__ __forceinline__ float term(float h, float E, Factor c) { return exp2_hw(fmaf(h, c.lo, fmaf(h, c.hi, -E))); }
+// 2^(h c - E), c in two parts or as one number
+template <int PARTS>
+__device__ __forceinline__ float term(float h, float E, Factor c) {
+    return exp2_hw(PARTS == 2 ? fmaf(h, c.lo, fmaf(h, c.hi, -E)) : fmaf(h, c.whole, -E));
+}
 
 // h - z, and a number for a token that the policy masks (-inf - -inf among them), whose term is 0 then.  +inf where the reference alone
 // masks one.
@@ -136,10 +138,13 @@ __device__ __forceinline__ void merge(SumRef& a, const SumRef& b) {
 }
 
 template <int N>
-__device__ __forceinline__ void raise(float& E, float& s, float& x, const float (&h)[N], Factor c) {
+__device__ __forceinline__ float largest(const float (&h)[N]) {
     float top = h[0];
 #pragma unroll
     for (int i = 1; i < N; ++i) top = fmaxf(top, h[i]);
+    return top;
+}
+__device__ __forceinline__ void raise(float& E, float& s, float& x, float top, Factor c) {
     top = fmaf(top, c.hi, -kBelow);
     if (top > E) {
         const float to = fminf(ceilf(top), 2.f * kFar);
@@ -156,24 +161,39 @@ __device__ __forceinline__ float tree_sum(float (&e)[N]) {
         for (int i = 0; i < w; ++i) e[i] += e[i + w];
     return e[0];
 }
-template <int N>
+template <int PARTS, int N>
+__device__ __forceinline__ void add_under(Sum& a, const float (&h)[N], Factor c);
+template <int PARTS, int N>
 __device__ __forceinline__ void add(Sum& a, const float (&h)[N], Factor c) {
-    float none = 0.f, e[N];
-    raise(a.E, a.s, none, h, c);
+    float none = 0.f;
+    raise(a.E, a.s, none, largest(h), c);
+    add_under<PARTS>(a, h, c);
+}
+// The same where the reference is as high as it has to be.
+template <int PARTS, int N>
+__device__ __forceinline__ void add_under(Sum& a, const float (&h)[N], Factor c) {
+    float e[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i) e[i] = term(h[i], a.E, c);
+    for (int i = 0; i < N; ++i) e[i] = term<PARTS>(h[i], a.E, c);
     a.s += tree_sum(e);
 }
-template <int N>
+template <int PARTS, int N>
+__device__ __forceinline__ void add_under(SumRef& a, const float (&h)[N], const float (&z)[N], Factor c);
+template <int PARTS, int N>
 __device__ __forceinline__ void add(SumRef& a, const float (&h)[N], const float (&z)[N], Factor c) {
-    float none = 0.f, e[N], ez[N], x[N];
-    raise(a.E, a.s, a.x, h, c);
-    raise(a.Ez, a.sz, none, z, c);
+    float none = 0.f;
+    raise(a.E, a.s, a.x, largest(h), c);
+    raise(a.Ez, a.sz, none, largest(z), c);
+    add_under<PARTS>(a, h, z, c);
+}
+template <int PARTS, int N>
+__device__ __forceinline__ void add_under(SumRef& a, const float (&h)[N], const float (&z)[N], Factor c) {
+    float e[N], ez[N], x[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        e[i] = term(h[i], a.E, c);
+        e[i] = term<PARTS>(h[i], a.E, c);
         x[i] = e[i] * logit_diff(h[i], z[i]);
-        ez[i] = term(z[i], a.Ez, c);
+        ez[i] = term<PARTS>(z[i], a.Ez, c);
     }
     a.s += tree_sum(e);
     a.x += tree_sum(x);
@@ -283,6 +303,7 @@ struct Rows {
     int far;               // all rows take the sweeps for those far from zero
     double c64;
     double inv_tau, scale; // 1 / tau, the gradient's factor
+    double rest;           // what c as one fp32 number leaves out, in shares of it
 };
 
 // The row of a workgroup.  Rows of a call are spread over two dimensions, in either of which a launch holds less than 2^32 lanes.
@@ -306,7 +327,7 @@ __device__ __forceinline__ void zero_slice(void* g, const Layout<DT>& lay, int f
 }
 
 // One lane's share of a row: vectors [first, end) by step, and its extra element if `extra`.
-template <int DT, typename S, bool ONCE = false>
+template <int DT, typename S, int PARTS, bool ONCE = false>
 __device__ __forceinline__ S lane_sum(const void* h, const void* z, const Layout<DT>& lay, int first, int end, int step, bool extra, Factor c) {
     constexpr int kVec = Row<DT>::kVec, kUnroll = 4, kElem = DT == SS_BF16 ? 2 : 4;
     constexpr bool kRef = std::is_same<S, SumRef>::value;
@@ -320,9 +341,9 @@ __device__ __forceinline__ S lane_sum(const void* h, const void* z, const Layout
         if constexpr (kRef) {
             float y[kVec];
             unpack(rz, y);
-            add(a, x, y, c);
+            add<PARTS>(a, x, y, c);
         } else {
-            add(a, x, c);
+            add<PARTS>(a, x, c);
         }
     };
     int i = first;
@@ -345,9 +366,9 @@ __device__ __forceinline__ S lane_sum(const void* h, const void* z, const Layout
         const float x[1] = {ld_elem<DT>(h, lay.extra)};
         if constexpr (kRef) {
             const float y[1] = {ld_elem<DT>(z, lay.extra)};
-            add(a, x, y, c);
+            add<PARTS>(a, x, y, c);
         } else {
-            add(a, x, c);
+            add<PARTS>(a, x, c);
         }
     }
     return a;
@@ -411,13 +432,13 @@ struct RowGrad {
 };
 
 // g = weight of the row's log-prob, k that of its KL, both with the call's factor; diff = D, the difference of the log-sum-exps.
-// bf16 gradients are formed with c as one number: what its rest adds at the reference goes into the factor here, and the rest is below
-// 2^-24 of |h c - E|, which half a step of the result is thousands of times.
-template <int DT, bool REF>
+// Gradients are formed with c as one number: where the sums are not, what its rest adds at the reference goes into the factor here, and what is
+// left is 2^-24 of |h c - E| of a term.
+template <int DT, bool REF, int PARTS>
 __device__ __forceinline__ RowGrad row_grad(const Rows& a, bool far, float E, double s, double g, double k, double diff, double kl) {
     RowGrad r;
     double f = a.inv_tau / s;
-    if (DT == SS_BF16 && !far) f *= (double)exp2_hw(E * (a.c.rest / a.c.whole));
+    if (PARTS == 2 && !far) f *= (double)exp2_hw(E * (float)a.rest);
     r.E = E;
     r.scale = (float)((REF ? -g - k * (diff + kl) : -g) * f);
     r.cross = REF ? (float)(k * (far ? 1.0 : a.inv_tau) * f) : 0.f;
@@ -432,7 +453,7 @@ __device__ __forceinline__ float grad_of_term(const RowGrad& r, float e, float h
 }
 template <int DT, bool REF>
 __device__ __forceinline__ float grad_of(const RowGrad& r, float h, float z, Factor c) {
-    return grad_of_term<REF>(r, DT == SS_BF16 ? exp2_hw(fmaf(h, c.whole, -r.E)) : term(h, r.E, c), h, z);
+    return grad_of_term<REF>(r, term<1>(h, r.E, c), h, z);
 }
 
 // The gradient of a row far from zero, element by element over a workgroup.
@@ -500,16 +521,24 @@ __device__ __forceinline__ void write_grad(const void* h, const void* z, void* g
 }
 
 __device__ __forceinline__ double nan64() { return __longlong_as_double(0x7FF8000000000000ll); }
+// What a sum's reference is worth.  In sums with c as one number the terms that carry them lie near the reference, where c's rest moves all of them
+// alike; what is left out then is 2^-24 of their distances to it.
+template <int PARTS>
+__device__ __forceinline__ double reference(const Rows& a, float E) { return PARTS == 2 ? (double)E : (double)E * (1.0 + a.rest); }
+
 // log P(y) of a row's token with logit h, from the row's sums
+template <int PARTS>
 __device__ __forceinline__ double token_logprob(const Rows& a, bool far, int token, float h, float E, double s) {
     if (token < 0 || token >= a.V) return nan64();
     if (far) return ((double)h - (double)E) * a.inv_tau - log(s);
-    return ((double)h * a.c64 - (double)E - log2(s)) * kLn2;
+    return ((double)h * a.c64 - reference<PARTS>(a, E) - log2(s)) * kLn2;
 }
 // log-sum-exp of the policy's row less that of the reference's
+template <int PARTS>
 __device__ __forceinline__ double lse_difference(const Rows& a, bool far, const Total<SumRef>& s) {
-    const double sums = log2(s.s) - log2(s.sz), by = (double)s.E - (double)s.Ez;
-    return far ? by * a.inv_tau + sums * kLn2 : (by + sums) * kLn2;
+    const double sums = log2(s.s) - log2(s.sz);
+    if (far) return ((double)s.E - (double)s.Ez) * a.inv_tau + sums * kLn2;
+    return (reference<PARTS>(a, s.E) - reference<PARTS>(a, s.Ez) + sums) * kLn2;
 }
 
 // The sum of x over the workgroup, in every lane of wave 0.  The order is fixed.
@@ -570,7 +599,7 @@ __device__ __forceinline__ void score_far_row(const ScoreArgs& a, long row, int 
     const Total<Sum> s = far_sum<DT, Sum>(h, nullptr, a.r.V, a.r.c, threads, part);
     if (threadIdx.x == 0) {
         const int y = a.r.tokens[row];
-        write_score(a, row, token_logprob(a.r, true, y, y >= 0 && y < a.r.V ? ld_elem<DT>(h, y) : 0.f, s.E, s.s), s.E, -s.s);
+        write_score(a, row, token_logprob<2>(a.r, true, y, y >= 0 && y < a.r.V ? ld_elem<DT>(h, y) : 0.f, s.E, s.s), s.E, -s.s);
     }
 }
 
@@ -590,13 +619,13 @@ __global__ __launch_bounds__(kMaxThreads) void score_kernel(const ScoreArgs a) {
     place(a.r, row, at, grad_at);
     const void* const h = row_ptr<DT>(a.r.logits, at);
     const Layout<DT> lay(h, a.r.V, threadIdx.x);
-    const Sum mine = lane_sum<DT, Sum, true>(h, nullptr, lay, threadIdx.x, lay.vecs, threads, true, a.r.c);
+    const Sum mine = lane_sum<DT, Sum, 2, true>(h, nullptr, lay, threadIdx.x, lay.vecs, threads, true, a.r.c);
     const Total<Sum> s = block_total(mine, threads, part);
     if (is_far(s)) {
         score_far_row<DT>(a, row, threads, part);
     } else if (threadIdx.x == 0) {
         const int y = a.r.tokens[row];
-        write_score(a, row, token_logprob(a.r, false, y, y >= 0 && y < a.r.V ? ld_elem<DT>(h, y) : 0.f, s.E, s.s), s.E, s.s);
+        write_score(a, row, token_logprob<2>(a.r, false, y, y >= 0 && y < a.r.V ? ld_elem<DT>(h, y) : 0.f, s.E, s.s), s.E, s.s);
     }
 }
 
@@ -625,7 +654,7 @@ __global__ __launch_bounds__(kSliceThreads) void slice_kernel(const Rows r, cons
     const void* const z = std::is_same<S, SumRef>::value ? row_ptr<DT>(r.ref, at) : nullptr;
     const Layout<DT> lay(h, r.V, threadIdx.x);
     const int end = slice + 1 == p.n ? lay.vecs : min(lay.vecs, (slice + 1) * p.vecs);
-    const S mine = lane_sum<DT, S>(h, z, lay, slice * p.vecs + threadIdx.x, end, kSliceThreads, slice == 0, r.c);
+    const S mine = lane_sum<DT, S, 2>(h, z, lay, slice * p.vecs + threadIdx.x, end, kSliceThreads, slice == 0, r.c);
     const Total<S> s = block_total(mine, kSliceThreads, part);
     if (threadIdx.x == 0) {
         parts_of<S>(p, row)[slice] = s;
@@ -652,7 +681,7 @@ __device__ __forceinline__ bool score_joined(const ScoreArgs& a, const Slices& p
     }
     const Total<Sum> s = join_slices<Sum>(p, row);
     if (is_far(s)) return true;
-    if (first) write_score(a, row, token_logprob(a.r, false, a.r.tokens[row], p.token_logits[row], s.E, s.s), s.E, s.s);
+    if (first) write_score(a, row, token_logprob<2>(a.r, false, a.r.tokens[row], p.token_logits[row], s.E, s.s), s.E, s.s);
     return false;
 }
 
@@ -707,7 +736,7 @@ __global__ __launch_bounds__(kGradThreads) void grad_kernel(const GradArgs a) {
     if (y < 0 || y >= a.r.V) w = nan64();
     const float s = a.stats[2 * row + 1];
     const bool far = s < 0.f;
-    const RowGrad rg = row_grad<DT, false>(a.r, far, a.stats[2 * row], fabsf(s), w, 0.0, 0.0, 0.0);
+    const RowGrad rg = row_grad<DT, false, 2>(a.r, far, a.stats[2 * row], fabsf(s), w, 0.0, 0.0, 0.0);
     if (far) {
         if (slice == 0) far_grad<DT, false>(h, nullptr, g, a.r.V, rg, y, a.r.c, kGradThreads);
         return;
@@ -744,12 +773,12 @@ __device__ __forceinline__ double token_norm(const PolicyArgs& a, long row) {
 }
 
 // A row's log-prob, KL and share of the loss, and their gradients, from its sums; hy is its token's logit.
-template <bool REF, typename S>
+template <bool REF, int PARTS, typename S>
 __device__ __forceinline__ RowLoss row_loss(const PolicyArgs& a, bool far, long row, int y, float hy, float old, float advantage, double n,
                                                const Total<S>& s) {
     RowLoss o;
     const double adv = advantage;
-    o.lp = token_logprob(a.r, far, y, hy, s.E, s.s);
+    o.lp = token_logprob<PARTS>(a.r, far, y, hy, s.E, s.s);
     o.kl = o.k = o.diff = 0.0;
     const double ratio = exp(o.lp - (double)old);
     const double plain = ratio * adv, bound = fmin(fmax(ratio, a.clip_lo), a.clip_hi) * adv;
@@ -757,7 +786,7 @@ __device__ __forceinline__ RowLoss row_loss(const PolicyArgs& a, bool far, long 
     o.term = clipped ? -bound : -plain;
     o.g = clipped ? 0.0 : -plain;
     if constexpr (REF) {
-        o.diff = lse_difference(a.r, far, s);
+        o.diff = lse_difference<PARTS>(a.r, far, s);
         o.kl = s.x / s.s * a.r.inv_tau - o.diff;
         if (o.kl < 0.0) o.kl = 0.0;  // by rounding only
         o.k = a.kl_coef;
@@ -784,10 +813,10 @@ __device__ __forceinline__ void write_policy(const PolicyArgs& a, long row, doub
 template <int DT, bool REF, typename S>
 __device__ __forceinline__ RowGrad finish_row(const PolicyArgs& a, bool far, long row, int y, float hy, float old, float advantage, double n,
                                              const Total<S>& s) {
-    const RowLoss o = row_loss<REF>(a, far, row, y, hy, old, advantage, n, s);
+    const RowLoss o = row_loss<REF, 1>(a, far, row, y, hy, old, advantage, n, s);
     write_policy(a, row, o.lp, o.kl);
     a.terms[row] = o.term;
-    return row_grad<DT, REF>(a.r, far, s.E, s.s, o.g, o.k, o.diff, o.kl);
+    return row_grad<DT, REF, 1>(a.r, far, s.E, s.s, o.g, o.k, o.diff, o.kl);
 }
 
 // The compiler is not to keep anything it has formed of a held vector (its logits widened, twice the registers) for the next use.
@@ -865,23 +894,31 @@ __global__ __launch_bounds__(kMaxThreads) void policy_kernel(const PolicyArgs a)
         S sums;
         clear(sums);
 #pragma unroll
-        for (int u = 0; u < NV; ++u) {
+        for (int u = 0; u < NV; u += 2) {  // one look at the reference for two vectors
             if (u * threads >= lay.vecs) break;
-            if ((u + 1) * threads > lay.vecs && tid >= lay.vecs - u * threads) {
-                r[u] = neg_inf_raw<DT, kVec>();
-                if constexpr (REF) rz[u] = r[u];
+            float x[2][kVec], w[2][kVec];
+#pragma unroll
+            for (int v = 0; v < 2; ++v) {
+                if ((u + v + 1) * threads > lay.vecs && tid >= lay.vecs - (u + v) * threads) {
+                    r[u + v] = neg_inf_raw<DT, kVec>();
+                    if constexpr (REF) rz[u + v] = r[u + v];
+                }
+                unpack(r[u + v], x[v]);
+                if constexpr (REF) unpack(rz[u + v], w[v]);
             }
-            float x[kVec];
-            unpack(r[u], x);
+            float none = 0.f;
             if constexpr (REF) {
-                float w[kVec];
-                unpack(rz[u], w);
-                add(sums, x, w, a.r.c);
+                raise(sums.E, sums.s, sums.x, fmaxf(largest(x[0]), largest(x[1])), a.r.c);
+                raise(sums.Ez, sums.sz, none, fmaxf(largest(w[0]), largest(w[1])), a.r.c);
+                add_under<1>(sums, x[0], w[0], a.r.c);
+                add_under<1>(sums, x[1], w[1], a.r.c);
             } else {
-                add(sums, x, a.r.c);
+                raise(sums.E, sums.s, none, fmaxf(largest(x[0]), largest(x[1])), a.r.c);
+                add_under<1>(sums, x[0], a.r.c);
+                add_under<1>(sums, x[1], a.r.c);
             }
         }
-        const S rest = lane_sum<DT, S>(h, z, lay, tid + NV * threads, lay.vecs, threads, true, a.r.c);
+        const S rest = lane_sum<DT, S, 1>(h, z, lay, tid + NV * threads, lay.vecs, threads, true, a.r.c);
         merge(sums, rest);
         const Total<S> mine = wave_total(sums);
         if ((tid & 63) == 0) part[tid >> 6] = mine;
@@ -895,20 +932,21 @@ __global__ __launch_bounds__(kMaxThreads) void policy_kernel(const PolicyArgs a)
             const int e = y - lay.head, vec = e / kVec;
             const bool mine = valid && e >= 0 && vec < min(lay.vecs, NV * threads) && vec % threads == tid;
             const float hy = mine ? ld_elem<DT>(h, y) : 0.f, zy = REF && mine ? ld_elem<DT>(z, y) : 0.f;
+            const auto write_held = [&](const Raw& raw, const Raw& rawz, int u) {
+                float x[kVec], w[kVec];
+                unpack(raw, x);
+                if constexpr (REF) unpack(rawz, w);
+#pragma unroll
+                for (int j = 0; j < kVec; ++j) x[j] = grad_of<DT, REF>(rg, x[j], REF ? w[j] : 0.f, a.r.c);
+                st_vec<DT>(gv + (long)(u * threads) * 16 + (unsigned)tid * 16u, 0, x);
+            };
 #pragma unroll
             for (int u = 0; u < NV; ++u) {
                 if (u * threads >= lay.vecs) break;
                 if (tid < lay.vecs - u * threads) {
-                    float x[kVec], w[kVec];
                     forget(r[u]);
-                    unpack(r[u], x);
-                    if constexpr (REF) {
-                        forget(rz[u]);
-                        unpack(rz[u], w);
-                    }
-#pragma unroll
-                    for (int j = 0; j < kVec; ++j) x[j] = grad_of<DT, REF>(rg, x[j], REF ? w[j] : 0.f, a.r.c);
-                    st_vec<DT>(gv + (long)(u * threads) * 16 + (unsigned)tid * 16u, 0, x);
+                    if constexpr (REF) forget(rz[u]);
+                    write_held(r[u], rz[REF ? u : 0], u);
                 }
             }
             if (mine) {
@@ -962,7 +1000,7 @@ __device__ __forceinline__ void policy_slices_loss(const PolicyArgs& a, const Sl
         if (!kept) {
             write_policy(a, tid, 0.0, 0.0);
         } else if (!any_far) {
-            const RowLoss o = row_loss<REF>(a, false, tid, a.r.tokens[tid], p.token_logits[tid], a.old_logprobs[tid], advantage_of(a, tid),
+            const RowLoss o = row_loss<REF, 2>(a, false, tid, a.r.tokens[tid], p.token_logits[tid], a.old_logprobs[tid], advantage_of(a, tid),
                                             a.count ? counted : row_norm(a, tid), s);
             write_policy(a, tid, o.lp, o.kl);
             loss = o.term;
@@ -978,11 +1016,11 @@ __device__ __forceinline__ void policy_slices_loss(const PolicyArgs& a, const Sl
             const int y = a.r.tokens[row];
             const Total<S> s = far_sum<DT, S>(h, z, a.r.V, a.r.c, kSliceThreads, part);
             if (tid == 0) {
-                const RowLoss o = row_loss<REF>(a, true, row, y, p.token_logits[row], a.old_logprobs[row], advantage_of(a, row),
+                const RowLoss o = row_loss<REF, 2>(a, true, row, y, p.token_logits[row], a.old_logprobs[row], advantage_of(a, row),
                                                 a.count ? counted : row_norm(a, row), s);
                 write_policy(a, row, o.lp, o.kl);
                 loss += o.term;
-                shared_grad = row_grad<DT, REF>(a.r, true, s.E, s.s, o.g, o.k, o.diff, o.kl);
+                shared_grad = row_grad<DT, REF, 2>(a.r, true, s.E, s.s, o.g, o.k, o.diff, o.kl);
             }
             __syncthreads();
             const RowGrad rg = shared_grad;
@@ -1031,8 +1069,8 @@ __global__ __launch_bounds__(kSliceThreads) void policy_slices_kernel(const Poli
     const Total<S> s = join_slices<S>(p, row);
     if (a.r.far || is_far(s)) return;
     const int y = a.r.tokens[row];
-    const RowLoss o = row_loss<REF>(a, false, row, y, p.token_logits[row], a.old_logprobs[row], advantage_of(a, row), token_norm(a, row), s);
-    const RowGrad rg = row_grad<DT, REF>(a.r, false, s.E, s.s, o.g, o.k, o.diff, o.kl);
+    const RowLoss o = row_loss<REF, 2>(a, false, row, y, p.token_logits[row], a.old_logprobs[row], advantage_of(a, row), token_norm(a, row), s);
+    const RowGrad rg = row_grad<DT, REF, 2>(a.r, false, s.E, s.s, o.g, o.k, o.diff, o.kl);
     write_grad<DT, REF>(h, z, g, lay, rg, y, first, end, kSliceThreads, slice == 0, a.r.c, kAhead, r, rz);
 }
 
@@ -1180,11 +1218,11 @@ Rows make_rows(const void* logits, const void* ref, void* grad, const int32_t* t
     r.c.hi = (float)std::ldexp(std::floor(std::ldexp(frac, 16)), e - 16);
     r.c.lo = std::fmax((float)(r.c64 - (double)r.c.hi), 1.1754944e-38f);
     r.c.whole = (float)r.c64;
-    r.c.rest = (float)(r.c64 - (double)r.c.whole);
     r.c.inv_tau = (float)(1.0 / (double)p.temperature);
     r.far = !(p.temperature > 1e-12f && p.temperature < 1e12f);  // 1 / tau^2 is a factor otherwise, which fp32 may not hold
     r.inv_tau = 1.0 / (double)p.temperature;
     r.scale = (double)p.grad_scale;
+    r.rest = (r.c64 - (double)r.c.whole) / (double)r.c.whole;
     return r;
 }
 
@@ -1231,13 +1269,14 @@ template <bool REF>
 bool launch_policy(const ss_loss_params& p, const PolicyArgs& a, const LossScratch& w, void* workspace, hipStream_t q) {
     constexpr int kHeld = REF ? kHeldPairs : kHeldVecs;
     Slices c;
-    if (launch_slices<typename std::conditional<REF, SumRef, Sum>::type>(p, a.r, w, workspace, row_slices(a.r.rows, row_vecs(p)), c, q)) {
+    const int vecs = row_vecs(p);
+    if (launch_slices<typename std::conditional<REF, SumRef, Sum>::type>(p, a.r, w, workspace, row_slices(a.r.rows, vecs), c, q)) {
         const unsigned groups = 1 + (a.r.grad ? (unsigned)(a.r.rows * c.n) : 0u);
         launch(p.dtype == SS_BF16 ? policy_slices_kernel<SS_BF16, REF> : policy_slices_kernel<SS_F32, REF>, dim3(groups), dim3(kSliceThreads), 0, q, a, c);
         return true;
     }
-    void (*const k)(PolicyArgs) = p.dtype == SS_BF16 ? policy_kernel<SS_BF16, REF, kHeld> : policy_kernel<SS_F32, REF, kHeld>;
-    launch(k, row_grid(a.r.rows), dim3((unsigned)(kWave * call_waves(a.r.rows, device_cu_count(), row_vecs(p), kHeld))), 0, q, a);
+    launch(p.dtype == SS_BF16 ? policy_kernel<SS_BF16, REF, kHeld> : policy_kernel<SS_F32, REF, kHeld>, row_grid(a.r.rows),
+           dim3((unsigned)(kWave * call_waves(a.r.rows, device_cu_count(), vecs, kHeld))), 0, q, a);
     return false;
 }
 
