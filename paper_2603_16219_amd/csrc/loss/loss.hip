@@ -572,7 +572,9 @@ __device__ __forceinline__ int wave_count(const uint8_t* m, long n) {
 
 // ------------------------------------------------------------------ token log-probs
 
-constexpr int kRowThreads = 512;
+// Threads of a workgroup that sums a row, and of one for a row of up to kShortVecs vectors, where half as many waves start for nothing at rows
+// that do not count (8192 of 16384 rows of V = 32000 bf16 104 us in 512, 98 in 256; 1024 rows of V = 151936 50 in either).
+constexpr int kRowThreads = 512, kShortThreads = 256, kShortVecs = 4096;
 constexpr int kMaxThreads = kWave * kUnitWaves;
 
 struct ScoreArgs {
@@ -580,6 +582,7 @@ struct ScoreArgs {
     float* logprobs;    // or NULL
     float* stats;       // or NULL
     double* logprob64;  // or NULL
+    long keep_from;     // rows from here on are read through the caches, for a gradient that reads them again soon
 };
 
 __device__ __forceinline__ void write_score(const ScoreArgs& a, long row, double lp, float E, double s) {
@@ -619,7 +622,8 @@ __global__ __launch_bounds__(kMaxThreads) void score_kernel(const ScoreArgs a) {
     place(a.r, row, at, grad_at);
     const void* const h = row_ptr<DT>(a.r.logits, at);
     const Layout<DT> lay(h, a.r.V, threadIdx.x);
-    const Sum mine = lane_sum<DT, Sum, 2, true>(h, nullptr, lay, threadIdx.x, lay.vecs, threads, true, a.r.c);
+    const Sum mine = row >= a.keep_from ? lane_sum<DT, Sum, 2, false>(h, nullptr, lay, threadIdx.x, lay.vecs, threads, true, a.r.c)
+                                        : lane_sum<DT, Sum, 2, true>(h, nullptr, lay, threadIdx.x, lay.vecs, threads, true, a.r.c);
     const Total<Sum> s = block_total(mine, threads, part);
     if (is_far(s)) {
         score_far_row<DT>(a, row, threads, part);
@@ -716,10 +720,11 @@ constexpr int kGradThreads = 256, kGradVecs = kGradThreads * 4;
 
 template <int DT>
 __global__ __launch_bounds__(kGradThreads) void grad_kernel(const GradArgs a) {
-    const long id = this_row();
+    // from the last row on: what the sums' sweep read last may be in the caches still
+    const long id = a.r.rows * a.slices - 1 - this_row();
+    if (id < 0) return;
     const long row = (unsigned)id / (unsigned)a.slices;
     const int slice = (int)(id - row * a.slices);
-    if (row >= a.r.rows) return;
     long at, grad_at;
     place(a.r, row, at, grad_at);
     void* const g = const_cast<void*>(row_ptr<DT>(a.r.grad, grad_at));
@@ -1255,7 +1260,7 @@ void launch_score(const ss_loss_params& p, const ScoreArgs& a, const LossScratch
                dim3(kSliceThreads), 0, q, a, c);
         return;
     }
-    launch(p.dtype == SS_BF16 ? score_kernel<SS_BF16> : score_kernel<SS_F32>, row_grid(a.r.rows), dim3(a.r.rows <= device_cu_count() ? kMaxThreads : kRowThreads), 0, q, a);
+    launch(p.dtype == SS_BF16 ? score_kernel<SS_BF16> : score_kernel<SS_F32>, row_grid(a.r.rows), dim3(a.r.rows <= device_cu_count() ? kMaxThreads : row_vecs(p) <= kShortVecs ? kShortThreads : kRowThreads), 0, q, a);
 }
 
 void launch_grad(const ss_loss_params& p, GradArgs& a, hipStream_t q) {
@@ -1299,7 +1304,7 @@ ss_status specsteer_token_logprobs(const void* logits, const int32_t* tokens, co
     if (off_element(logits, *params)) return SS_ERR_STRIDE;
     const LossScratch w = loss_scratch(*params);
     if (check_workspace(workspace, workspace_bytes, w.bytes) != SS_OK) return SS_ERR_WORKSPACE;
-    const ScoreArgs a{make_rows(logits, nullptr, nullptr, tokens, mask, *params, s), logprobs, stats, nullptr};
+    const ScoreArgs a{make_rows(logits, nullptr, nullptr, tokens, mask, *params, s), logprobs, stats, nullptr, s.rows - (stats ? cached_rows(*params, s.rows, false) : 0)};
     launch_score(*params, a, w, workspace, static_cast<hipStream_t>(stream));
     return launched();
 }
@@ -1389,7 +1394,7 @@ ss_status specsteer_preference_loss(const void* logits, const int32_t* tokens, c
     float* const stats = reinterpret_cast<float*>(base + w.stats);
     double *const weight = reinterpret_cast<double*>(base + w.seq), *const loss64 = weight + pairs;
     const Rows r = make_rows(logits, nullptr, grad_logits, tokens, mask, *params, s);
-    const ScoreArgs sa{r, logprobs, stats, lp64};
+    const ScoreArgs sa{r, logprobs, stats, lp64, s.rows - (grad_logits ? cached_rows(*params, s.rows, mask != nullptr) : 0)};
     Slices c{nullptr, nullptr, 1, 0};
     const bool one = pairs_in_one(pairs, params->length), join = one && s.rows > 0 && s.rows <= kJoinRows && score_slices(s.rows, row_vecs(*params)) > 1;
     if (join) launch_slices<Sum>(*params, r, w, workspace, score_slices(s.rows, row_vecs(*params)), c, q);

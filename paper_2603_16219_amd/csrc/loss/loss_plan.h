@@ -93,6 +93,17 @@ inline bool pairs_in_one(int pairs, int length) { return pairs <= 16 && length <
 constexpr long kJoinRows = 64;
 inline int row_vecs(const ss_loss_params& p) { return p.vocab / (p.dtype == SS_BF16 ? 8 : 4); }
 
+// How many of a call's last rows are read through the caches for a gradient behind it.  All where 256 MiB of last-level cache may hold them (2048
+// rows of V = 50257 bf16 scored and their gradient 108 us past the caches, 101 through them).  In larger calls the gradient, which begins
+// at the end, finds little, and reading past the caches is faster (4096 rows of V = 128256 515 us a preference loss, 531 with 300 MB through them) -- but
+// for a preference loss with a mask: of 600 MB of rows those that count are about what the caches hold (16 x 1024 tokens of V = 32000 with half of
+// them masked 389 and 372 us, 8 x 512 of V = 128256 405 and 385).
+inline long cached_rows(const ss_loss_params& p, long rows, bool masked) {
+    const double row = (double)p.vocab * (p.dtype == SS_BF16 ? 2 : 4), most = rows * row <= 268435456.0 ? rows * row : masked ? 600e6 : 0.0;
+    const long n = (long)(most / row);
+    return n < rows ? n : rows;
+}
+
 inline LossScratch loss_scratch(const ss_loss_params& p) {
     const auto up = [](size_t n) { return (n + 255) / 256 * 256; };
     const size_t rows = (size_t)p.batch * (size_t)p.length;
