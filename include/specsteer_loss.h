@@ -104,6 +104,7 @@ typedef struct {
  * averaged over the tokens that count (see the flags).  KL is
  *     exp(d) - d - 1, d = ref_logprobs - lp               if ref_logprobs is given (an estimate from the token drawn),
  *     sum_v P(v) (log P(v) - log Q(v)), Q = Softmax(ref_logits / tau)     if ref_logits is.
+ * With kl_coef 0 the KL is written to kl only.
  *   ref_logits    device, [B, T, V] with the logits' type and strides, or NULL
  *   old_logprobs  device, [B, T] fp32, of the policy that drew the tokens
  *   ref_logprobs  device, [B, T] fp32, or NULL; not both references

@@ -12,7 +12,7 @@
 // share counts: c goes into the sums' exponents in two parts, rounded to one it left 6e-8 a token, 1e-5 of a margin over 16 pairs of 1024.
 //
 // Rows whose largest |h c| is beyond 2^20, rows of the type's lowest value among them, take a sweep of their own that subtracts
-// the maximum first (far_row).
+// the maximum first (far_sum).
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -440,7 +440,7 @@ __device__ __forceinline__ RowGrad row_grad(const Rows& a, bool far, float E, do
     double f = a.inv_tau / s;
     if (PARTS == 2 && !far) f *= (double)exp2_hw(E * (float)a.rest);
     r.E = E;
-    r.scale = (float)((REF ? -g - k * (diff + kl) : -g) * f);
+    r.scale = (float)((REF && k != 0.0 ? -g - k * (diff + kl) : -g) * f);
     r.cross = REF ? (float)(k * (far ? 1.0 : a.inv_tau) * f) : 0.f;
     r.at_token = (float)(g * a.inv_tau);
     return r;
@@ -448,7 +448,8 @@ __device__ __forceinline__ RowGrad row_grad(const Rows& a, bool far, float E, do
 
 template <bool REF>
 __device__ __forceinline__ float grad_of_term(const RowGrad& r, float e, float h, float z) {
-    if constexpr (REF) return e * fmaf(r.cross, logit_diff(h, z), r.scale);
+    // bounded above as well: without a weight of the KL a token that the reference alone masks takes nothing from it
+    if constexpr (REF) return e * fmaf(r.cross, __builtin_amdgcn_fmed3f(h - z, -3e38f, 3e38f), r.scale);
     return e * r.scale;
 }
 template <int DT, bool REF>
@@ -462,7 +463,7 @@ __device__ __forceinline__ void far_grad(const void* h, const void* z, void* g, 
     for (int i = threadIdx.x; i < V; i += threads) {
         const float hv = ld_elem<DT>(h, i), zv = REF ? ld_elem<DT>(z, i) : 0.f, e = exp2_hw((hv - r.E) * c.whole);
         // a token that the policy masks counts nothing, whatever the reference says of it
-        const float by = REF && e > 0.f ? fmaf(r.cross, (hv - zv) * c.inv_tau, r.scale) : r.scale;
+        const float by = REF && e > 0.f && r.cross != 0.f ? fmaf(r.cross, (hv - zv) * c.inv_tau, r.scale) : r.scale;
         st_elem<DT>(g, i, e * by + (i == token ? r.at_token : 0.f));
     }
 }
@@ -1083,16 +1084,21 @@ __global__ __launch_bounds__(kSliceThreads) void policy_slices_kernel(const Poli
 
 constexpr int kOneThreads = 1024;
 
-// What a token of each sequence counts for the mean over tokens or over sequences: one workgroup, a wave a sequence.
+// What a token of each sequence counts for the mean over tokens or over sequences: one workgroup, a wave a sequence or a lane a short one.
 __global__ __launch_bounds__(kOneThreads) void norm_kernel(const uint8_t* mask, int B, int T, int seq_mean, double* norm) {
     __shared__ double part[kOneThreads / kWave];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const bool short_ones = T <= kWave;
+    const int lane = threadIdx.x & 63, step = short_ones ? kOneThreads : kOneThreads / kWave;
     double all = 0.0;  // tokens, or sequences that have any
-    for (int b = wave; b < B; b += kOneThreads / kWave) {
+    for (int b = short_ones ? threadIdx.x : threadIdx.x >> 6; b < B; b += step) {
+        const uint8_t* const m = mask + (long)b * T;
         int n = 0;
-        for (int t = lane; t < T; t += kWave) n += mask[(long)b * T + t] != 0 ? 1 : 0;
-        n = wave_sum_i32(n);
-        if (lane == 0) {
+        if (short_ones) {
+            for (int t = 0; t < T; ++t) n += m[t] != 0 ? 1 : 0;
+        } else {
+            n = wave_count(m, T);
+        }
+        if (short_ones || lane == 0) {
             norm[b] = (double)n;
             all += seq_mean ? (n > 0 ? 1.0 : 0.0) : (double)n;
         }

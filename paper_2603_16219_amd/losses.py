@@ -259,8 +259,8 @@ def policy_loss(logits: torch.Tensor, tokens: torch.Tensor, old_logprobs: torch.
     has_ref = ref_logits is not None or ref_logprobs is not None
     if kl_coef != 0.0 and not has_ref:
         raise ValueError("a KL term needs ref_logits or ref_logprobs")
-    if ref_logits is not None and (ref_logits.shape != logits.shape or ref_logits.dtype != logits.dtype or
-                                   ref_logits.stride() != logits.stride() or ref_logits.device != logits.device):
+    if ref_logits is not None and (logits.dim() != 3 or ref_logits.shape != logits.shape or ref_logits.dtype != logits.dtype or
+                                   _strides(ref_logits, "ref_logits") != _strides(logits, "logits") or ref_logits.device != logits.device):
         raise ValueError("ref_logits must have the logits' shape, type, strides and device")
     grad_logits = _gradient(logits, want_grad, grad_logits, ref_logits)
     params = _make_params(logits, tokens, temperature, grad_scale, grad_logits)

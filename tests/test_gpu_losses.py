@@ -327,6 +327,37 @@ def test_masked_vocabulary(losses, dtype, low):
             check_policy(losses, {"logits": x, "tokens": y, "ref_logits": z}, g, kl=kl, mask=~whole, tau=tau)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [(2, 5, 1003), (2, 5, 50257), (4, 30, 1003)])
+def test_tokens_that_the_reference_alone_masks(losses, rows, dtype):
+    """Their rows' KL is infinite and so is the loss; without a coefficient the KL is reported and loss and gradient are those without a reference."""
+    inp, g = make(*rows, dtype, ref=True)
+    x, y, z = inp["logits"], inp["tokens"], inp["ref_logits"]
+    z[0, :2, 7] = -math.inf
+    x[0, 1, 7] = x[0, 0].float().amin() - 500  # a token whose term is nothing: no matter what the reference says of it
+    y[0, 1] = 8
+    x[1, 3, 9] = -math.inf
+    y[1, 3] = 8
+    old, adv = torch.zeros(rows[:2], device="cuda") - 8, torch.randn(rows[:2], generator=g, device="cuda")
+    want = losses.policy_loss(x, y, old, adv)
+    got = losses.policy_loss(x, y, old, adv, ref_logits=z)
+    assert torch.equal(got["loss"], want["loss"]) and torch.equal(got["logprobs"], want["logprobs"])
+    half = torch.finfo(x.dtype).eps
+    assert ((got["grad_logits"].float() - want["grad_logits"].float()).abs() <= half * want["grad_logits"].float().abs() + 1e-30).all()
+    assert got["kl"][0, 0] == math.inf and got["kl"].flatten()[1:].isfinite().all()
+    with_kl = losses.policy_loss(x, y, old, adv, ref_logits=z, kl_coef=0.1)
+    assert not with_kl["loss"].isfinite() and not with_kl["grad_logits"][0, 0].isfinite().all()
+    assert with_kl["grad_logits"].flatten(0, 1)[1:].isfinite().all()
+
+
+@pytest.mark.parametrize("B,T", [(20000, 1), (2000, 40), (300, 65)])
+def test_means_over_many_sequences(losses, B, T):
+    inp, g = make(B, T, 37, "f32")
+    mask = torch.rand(B, T, generator=g, device="cuda") < 0.4
+    for reduction in ("token_mean", "seq_mean"):
+        check_policy(losses, inp, g, kl="none", mask=mask, reduction=reduction)
+
+
 @pytest.mark.parametrize("rows", [(3, 4, 2051), (3, 4, 70003), (2, 60, 1999)])  # one workgroup a row, slices, and the same of many rows
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 @pytest.mark.parametrize("shift", [700.0, -7e5, 9e5, 3e7, -1e30])

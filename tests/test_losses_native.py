@@ -90,6 +90,14 @@ def test_what_has_to_be_converted():
     assert losses.token_logprobs(i["x"], y)["logprobs"].isnan().sum() == 1
 
 
+def test_a_reference_whose_strides_differ_where_they_mean_nothing():
+    i = inputs(B=3, T=1, V=515)
+    want = losses.policy_loss(i["x"], i["y"], i["old"], i["adv"], ref_logits=i["z"], kl_coef=0.1)
+    z = torch.as_strided(torch.empty(3 * 515, dtype=i["z"].dtype, device="cuda"), (3, 1, 515), (515, 7777, 1))
+    z.copy_(i["z"])
+    alike(want, losses.policy_loss(i["x"], i["y"], i["old"], i["adv"], ref_logits=z, kl_coef=0.1))
+
+
 @pytest.mark.parametrize("native", [True, False])
 def test_refusals(monkeypatch, native):
     if not native:
