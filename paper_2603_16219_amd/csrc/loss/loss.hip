@@ -64,8 +64,9 @@ __device__ __forceinline__ typename Row<DT>::Raw ld_vec(const void* p, long vec)
     }
 }
 
-// A vector that this launch reads once: past the caches, like the gradient's stores.  Both together are 3 to 8 % of a policy loss (4096 rows of
-// V = 256000 bf16 443 us with loads and stores through the caches, 437 with the stores, 414).
+// A vector that this launch reads once: past the caches, like the gradient's stores.  Both together are 3 to 8 % of a policy loss (2048 rows of
+// V = 256000 bf16 443 us with loads and stores through the caches, 437 with the stores, 414); the zeros of rows that do not count gain most (4
+// pairs of 512 tokens, V = 128256, 391 us, 421 with those through the caches, 450 with all stores).
 template <int DT>
 __device__ __forceinline__ typename Row<DT>::Raw ld_once(const void* p, long vec) { return ld_raw<DT, Row<DT>::kVec>(p, vec); }
 template <int DT>
