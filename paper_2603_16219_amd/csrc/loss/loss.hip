@@ -608,8 +608,8 @@ __device__ __forceinline__ void score_far_row(const ScoreArgs& a, long row, int 
     }
 }
 
-// One workgroup a row, past the caches: 1024 rows of V = 151936 bf16 50 us (6.2 TB/s), 56 through them; fp32 6.6 TB/s.  bf16 rows take half the
-// arithmetic units' time for the exponentials.
+// One workgroup a row, past the caches: 1024 rows of V = 151936 bf16 50 us (6.2 TB/s), 56 through them; fp32 6.6 TB/s.  Bound by the memory:
+// the exponentials of bf16 rows take half the arithmetic units' time.
 template <int DT>
 __global__ __launch_bounds__(kMaxThreads) void score_kernel(const ScoreArgs a) {
     __shared__ Total<Sum> part[kUnitWaves];
@@ -839,7 +839,7 @@ struct RowShared {
 // rows the rest is read again, first in the gradient since it was read last in the sums.  The last wave has no part of the row: it forms what
 // is formed once a row, whose double arithmetic beside the held vectors would not fit the registers.
 // Bound by the memory's bandwidth; what a workgroup stores and what another loads overlap, so that holding as much as a compute unit can is
-// worth more than reading less again.  4096 rows of V = 128256 bf16 402 us a call (5.2 TB/s, a large copy reaches 4.8 to 5.3; swept
+// worth more than reading less again.  4096 rows of V = 128256 bf16 394 us a call (5.3 TB/s, a large copy reaches 4.8 to 5.3; swept
 // twice 498), of V = 32000 95 (147).  8, 12, 16 and 20 vectors a lane were measured: 20 gains 3 % at V = 256000 and loses 4 at 151936.
 template <int DT, bool REF, int NV>
 __global__ __launch_bounds__(kMaxThreads) void policy_kernel(const PolicyArgs a) {

@@ -87,7 +87,7 @@ inline int row_slices(long rows, int vecs) {
     return (int)(n > kMaxRowSlices ? kMaxRowSlices : n < 1 ? 1 : n);
 }
 inline int score_slices(long rows, int vecs) { return vecs > kScoreVecs ? row_slices(rows, vecs) : 1; }
-// Pairs that one workgroup of 16 waves forms with their loss, a wave a pair: 14 rows 3.2 us, a launch of its own for the loss 2 more.
+// Pairs that one workgroup of 16 waves forms with their loss, a wave a pair: 14 rows 4.1 us, a launch of its own for the loss 2 more.
 inline bool pairs_in_one(int pairs, int length) { return pairs <= 16 && length <= 512; }
 // Rows in slices that the same workgroup joins first.
 constexpr long kJoinRows = 64;
@@ -120,7 +120,8 @@ inline LossScratch loss_scratch(const ss_loss_params& p) {
 
 // Waves of a workgroup that holds a row of so many vectors with `held` of them a lane, one wave of it for what is formed once a row.  16
 // waves share a compute unit at the registers that takes (128 a lane): as many as hold the most there, over all workgroups.  A pair of
-// rows of 4000 vectors, 8 a lane, in 9 waves leaves 7 waves' registers unused: 225 us for 4096 of them, 164 in 8.
+// rows of 4000 vectors, 8 a lane, in 9 waves leaves 7 waves' registers unused: 225 us for 4096 of them, 164 in 8, before the arithmetic was
+// cut down to 158.
 constexpr int kUnitWaves = 16;
 constexpr int kHeldVecs = 16, kHeldPairs = 8;  // of a row, and of a row and its reference
 inline int row_waves(int vecs, int held) {

@@ -142,8 +142,8 @@ def _make_params(logits: torch.Tensor, tokens: torch.Tensor, temperature: float,
 def _ready_tokens(tokens: torch.Tensor, device: torch.device) -> torch.Tensor:
     if tokens.dtype is torch.int64:  # an id beyond 32 bits must not come out as another, valid one
         tokens = tokens.clamp(-1, 2**31 - 1)
-    elif tokens.dtype.is_floating_point or tokens.dtype.is_complex or tokens.dtype is torch.bool:
-        raise TypeError(f"tokens must be integers, got {tokens.dtype}")
+    elif tokens.dtype.is_floating_point or tokens.dtype.is_complex or tokens.dtype in (torch.bool, torch.uint64):
+        raise TypeError(f"tokens must be integers that int64 holds, got {tokens.dtype}")
     return _ready(tokens, device, torch.int32)
 
 

@@ -515,6 +515,61 @@ def test_on_another_stream(losses):
     assert all(torch.equal(want[k], got[k]) for k in want)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_more_rows_than_one_dimension_of_a_grid_holds(losses, dtype):
+    B, T, V = 2, 70001, 11
+    inp, g = make(B, T, V, dtype, ref=True)
+    mask = ragged_mask(B, T, g, "lengths")
+    check_score(losses, inp, mask=mask)
+    check_policy(losses, inp, g, kl="none", mask=mask)
+    check_policy(losses, inp, g, kl="full", reduction="seq_mean", mask=mask)
+    check_preference(losses, inp, g, mask=mask, beta=0.01)
+
+
+@pytest.mark.parametrize("rows", [1, 101])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_the_largest_vocabulary(losses, dtype, rows):
+    inp, g = make(2 if rows == 1 else 1, rows, 1 << 20, dtype, ref=True)
+    if rows == 1:
+        check_score(losses, inp)
+        check_preference(losses, inp, g)
+    for kl in ("none", "full"):
+        check_policy(losses, inp, g, kl=kl)
+
+
+def test_calls_from_several_threads_and_streams_at_once(losses):
+    """Four threads, each with a stream, inputs and a workspace of its own, and each of the calls over and over: what they give alone."""
+    import threading
+
+    def work(k):
+        inp, g = make(2, 3 + 30 * k, 5003, "bf16", seed=k, ref=True)
+        x, y, z = inp["logits"], inp["tokens"], inp["ref_logits"]
+        old, adv = torch.zeros(y.shape, device="cuda") - 8, torch.randn(y.shape, generator=g, device="cuda")
+        return lambda: [t for o in (losses.policy_loss(x, y, old, adv), losses.policy_loss(x, y, old, adv, ref_logits=z, kl_coef=0.1),
+                                    losses.preference_loss(x, y), losses.token_logprobs(x, y)) for t in o.values() if t is not None]
+
+    calls = [work(k) for k in range(4)]
+    want = [c() for c in calls]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def run(k):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            for _ in range(20):
+                got = calls[k]()
+                stream.synchronize()
+                if not all(torch.equal(a, b) for a, b in zip(want[k], got)):
+                    wrong.append(k)
+
+    threads = [threading.Thread(target=run, args=(k,)) for k in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong
+
+
 def test_offsets_beyond_32_bits(losses):
     """Logits of more than 2^31 elements: rows at the end against the same rows on their own."""
     T, V = 8400, 256000
@@ -531,6 +586,25 @@ def test_offsets_beyond_32_bits(losses):
     got = losses.policy_loss(x, y, old, adv, mask=mask, grad_logits=x)
     assert torch.equal(got["logprobs"][:, -3:], want["logprobs"]) and torch.equal(got["loss"], want["loss"])
     assert torch.equal(x[:, -3:], want["grad_logits"]) and not x[:, 4000:4003].any()
+    x = x.view(2, T // 2, V)
+    x[:, -3:] = tail
+    y, mask, two = y.view(2, T // 2), mask.view(2, T // 2), torch.cat([tail, tail])
+    mask[:, -3:] = True
+    short = y[:, -3:].contiguous()
+    want = losses.preference_loss(two, short)
+    stats = losses.token_logprobs(two, short, want_stats=True)
+    w = torch.randn(2, T // 2, generator=g, device="cuda")
+    want_grad = losses.token_logprobs_grad(two, short, stats["stats"], w[:, -3:].contiguous())
+    got = losses.token_logprobs(x, y, mask=mask, want_stats=True)
+    # few rows are summed by other workgroups than many.  Log-probs of about -13: each result is rounded by 4.8e-7 at most, the sums before
+    # differ by less; gradients: each is rounded to bf16, by 2^-8 at most.
+    assert (got["logprobs"][:, -3:] - stats["logprobs"]).abs().max() <= 2e-6
+    grad = losses.token_logprobs_grad(x, y, got["stats"], w, mask=mask)
+    assert ((grad[:, -3:].float() - want_grad.float()).abs() <= 2.0 ** -7 * want_grad.float().abs() + 1e-30).all() and not grad[1, 2000:2003].any()
+    del grad
+    got = losses.preference_loss(x, y, mask=mask, grad_logits=x)
+    assert (got["margin"] - want["margin"]).abs().max() <= 2e-6
+    assert ((x[:, -3:].float() - want["grad_logits"].float()).abs() <= 2.0 ** -7 * want["grad_logits"].float().abs() + 1e-30).all()
 
 
 @pytest.mark.parametrize("kl", ["sampled", "full"])

@@ -219,3 +219,12 @@ def test_slices_of_calls_with_few_rows(tmp_path, losses):
             if p.vocab <= 1 << 20:
                 assert losses.workspace_bytes(p) >= rows * (n * 32 + 4 + 16)
     assert {1, 2, 64} <= seen
+
+
+def test_token_ids_beyond_32_bits_do_not_become_others(losses):
+    cpu = torch.device("cpu")
+    big = torch.tensor([[7, 2**32 + 7, -1, -2**33]])
+    assert losses._ready_tokens(big, cpu).tolist() == [[7, 2**31 - 1, -1, -1]]
+    assert losses._ready_tokens(torch.tensor([[2**32 - 1, 7]]).to(torch.uint32), cpu).tolist() == [[-1, 7]]
+    with pytest.raises(TypeError):
+        losses._ready_tokens(big.abs().to(torch.uint64), cpu)
