@@ -427,9 +427,10 @@ __device__ __forceinline__ Total<S> far_sum(const void* h, const void* z, int V,
 }
 
 // What the gradient of a row needs: dL/dh_v = e (scale + cross (h_v - z_v)) + at_token 1[v = y], e = 2^(h_v c - E).  For a row far from zero
-// e = 2^((h_v - m) c) with the maximum m in E, and cross is to be divided by tau still.
+// e = 2^((h_v - m) c) with the maximum m in E, and cross is to be divided by tau still.  Differences count up to +-limit, which times
+// cross is a number: that of a token which either side masks is infinite or the type's largest, and its e = 0 has to come out as 0.
 struct RowGrad {
-    float E, scale, cross, at_token;
+    float E, scale, cross, at_token, limit;
 };
 
 // g = weight of the row's log-prob, k that of its KL, both with the call's factor; diff = D, the difference of the log-sum-exps.
@@ -443,6 +444,7 @@ __device__ __forceinline__ RowGrad row_grad(const Rows& a, bool far, float E, do
     r.E = E;
     r.scale = (float)((REF && k != 0.0 ? -g - k * (diff + kl) : -g) * f);
     r.cross = REF ? (float)(k * (far ? 1.0 : a.inv_tau) * f) : 0.f;
+    r.limit = 1e38f / fmaxf(1.f, fabsf(r.cross));
     r.at_token = (float)(g * a.inv_tau);
     return r;
 }
@@ -450,7 +452,7 @@ __device__ __forceinline__ RowGrad row_grad(const Rows& a, bool far, float E, do
 template <bool REF>
 __device__ __forceinline__ float grad_of_term(const RowGrad& r, float e, float h, float z) {
     // bounded above as well: without a weight of the KL a token that the reference alone masks takes nothing from it
-    if constexpr (REF) return e * fmaf(r.cross, __builtin_amdgcn_fmed3f(h - z, -3e38f, 3e38f), r.scale);
+    if constexpr (REF) return e * fmaf(r.cross, __builtin_amdgcn_fmed3f(h - z, -r.limit, r.limit), r.scale);
     return e * r.scale;
 }
 template <int DT, bool REF>
