@@ -1152,7 +1152,7 @@ __device__ __forceinline__ double pair_side(const PairArgs& a, long p, int side,
 // A pair's loss from the difference of its sequences' log ratios.
 __device__ __forceinline__ double finish_pair(const PairArgs& a, long p, double x, bool write) {
     const double h = a.beta * x, e = a.smoothing;
-    const double loss = (1.0 - e) * softplus(-h) + e * softplus(h);
+    const double loss = (1.0 - e) * softplus(-h) + (e > 0.0 ? e * softplus(h) : 0.0);  // a margin of +inf costs nothing without smoothing
     const double dh = (e - 1.0) / (1.0 + exp(h)) + e / (1.0 + exp(-h));
     if (write) {
         a.weight[p] = a.beta * a.factor * dh;

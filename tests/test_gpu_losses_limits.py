@@ -4,6 +4,7 @@ import math
 import pytest
 import torch
 
+import loss_reference as R
 from test_gpu_losses import check_policy, losses, make  # noqa: F401
 
 pytestmark = pytest.mark.gpu
@@ -28,3 +29,31 @@ def test_masked_tokens_under_a_large_weight_of_the_kl(losses, rows, low, dtype, 
     x[0, 1, 150] = x[0, 1, 200:].float().amin() - 500  # nothing of it is left in the policy, and the reference masks it
     z[0, 1, 150] = torch.finfo(x.dtype).min
     check_policy(losses, inp, g, kl="full", tau=tau, reduction="sum", kl_coef=coef, scale=scale)
+
+
+@pytest.mark.parametrize("rows", [(4, 3), (4, 513), (34, 2)])  # one workgroup for all pairs, and one each
+@pytest.mark.parametrize("beta", [0.25, -0.25])
+def test_pairs_with_a_token_of_probability_zero(losses, rows, beta):
+    """Pair 0 rejects such a sequence, pair 1 prefers one: margins of +-inf, whose losses are 0 and inf, and finite gradients."""
+    B, T = rows
+    P, V = B // 2, 50
+    inp, _ = make(B, T, V, "f32")
+    x, y = inp["logits"], inp["tokens"]
+    good, bad = (0, 1) if beta > 0 else (1, 0)
+    for row, t in ((P, 0), (1, T - 1)):
+        y[row, t] = 7
+        x[row, t, 7] = -math.inf
+    out = losses.preference_loss(x, y, beta=beta)
+    assert out["margin"][good] == math.inf and out["pair_loss"][good] == 0.0
+    assert out["margin"][bad] == -math.inf and out["pair_loss"][bad] == math.inf
+    assert out["loss"] == math.inf and out["pair_loss"][2:].isfinite().all()
+    grad = out["grad_logits"]
+    assert grad.isfinite().all() and not grad[[good, P + good]].any()
+    assert grad[1, T - 1, 7] == (-beta / P if bad == 1 else 0.0)  # the whole weight, at a token without probability
+    smooth = losses.preference_loss(x, y, beta=beta, label_smoothing=0.25)
+    assert (smooth["pair_loss"][:2] == math.inf).all() and smooth["grad_logits"].isfinite().all()
+    fine = torch.arange(B, device="cuda") % P != bad  # without the pair whose loss is infinite
+    pairs = fine[:P]
+    out = losses.preference_loss(x[fine].contiguous(), y[fine].contiguous(), beta=beta)
+    want = losses.preference_loss(x, y, beta=beta)["pair_loss"][pairs].double().mean()
+    assert abs(out["loss"].item() - want.item()) <= 2 * R.U * (want.item() + 1)  # each is rounded to fp32 once
