@@ -801,7 +801,7 @@ __device__ __forceinline__ RowLoss row_loss(const PolicyArgs& a, bool far, long 
         o.k = a.kl_coef;
     } else if (a.ref_logprobs) {
         const double d = (double)a.ref_logprobs[row] - o.lp, e = expm1(d);
-        o.kl = e - d;
+        o.kl = d == __builtin_huge_val() ? d : e - d;  // a token of probability zero: e^d outgrows d
         if (a.kl_coef != 0.0) o.g -= a.kl_coef * e;
     }
     if (a.kl_coef != 0.0) o.term += a.kl_coef * o.kl;

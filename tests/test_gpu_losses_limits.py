@@ -57,3 +57,22 @@ def test_pairs_with_a_token_of_probability_zero(losses, rows, beta):
     out = losses.preference_loss(x[fine].contiguous(), y[fine].contiguous(), beta=beta)
     want = losses.preference_loss(x, y, beta=beta)["pair_loss"][pairs].double().mean()
     assert abs(out["loss"].item() - want.item()) <= 2 * R.U * (want.item() + 1)  # each is rounded to fp32 once
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", ROWS)
+def test_the_sampled_kl_of_a_token_of_probability_zero(losses, rows, dtype):
+    """e^d - d - 1 grows with d without bound: +inf, and so is a loss with that term."""
+    inp, g = make(*rows, dtype)
+    x, y = inp["logits"], inp["tokens"]
+    zero = torch.zeros(y.shape, dtype=torch.bool, device="cuda")
+    zero[0, 1] = zero[1, 4] = True
+    y[zero] = 7
+    x[0, 1, 7] = x[1, 4, 7] = -math.inf
+    old, ref = torch.full(y.shape, -8.0, device="cuda"), torch.full(y.shape, -9.0, device="cuda")
+    adv = torch.randn(y.shape, generator=g, device="cuda")
+    want = losses.policy_loss(x, y, old, adv)
+    got = losses.policy_loss(x, y, old, adv, ref_logprobs=ref)
+    assert (got["kl"][zero] == math.inf).all() and got["kl"][~zero].isfinite().all()
+    assert torch.equal(got["loss"], want["loss"]) and torch.equal(got["grad_logits"], want["grad_logits"])
+    assert losses.policy_loss(x, y, old, adv, ref_logprobs=ref, kl_coef=0.1)["loss"] == math.inf
