@@ -82,6 +82,11 @@ bool gradient_of(PyObject* o, bool want, const at::Tensor& logits, const at::Ten
     return true;
 }
 
+// Autograd learns that a tensor of the caller's was written, which may be one that a backward pass has saved.
+void written(PyObject* given, const at::Tensor& t) {
+    if (given != Py_None && !t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 bool workspace_of(PyObject* o, const at::Tensor& logits, const ss_loss_params& p, at::Tensor& out) {
     if (o == Py_None) {
         const size_t need = lib.workspace_bytes(&p);
@@ -147,6 +152,7 @@ PyObject* token_logprobs_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
         return lib.token_logprobs_grad(data(x), data_as<int32_t>(y), data_as<uint8_t>(mask), data_as<float>(stats), data_as<float>(w), &p, grad.data_ptr(), stream);
     });
     if (rc != SS_OK) return PyLong_FromLong(rc);
+    written(a[7], grad);
     if (a[7] != Py_None) return Py_NewRef(a[7]);
     return THPVariable_Wrap(grad);
     END_HANDLE_TH_ERRORS
@@ -183,6 +189,7 @@ PyObject* policy_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
                                ptr<float>(loss), ptr<float>(lp), ptr<float>(kl), ptr<void>(grad), ws.data_ptr(), ws.nbytes(), stream);
     });
     if (rc != SS_OK) return PyLong_FromLong(rc);
+    written(a[14], grad);
     PyObject* out = result({{"loss", &loss}, {"logprobs", &lp}, {"kl", &kl}, {"grad_logits", &grad}});
     if (out && a[14] != Py_None && PyDict_SetItemString(out, "grad_logits", a[14]) != 0) Py_CLEAR(out);
     return out;
@@ -214,6 +221,7 @@ PyObject* preference_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
                                    ptr<float>(margin), ptr<float>(lp), ptr<void>(grad), ws.data_ptr(), ws.nbytes(), stream);
     });
     if (rc != SS_OK) return PyLong_FromLong(rc);
+    written(a[10], grad);
     PyObject* out = result({{"loss", &loss}, {"pair_loss", &pair}, {"margin", &margin}, {"logprobs", &lp}, {"grad_logits", &grad}});
     if (out && a[10] != Py_None && PyDict_SetItemString(out, "grad_logits", a[10]) != 0) Py_CLEAR(out);
     return out;

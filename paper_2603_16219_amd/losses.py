@@ -9,6 +9,9 @@ A loss comes with the gradient of the logits it was given, which the model's own
 
     out = losses.policy_loss(logits, tokens, old_logprobs, advantages, mask=mask, ref_logprobs=ref, kl_coef=0.05)
     logits.backward(out["grad_logits"])
+
+The gradient may go to a tensor of the caller's, `grad_logits=`, which may be the logits themselves.  Autograd takes that for an operation in place:
+the backward pass of a model whose last operation keeps its output (a tanh, say) refuses logits that were replaced.
 """
 from __future__ import annotations
 
@@ -184,6 +187,12 @@ def _gradient(logits: torch.Tensor, want: bool, out: Optional[torch.Tensor], ref
     return out
 
 
+def _written(grad_logits: Optional[torch.Tensor]) -> None:
+    """Autograd learns that the gradient was written to a tensor, which may be one that a backward pass has saved."""
+    if grad_logits is not None:
+        torch.autograd.graph.increment_version(grad_logits)
+
+
 def _scratch(workspace: Optional[torch.Tensor], params: SSLossParams, device: torch.device) -> torch.Tensor:
     if workspace is None:
         return torch.empty(max(workspace_bytes(params), 256), dtype=torch.uint8, device=device)
@@ -233,6 +242,7 @@ def token_logprobs_grad(logits: torch.Tensor, tokens: torch.Tensor, stats: torch
     tokens, stats = _ready_tokens(tokens, dev), stats.contiguous()
     _call(library().specsteer_token_logprobs_grad, dev, _ptr(logits), _ptr(tokens), _ptr(mask), _ptr(stats), _ptr(grad_logprobs),
           ctypes.byref(params), _ptr(grad_logits))
+    _written(grad_logits)
     return grad_logits
 
 
@@ -284,6 +294,7 @@ def policy_loss(logits: torch.Tensor, tokens: torch.Tensor, old_logprobs: torch.
           _ptr(ref_logprobs), _ptr(advantages), ctypes.byref(params),
           ctypes.byref(SSPolicyParams(clip_low, clip_high, kl_coef, flags)), _ptr(loss), _ptr(logprobs), _ptr(kl), _ptr(grad_logits),
           _ptr(workspace), _bytes(workspace))
+    _written(grad_logits)
     return {"loss": loss, "logprobs": logprobs, "kl": kl, "grad_logits": grad_logits}
 
 
@@ -317,4 +328,5 @@ def preference_loss(logits: torch.Tensor, tokens: torch.Tensor, *, mask: Optiona
     _call(library().specsteer_preference_loss, dev, _ptr(logits), _ptr(tokens), _ptr(mask), _ptr(ref_logprobs), ctypes.byref(params),
           ctypes.byref(SSPreferenceParams(beta, label_smoothing, flags)), _ptr(loss), _ptr(pair_loss),
           _ptr(margin), _ptr(logprobs), _ptr(grad_logits), _ptr(workspace), _bytes(workspace))
+    _written(grad_logits)
     return {"loss": loss, "pair_loss": pair_loss, "margin": margin, "logprobs": logprobs, "grad_logits": grad_logits}

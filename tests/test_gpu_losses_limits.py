@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import loss_reference as R
-from test_gpu_losses import check_policy, losses, make  # noqa: F401
+from test_gpu_losses import check_policy, gen, losses, make  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -76,3 +76,43 @@ def test_the_sampled_kl_of_a_token_of_probability_zero(losses, rows, dtype):
     assert (got["kl"][zero] == math.inf).all() and got["kl"][~zero].isfinite().all()
     assert torch.equal(got["loss"], want["loss"]) and torch.equal(got["grad_logits"], want["grad_logits"])
     assert losses.policy_loss(x, y, old, adv, ref_logprobs=ref, kl_coef=0.1)["loss"] == math.inf
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_autograd_learns_of_a_gradient_in_place_of_the_logits(losses, monkeypatch, native):
+    """The backward pass of a model that saved its output refuses an output that was replaced; one that did not goes on."""
+    if not native:
+        monkeypatch.setattr(losses, "_calls", None)
+    g = gen(3)
+    hidden = torch.randn(4, 6, 32, generator=g, device="cuda")
+    head = torch.randn(515, 32, generator=g, device="cuda").requires_grad_()
+    y = torch.randint(0, 515, (4, 6), generator=g, device="cuda", dtype=torch.int32)
+    old, adv = torch.zeros(4, 6, device="cuda") - 8, torch.randn(4, 6, generator=g, device="cuda")
+    stats = losses.token_logprobs((hidden @ head.T).detach(), y, want_stats=True)["stats"]
+    calls = [lambda x, to: losses.policy_loss(x, y, old, adv, grad_logits=to)["grad_logits"],
+             lambda x, to: losses.preference_loss(x, y, grad_logits=to)["grad_logits"],
+             lambda x, to: losses.token_logprobs_grad(x, y, stats, adv, grad_logits=to)]
+    for call in calls:
+        grads = []
+        for place in (False, True):
+            head.grad = None
+            logits = hidden @ head.T
+            before = logits._version
+            logits.backward(call(logits, logits if place else None))
+            assert logits._version == before + place
+            grads.append(head.grad)
+        assert torch.equal(*grads)
+        saved = torch.tanh(hidden @ head.T)
+        with pytest.raises(RuntimeError, match="inplace operation"):
+            saved.backward(call(saved, saved))
+        other = torch.tanh(hidden @ head.T)  # saved, and given for the gradient of something else
+        call(logits.detach(), other.detach())
+        with pytest.raises(RuntimeError, match="inplace operation"):
+            other.sum().backward()
+        with torch.inference_mode():  # tensors without a version
+            x = logits.detach().clone()
+            assert call(x, x) is x
+        before = logits._version
+        with pytest.raises(losses.SpecSteerError):  # refused, and nothing written
+            losses.policy_loss(logits, y, old, adv, clip_low=2.0, grad_logits=logits)
+        assert logits._version == before
