@@ -28,9 +28,8 @@ inline bool loss_strides(int64_t sb, int64_t st, const ss_loss_params& p, long& 
     if (!sb && __builtin_mul_overflow((long)p.length, out_st, &out_sb)) return false;
     // the last element's offset in bytes has to be a number too
     long end = 0;
-    if (p.batch > 1 && (__builtin_mul_overflow((long)(p.batch - 1), out_sb, &end) || __builtin_add_overflow(end, span, &end) ||
-                        __builtin_mul_overflow(end, 4L, &end)))
-        return false;
+    if (p.batch > 1 && __builtin_mul_overflow((long)(p.batch - 1), out_sb, &end)) return false;
+    if (__builtin_add_overflow(end, span, &end) || __builtin_mul_overflow(end, 4L, &end)) return false;
     return p.batch <= 1 || p.length == 0 || out_sb >= span;
 }
 

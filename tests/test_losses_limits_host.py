@@ -1,0 +1,27 @@
+"""CPU checks of what the losses' calls accept, at the limits of strides."""
+import pytest
+
+from test_losses_host import CALLS, STRIDE, Call, losses  # noqa: F401
+
+
+@pytest.mark.parametrize("name", CALLS)
+@pytest.mark.parametrize("spoiled", [
+    # the last element's offset in bytes is 2^63 or more: of a row far out, of a sequence far out, of both together
+    dict(batch=2, length=1, stride_b=1 << 61), dict(batch=2, length=2, stride_t=1 << 60, stride_b=(1 << 60) + 100),
+    dict(batch=2, length=2, grad_stride_t=1 << 61), dict(batch=2, length=1, grad_stride_b=(1 << 61) - 99)])
+def test_offsets_that_no_64_bits_hold(losses, name, spoiled):
+    assert Call(losses, name)(**spoiled) == STRIDE
+
+
+@pytest.mark.parametrize("name", [n for n in CALLS if n != "preference_loss"])
+@pytest.mark.parametrize("spoiled", [dict(stride_t=1 << 61), dict(stride_t=(1 << 61) - 99), dict(grad_stride_t=1 << 61)])
+def test_offsets_of_a_single_sequence_that_no_64_bits_hold(losses, name, spoiled):
+    assert Call(losses, name)(batch=1, length=2, **spoiled) == STRIDE
+
+
+@pytest.mark.parametrize("field", ["stride_t", "grad_stride_t", "stride_b", "grad_stride_b"])
+def test_the_largest_offsets_are_accepted(losses, field):
+    # the last byte behind the last element at 2^63 - 4: refused for its workspace only, which is looked at after the strides
+    shape = dict(batch=1, length=2) if field.endswith("t") else dict(batch=2, length=1)
+    for name in ("token_logprobs", "policy_loss"):
+        assert Call(losses, name)(**shape, **{field: (1 << 61) - 101}, workspace=None) == 6
