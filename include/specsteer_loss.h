@@ -66,8 +66,8 @@ size_t specsteer_loss_workspace_bytes(const ss_loss_params *params);
  *   mask      device, [B, T] bytes, 0 for positions that do not count; or NULL: all do
  *   logprobs  device, [B, T] fp32 out: log P(tokens[b][t])
  *   stats     device, [B, T, 2] fp32 out, or NULL: what specsteer_token_logprobs_grad takes, a power of two E and the
- *             row's sum of exponentials over 2^E (for logits beyond 2^20 their maximum m and minus the sum over exp(m / tau));
- *             0 and 1 at positions that do not count
+ *             row's sum of exponentials over 2^E (for logits beyond 2^20, and temperatures beyond 10^+-12, their maximum m and
+ *             minus the sum over exp(m / tau)); 0 and 1 at positions that do not count
  *   workspace, workspace_bytes, stream  as in specsteer.h
  */
 ss_status specsteer_token_logprobs(const void *logits, const int32_t *tokens, const uint8_t *mask,

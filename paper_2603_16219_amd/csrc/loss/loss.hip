@@ -11,8 +11,8 @@
 // weights, losses) is double.  Sums of hundreds of log-probs with either sign are small beside their terms, so an error that all rows
 // share counts: c goes into the sums' exponents in two parts, rounded to one it left 6e-8 a token, 1e-5 of a margin over 16 pairs of 1024.
 //
-// Rows whose largest |h c| is beyond 2^20, rows of the type's lowest value among them, take a sweep of their own that subtracts
-// the maximum first (far_sum).
+// Rows whose largest |h c| is beyond 2^20, rows of the type's lowest value among them, and all rows at temperatures beyond 10^+-12 take a
+// sweep of their own that subtracts the maximum first (far_sum).
 #include <hip/hip_runtime.h>
 
 #include <cmath>
@@ -98,9 +98,9 @@ __device__ __forceinline__ void st_vec(void* p, long vec, const float (&h)[Row<D
 
 // ------------------------------------------------------------------ statistics of a row
 
-// c = log2(e) / tau in two fp32 parts, the first of 16 bits, so that a bf16 logit's product with it is exact; as one fp32 number; and 1 / tau.
+// c = log2(e) / tau in two fp32 parts, the first of 16 bits, so that a bf16 logit's product with it is exact; and as one fp32 number.
 struct Factor {
-    float hi, lo, whole, inv_tau;
+    float hi, lo, whole;
 };
 // 2^(h c - E), c in two parts or as one number
 template <int PARTS>
@@ -377,10 +377,14 @@ __device__ __forceinline__ S lane_sum(const void* h, const void* z, const Layout
 
 // ------------------------------------------------------------------ rows far from zero
 
+// 2^((h - m) c), in double but for the exponential: at temperatures near the type's largest value the difference may not be a number in fp32,
+// and c have few bits.
+__device__ __forceinline__ float far_term(float h, double m, double c) { return exp2_hw((float)(((double)h - m) * c)); }
+
 // The sums of a row with its largest logit m for a reference: E = m and s = sum 2^((h - m) c), element by element over a workgroup.
 // Differences are exact where they matter, so that this holds for any finite row (of lowest values only: a uniform one).
 template <int DT, typename S>
-__device__ __forceinline__ Total<S> far_sum(const void* h, const void* z, int V, Factor c, int threads, Total<S>* part) {
+__device__ __forceinline__ Total<S> far_sum(const void* h, const void* z, int V, double c, int threads, Total<S>* part) {
     constexpr bool kRef = std::is_same<S, SumRef>::value;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = threads / kWave;
     float m = -__builtin_huge_valf(), mz = m;
@@ -402,12 +406,12 @@ __device__ __forceinline__ Total<S> far_sum(const void* h, const void* z, int V,
     if constexpr (kRef) a.Ez = mz = all_max(mz);
     double s = 0.0, x = 0.0, sz = 0.0;
     for (int i = threadIdx.x; i < V; i += threads) {
-        const float hv = ld_elem<DT>(h, i), e = exp2_hw((hv - m) * c.whole);
+        const float hv = ld_elem<DT>(h, i), e = far_term(hv, m, c);
         s += (double)e;
         if constexpr (kRef) {
             const float zv = ld_elem<DT>(z, i);
             x += e > 0.f ? (double)e * ((double)hv - (double)zv) : 0.0;
-            sz += (double)exp2_hw((zv - mz) * c.whole);
+            sz += (double)far_term(zv, mz, c);
         }
     }
     const auto all_sum = [&](double v) {
@@ -462,11 +466,11 @@ __device__ __forceinline__ float grad_of(const RowGrad& r, float h, float z, Fac
 
 // The gradient of a row far from zero, element by element over a workgroup.
 template <int DT, bool REF>
-__device__ __forceinline__ void far_grad(const void* h, const void* z, void* g, int V, const RowGrad& r, int token, Factor c, int threads) {
-    for (int i = threadIdx.x; i < V; i += threads) {
-        const float hv = ld_elem<DT>(h, i), zv = REF ? ld_elem<DT>(z, i) : 0.f, e = exp2_hw((hv - r.E) * c.whole);
+__device__ __forceinline__ void far_grad(const void* h, const void* z, void* g, const Rows& a, const RowGrad& r, int token, int threads) {
+    for (int i = threadIdx.x; i < a.V; i += threads) {
+        const float hv = ld_elem<DT>(h, i), zv = REF ? ld_elem<DT>(z, i) : 0.f, e = far_term(hv, r.E, a.c64);
         // a token that the policy masks counts nothing, whatever the reference says of it
-        const float by = REF && e > 0.f && r.cross != 0.f ? fmaf(r.cross, (hv - zv) * c.inv_tau, r.scale) : r.scale;
+        const float by = REF && e > 0.f && r.cross != 0.f ? fmaf(r.cross, (float)(((double)hv - (double)zv) * a.inv_tau), r.scale) : r.scale;
         st_elem<DT>(g, i, e * by + (i == token ? r.at_token : 0.f));
     }
 }
@@ -603,7 +607,7 @@ __device__ __forceinline__ void score_far_row(const ScoreArgs& a, long row, int 
     long at, grad_at;
     place(a.r, row, at, grad_at);
     const void* const h = row_ptr<DT>(a.r.logits, at);
-    const Total<Sum> s = far_sum<DT, Sum>(h, nullptr, a.r.V, a.r.c, threads, part);
+    const Total<Sum> s = far_sum<DT, Sum>(h, nullptr, a.r.V, a.r.c64, threads, part);
     if (threadIdx.x == 0) {
         const int y = a.r.tokens[row];
         write_score(a, row, token_logprob<2>(a.r, true, y, y >= 0 && y < a.r.V ? ld_elem<DT>(h, y) : 0.f, s.E, s.s), s.E, -s.s);
@@ -629,7 +633,7 @@ __global__ __launch_bounds__(kMaxThreads) void score_kernel(const ScoreArgs a) {
     const Sum mine = row >= a.keep_from ? lane_sum<DT, Sum, 2, false>(h, nullptr, lay, threadIdx.x, lay.vecs, threads, true, a.r.c)
                                         : lane_sum<DT, Sum, 2, true>(h, nullptr, lay, threadIdx.x, lay.vecs, threads, true, a.r.c);
     const Total<Sum> s = block_total(mine, threads, part);
-    if (is_far(s)) {
+    if (a.r.far || is_far(s)) {
         score_far_row<DT>(a, row, threads, part);
     } else if (threadIdx.x == 0) {
         const int y = a.r.tokens[row];
@@ -688,7 +692,7 @@ __device__ __forceinline__ bool score_joined(const ScoreArgs& a, const Slices& p
         return false;
     }
     const Total<Sum> s = join_slices<Sum>(p, row);
-    if (is_far(s)) return true;
+    if (a.r.far || is_far(s)) return true;
     if (first) write_score(a, row, token_logprob<2>(a.r, false, a.r.tokens[row], p.token_logits[row], s.E, s.s), s.E, s.s);
     return false;
 }
@@ -747,7 +751,7 @@ __global__ __launch_bounds__(kGradThreads) void grad_kernel(const GradArgs a) {
     const bool far = s < 0.f;
     const RowGrad rg = row_grad<DT, false, 2>(a.r, far, a.stats[2 * row], fabsf(s), w, 0.0, 0.0, 0.0);
     if (far) {
-        if (slice == 0) far_grad<DT, false>(h, nullptr, g, a.r.V, rg, y, a.r.c, kGradThreads);
+        if (slice == 0) far_grad<DT, false>(h, nullptr, g, a.r, rg, y, kGradThreads);
         return;
     }
     write_grad<DT, false, true>(h, nullptr, g, lay, rg, y, first, end, kGradThreads, slice == 0, a.r.c);
@@ -965,14 +969,14 @@ __global__ __launch_bounds__(kMaxThreads) void policy_kernel(const PolicyArgs a)
         }
     }
     if (shared.far) {
-        const Total<S> s = far_sum<DT, S>(h, z, a.r.V, a.r.c, blockDim.x, part);
+        const Total<S> s = far_sum<DT, S>(h, z, a.r.V, a.r.c64, blockDim.x, part);
         const double n = token_norm(a, row);
         if (tid == 0)
             shared.grad = finish_row<DT, REF>(a, true, row, y, valid ? ld_elem<DT>(h, y) : 0.f, a.old_logprobs[row],
                                               advantage_of(a, row), n, s);
         __syncthreads();
         const RowGrad rg = shared.grad;
-        if (g) far_grad<DT, REF>(h, z, g, a.r.V, rg, y, a.r.c, blockDim.x);
+        if (g) far_grad<DT, REF>(h, z, g, a.r, rg, y, blockDim.x);
     }
 }
 
@@ -1023,7 +1027,7 @@ __device__ __forceinline__ void policy_slices_loss(const PolicyArgs& a, const Sl
             const void* const h = row_ptr<DT>(a.r.logits, at);
             const void* const z = REF ? row_ptr<DT>(a.r.ref, at) : nullptr;
             const int y = a.r.tokens[row];
-            const Total<S> s = far_sum<DT, S>(h, z, a.r.V, a.r.c, kSliceThreads, part);
+            const Total<S> s = far_sum<DT, S>(h, z, a.r.V, a.r.c64, kSliceThreads, part);
             if (tid == 0) {
                 const RowLoss o = row_loss<REF, 2>(a, true, row, y, p.token_logits[row], a.old_logprobs[row], advantage_of(a, row),
                                                 a.count ? counted : row_norm(a, row), s);
@@ -1033,7 +1037,7 @@ __device__ __forceinline__ void policy_slices_loss(const PolicyArgs& a, const Sl
             }
             __syncthreads();
             const RowGrad rg = shared_grad;
-            if (a.r.grad) far_grad<DT, REF>(h, z, const_cast<void*>(row_ptr<DT>(a.r.grad, grad_at)), a.r.V, rg, y, a.r.c, kSliceThreads);
+            if (a.r.grad) far_grad<DT, REF>(h, z, const_cast<void*>(row_ptr<DT>(a.r.grad, grad_at)), a.r, rg, y, kSliceThreads);
             __syncthreads();
         }
     }
@@ -1232,8 +1236,8 @@ Rows make_rows(const void* logits, const void* ref, void* grad, const int32_t* t
     r.c.hi = (float)std::ldexp(std::floor(std::ldexp(frac, 16)), e - 16);
     r.c.lo = std::fmax((float)(r.c64 - (double)r.c.hi), 1.1754944e-38f);
     r.c.whole = (float)r.c64;
-    r.c.inv_tau = (float)(1.0 / (double)p.temperature);
-    r.far = !(p.temperature > 1e-12f && p.temperature < 1e12f);  // 1 / tau^2 is a factor otherwise, which fp32 may not hold
+    // 1 / tau^2 is a factor otherwise, which fp32 may not hold, nor c's lower part
+    r.far = !(p.temperature > 1e-12f && p.temperature < 1e12f);
     r.inv_tau = 1.0 / (double)p.temperature;
     r.scale = (double)p.grad_scale;
     r.rest = (r.c64 - (double)r.c.whole) / (double)r.c.whole;

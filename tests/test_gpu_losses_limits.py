@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import loss_reference as R
-from test_gpu_losses import check_policy, gen, losses, make  # noqa: F401
+from test_gpu_losses import check_policy, check_preference, check_score, gen, losses, make  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -116,3 +116,17 @@ def test_autograd_learns_of_a_gradient_in_place_of_the_logits(losses, monkeypatc
         with pytest.raises(losses.SpecSteerError):  # refused, and nothing written
             losses.policy_loss(logits, y, old, adv, clip_low=2.0, grad_logits=logits)
         assert logits._version == before
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("tau", [3e38, 1e35, 1e20, 1e13, 1e-13, 1e-20, 1e-30])
+@pytest.mark.parametrize("rows", [(2, 3, 3001), (2, 3, 70001), (2, 60, 515)])
+def test_temperatures_far_from_1(losses, rows, tau, dtype):
+    """Logits as large or small as the temperature: distributions as any others."""
+    inp, g = make(*rows, dtype, sigma=1.0, ref=True)
+    unit = min(tau, 6e37)  # the largest logits of these, about 5, are numbers of the type still
+    inp["logits"], inp["ref_logits"] = ((inp[k].float() * unit).to(inp[k].dtype) for k in ("logits", "ref_logits"))
+    check_score(losses, inp, tau=tau)
+    check_preference(losses, inp, g, tau=tau)
+    for kl in ("none", "sampled", "full"):
+        check_policy(losses, inp, g, kl=kl, tau=tau)
