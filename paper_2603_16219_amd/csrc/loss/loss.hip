@@ -4,9 +4,11 @@
 //     s = sum_v 2^(h_v c - E),
 // a token's log-prob is (h_y c - E - log2 s) ln 2 and every gradient of a loss of log-probs is, in the row's logits,
 //     dL/dh_v = (g / tau) (1[v = y] - 2^(h_v c - E) / s),    g = dL/dlp.
-// A whole-vocabulary KL to a reference with logits z takes, in the same pass, sum_v 2^(h_v c - E) (h_v - z_v) and the
-// reference's own (E', s'):  KL = E[h - z] / tau - D with D = log-sum-exp(h) - log-sum-exp(z), and adds
-//     (k / tau) P(v) ((h_v - z_v) / tau - D - KL)     to the gradient.
+// A whole-vocabulary KL to a reference with logits z takes, in the same pass, the reference's own (E', s') and
+//     x = sum_v 2^(h_v c - E) ((h_v c - E) - (z_v c - E')):     KL = (x / s - log2 s + log2 s') ln 2,
+// of exponents that are there anyway: what is common to a row's logits, by which policy and reference may differ, is in E and E'.  With the
+// mean M = E[h - z] / tau, from x / s + E - E', it adds
+//     (k / tau) P(v) ((h_v - z_v) / tau - M)     to the gradient.
 // A whole E makes moving a sum to another reference exact.  Terms and a lane's sums are fp32; what is formed once a row (log-probs, KL,
 // weights, losses) is double.  Sums of hundreds of log-probs with either sign are small beside their terms, so an error that all rows
 // share counts: c goes into the sums' exponents in two parts, rounded to one it left 6e-8 a token, 1e-5 of a margin over 16 pairs of 1024.
@@ -102,27 +104,30 @@ __device__ __forceinline__ void st_vec(void* p, long vec, const float (&h)[Row<D
 struct Factor {
     float hi, lo, whole;
 };
-// 2^(h c - E), c in two parts or as one number
+// h c - E, c in two parts or as one number
 template <int PARTS>
-__device__ __forceinline__ float term(float h, float E, Factor c) {
-    return exp2_hw(PARTS == 2 ? fmaf(h, c.lo, fmaf(h, c.hi, -E)) : fmaf(h, c.whole, -E));
-}
+__device__ __forceinline__ float exponent(float h, float E, Factor c) { return PARTS == 2 ? fmaf(h, c.lo, fmaf(h, c.hi, -E)) : fmaf(h, c.whole, -E); }
+template <int PARTS>
+__device__ __forceinline__ float term(float h, float E, Factor c) { return exp2_hw(exponent<PARTS>(h, E, c)); }
 
-// h - z, and a number for a token that the policy masks (-inf - -inf among them), whose term is 0 then.  +inf where the reference alone
-// masks one.
-__device__ __forceinline__ float logit_diff(float h, float z) { return fmaxf(h - z, -3e38f); }
+// The difference of a token's exponents, and a number for one that the policy masks (-inf - -inf among them), whose term is 0 then.  +inf where
+// the reference alone masks one.
+__device__ __forceinline__ float exponent_diff(float t, float tz) { return fmaxf(t - tz, -3e38f); }
 
 // A running sum: the reference E and sum 2^(h c - E).
 struct Sum {
     float E, s;
 };
-// The same with the cross term sum 2^(h c - E) (h - z) and the reference's own sum.
+// The same with the cross term sum 2^(h c - E) ((h c - E) - (z c - Ez)) and the reference's own sum.
 struct SumRef {
     float E, s, x, Ez, sz;
 };
 __device__ __forceinline__ void clear(Sum& a) { a.E = -kFar; a.s = 0.f; }
 __device__ __forceinline__ void clear(SumRef& a) { a.E = a.Ez = -kFar; a.s = a.x = a.sz = 0.f; }
 __device__ __forceinline__ float moved(float s, float from, float to) { return __builtin_ldexpf(s, (int)(from - to)); }
+// A cross term at other references, by and byz higher, from what it is with only its terms moved to them, and their sum.
+__device__ __forceinline__ float crossed(float x, float s, float by, float byz) { return fmaf(s, byz - by, x); }
+__device__ __forceinline__ double crossed(double x, double s, float by, float byz) { return x + s * (double)(byz - by); }
 
 __device__ __forceinline__ void merge(Sum& a, const Sum& b) {
     const float E = fmaxf(a.E, b.E);
@@ -130,9 +135,9 @@ __device__ __forceinline__ void merge(Sum& a, const Sum& b) {
     a.E = E;
 }
 __device__ __forceinline__ void merge(SumRef& a, const SumRef& b) {
-    const float E = fmaxf(a.E, b.E), Ez = fmaxf(a.Ez, b.Ez);
-    a.s = moved(a.s, a.E, E) + moved(b.s, b.E, E);
-    a.x = moved(a.x, a.E, E) + moved(b.x, b.E, E);
+    const float E = fmaxf(a.E, b.E), Ez = fmaxf(a.Ez, b.Ez), sa = moved(a.s, a.E, E), sb = moved(b.s, b.E, E);
+    a.s = sa + sb;
+    a.x = crossed(moved(a.x, a.E, E), sa, E - a.E, Ez - a.Ez) + crossed(moved(b.x, b.E, E), sb, E - b.E, Ez - b.Ez);
     a.sz = moved(a.sz, a.Ez, Ez) + moved(b.sz, b.Ez, Ez);
     a.E = E;
     a.Ez = Ez;
@@ -145,13 +150,29 @@ __device__ __forceinline__ float largest(const float (&h)[N]) {
     for (int i = 1; i < N; ++i) top = fmaxf(top, h[i]);
     return top;
 }
-__device__ __forceinline__ void raise(float& E, float& s, float& x, float top, Factor c) {
+// The references as high as logits up to `top` (and the reference's up to `topz`) take.
+__device__ __forceinline__ void raise(Sum& a, float top, Factor c) {
     top = fmaf(top, c.hi, -kBelow);
-    if (top > E) {
+    if (top > a.E) {
         const float to = fminf(ceilf(top), 2.f * kFar);
-        s = moved(s, E, to);
-        x = moved(x, E, to);
-        E = to;
+        a.s = moved(a.s, a.E, to);
+        a.E = to;
+    }
+}
+__device__ __forceinline__ void raise(SumRef& a, float top, float topz, Factor c) {
+    top = fmaf(top, c.hi, -kBelow);
+    topz = fmaf(topz, c.hi, -kBelow);
+    if (top > a.E) {
+        const float to = fminf(ceilf(top), 2.f * kFar);
+        a.s = moved(a.s, a.E, to);
+        a.x = crossed(moved(a.x, a.E, to), a.s, to - a.E, 0.f);
+        a.E = to;
+    }
+    if (topz > a.Ez) {
+        const float to = fminf(ceilf(topz), 2.f * kFar);
+        a.sz = moved(a.sz, a.Ez, to);
+        a.x = crossed(a.x, a.s, 0.f, to - a.Ez);
+        a.Ez = to;
     }
 }
 template <int N>
@@ -166,8 +187,7 @@ template <int PARTS, int N>
 __device__ __forceinline__ void add_under(Sum& a, const float (&h)[N], Factor c);
 template <int PARTS, int N>
 __device__ __forceinline__ void add(Sum& a, const float (&h)[N], Factor c) {
-    float none = 0.f;
-    raise(a.E, a.s, none, largest(h), c);
+    raise(a, largest(h), c);
     add_under<PARTS>(a, h, c);
 }
 // The same where the reference is as high as it has to be.
@@ -182,9 +202,7 @@ template <int PARTS, int N>
 __device__ __forceinline__ void add_under(SumRef& a, const float (&h)[N], const float (&z)[N], Factor c);
 template <int PARTS, int N>
 __device__ __forceinline__ void add(SumRef& a, const float (&h)[N], const float (&z)[N], Factor c) {
-    float none = 0.f;
-    raise(a.E, a.s, a.x, largest(h), c);
-    raise(a.Ez, a.sz, none, largest(z), c);
+    raise(a, largest(h), largest(z), c);
     add_under<PARTS>(a, h, z, c);
 }
 template <int PARTS, int N>
@@ -192,9 +210,10 @@ __device__ __forceinline__ void add_under(SumRef& a, const float (&h)[N], const 
     float e[N], ez[N], x[N];
 #pragma unroll
     for (int i = 0; i < N; ++i) {
-        e[i] = term<PARTS>(h[i], a.E, c);
-        x[i] = e[i] * logit_diff(h[i], z[i]);
-        ez[i] = term<PARTS>(z[i], a.Ez, c);
+        const float t = exponent<PARTS>(h[i], a.E, c), tz = exponent<PARTS>(z[i], a.Ez, c);
+        e[i] = exp2_hw(t);
+        x[i] = e[i] * exponent_diff(t, tz);
+        ez[i] = exp2_hw(tz);
     }
     a.s += tree_sum(e);
     a.x += tree_sum(x);
@@ -231,8 +250,9 @@ __device__ __forceinline__ Total<SumRef> wave_total(const SumRef& a) {
     Total<SumRef> r;
     r.E = (float)wave_max_i32((int)a.E);
     r.Ez = (float)wave_max_i32((int)a.Ez);
-    r.s = wave_sum_f64((double)moved(a.s, a.E, r.E));
-    r.x = wave_sum_f64((double)moved(a.x, a.E, r.E));
+    const double s = (double)moved(a.s, a.E, r.E);
+    r.s = wave_sum_f64(s);
+    r.x = wave_sum_f64(crossed((double)moved(a.x, a.E, r.E), s, r.E - a.E, r.Ez - a.Ez));
     r.sz = wave_sum_f64((double)moved(a.sz, a.Ez, r.Ez));
     return r;
 }
@@ -249,8 +269,9 @@ __device__ __forceinline__ Total<SumRef> join(const Total<SumRef>& a, int n) {
     Total<SumRef> r;
     r.E = (float)wave_max_i32((int)a.E);
     r.Ez = (float)wave_max_i32((int)a.Ez);
-    r.s = wave_sum_f64(has ? moved(a.s, a.E, r.E) : 0.0);
-    r.x = wave_sum_f64(has ? moved(a.x, a.E, r.E) : 0.0);
+    const double s = moved(a.s, a.E, r.E);
+    r.s = wave_sum_f64(has ? s : 0.0);
+    r.x = wave_sum_f64(has ? crossed(moved(a.x, a.E, r.E), s, r.E - a.E, r.Ez - a.Ez) : 0.0);
     r.sz = wave_sum_f64(has ? moved(a.sz, a.Ez, r.Ez) : 0.0);
     return r;
 }
@@ -275,8 +296,9 @@ __device__ __forceinline__ Total<SumRef> join_group(const Total<SumRef>& a, int 
     Total<SumRef> r;
     r.E = group_max(a.E, group);
     r.Ez = group_max(a.Ez, group);
-    r.s = group_sum(moved(a.s, a.E, r.E), group);
-    r.x = group_sum(moved(a.x, a.E, r.E), group);
+    const double s = moved(a.s, a.E, r.E);
+    r.s = group_sum(s, group);
+    r.x = group_sum(crossed(moved(a.x, a.E, r.E), s, r.E - a.E, r.Ez - a.Ez), group);
     r.sz = group_sum(moved(a.sz, a.Ez, r.Ez), group);
     return r;
 }
@@ -303,7 +325,8 @@ struct Rows {
     Factor c;              // log2(e) / tau
     int far;               // all rows take the sweeps for those far from zero
     double c64;
-    double inv_tau, scale; // 1 / tau, the gradient's factor
+    double tau, inv_tau;
+    double scale;          // the gradient's factor
     double rest;           // what c as one fp32 number leaves out, in shares of it
 };
 
@@ -381,7 +404,8 @@ __device__ __forceinline__ S lane_sum(const void* h, const void* z, const Layout
 // and c have few bits.
 __device__ __forceinline__ float far_term(float h, double m, double c) { return exp2_hw((float)(((double)h - m) * c)); }
 
-// The sums of a row with its largest logit m for a reference: E = m and s = sum 2^((h - m) c), element by element over a workgroup.
+// The sums of a row with its largest logit m for a reference: E = m and s = sum 2^((h - m) c), x = sum 2^((h - m) c) (h - z), element by element
+// over a workgroup.
 // Differences are exact where they matter, so that this holds for any finite row (of lowest values only: a uniform one).
 template <int DT, typename S>
 __device__ __forceinline__ Total<S> far_sum(const void* h, const void* z, int V, double c, int threads, Total<S>* part) {
@@ -431,37 +455,45 @@ __device__ __forceinline__ Total<S> far_sum(const void* h, const void* z, int V,
 }
 
 // What the gradient of a row needs: dL/dh_v = e (scale + cross (h_v - z_v)) + at_token 1[v = y], e = 2^(h_v c - E).  For a row far from zero
-// e = 2^((h_v - m) c) with the maximum m in E, and cross is to be divided by tau still.  Differences count up to +-limit, which times
-// cross is a number: that of a token which either side masks is infinite or the type's largest, and its e = 0 has to come out as 0.
+// e = 2^((h_v - m) c) with the maximum m in E, and cross is to be divided by tau still.  Differences of logits count up to +-limit, which times
+// cross is a number: that of a token which either side masks is infinite or the type's largest, and its e = 0 has to come out as 0.  For an fp32
+// gradient they are taken less their mean, `shift`, which leaves nothing for `scale` to cancel.  A bf16 one is rounded by far more than the
+// cancelling loses (2^-24 of the mean against 2^-9 of the difference to it), and the subtraction is 1 to 2 % of the policy loss.
 struct RowGrad {
-    float E, scale, cross, at_token, limit;
+    float E, scale, cross, at_token, shift, limit;
 };
 
-// g = weight of the row's log-prob, k that of its KL, both with the call's factor; diff = D, the difference of the log-sum-exps.
+// g = weight of the row's log-prob, k that of its KL, both with the call's factor; mean = E[h - z] / tau.
 // Gradients are formed with c as one number: where the sums are not, what its rest adds at the reference goes into the factor here, and what is
 // left is 2^-24 of |h c - E| of a term.
 template <int DT, bool REF, int PARTS>
-__device__ __forceinline__ RowGrad row_grad(const Rows& a, bool far, float E, double s, double g, double k, double diff, double kl) {
+__device__ __forceinline__ RowGrad row_grad(const Rows& a, bool far, float E, double s, double g, double k, double mean) {
     RowGrad r;
     double f = a.inv_tau / s;
     if (PARTS == 2 && !far) f *= (double)exp2_hw(E * (float)a.rest);
     r.E = E;
-    r.scale = (float)((REF && k != 0.0 ? -g - k * (diff + kl) : -g) * f);
+    r.shift = REF && DT == SS_F32 ? (float)(mean * a.tau) : 0.f;
+    if (!(fabsf(r.shift) < 3e38f)) r.shift = 0.f;
+    r.scale = (float)((REF && k != 0.0 ? -g - k * (mean - (double)r.shift * a.inv_tau) : -g) * f);
     r.cross = REF ? (float)(k * (far ? 1.0 : a.inv_tau) * f) : 0.f;
-    r.limit = 1e38f / fmaxf(1.f, fabsf(r.cross));
+    const int e = __builtin_amdgcn_frexp_expf(r.cross);  // |cross| < 2^e
+    r.limit = __builtin_ldexpf(1.f, 126 - (e > 0 ? e : 0));
     r.at_token = (float)(g * a.inv_tau);
     return r;
 }
 
-template <bool REF>
+template <int DT, bool REF>
 __device__ __forceinline__ float grad_of_term(const RowGrad& r, float e, float h, float z) {
     // bounded above as well: without a weight of the KL a token that the reference alone masks takes nothing from it
-    if constexpr (REF) return e * fmaf(r.cross, __builtin_amdgcn_fmed3f(h - z, -r.limit, r.limit), r.scale);
+    if constexpr (REF) {
+        const float d = DT == SS_F32 ? h - z - r.shift : h - z;
+        return e * fmaf(r.cross, __builtin_amdgcn_fmed3f(d, -r.limit, r.limit), r.scale);
+    }
     return e * r.scale;
 }
 template <int DT, bool REF>
 __device__ __forceinline__ float grad_of(const RowGrad& r, float h, float z, Factor c) {
-    return grad_of_term<REF>(r, term<1>(h, r.E, c), h, z);
+    return grad_of_term<DT, REF>(r, term<1>(h, r.E, c), h, z);
 }
 
 // The gradient of a row far from zero, element by element over a workgroup.
@@ -470,7 +502,7 @@ __device__ __forceinline__ void far_grad(const void* h, const void* z, void* g, 
     for (int i = threadIdx.x; i < a.V; i += threads) {
         const float hv = ld_elem<DT>(h, i), zv = REF ? ld_elem<DT>(z, i) : 0.f, e = far_term(hv, r.E, a.c64);
         // a token that the policy masks counts nothing, whatever the reference says of it
-        const float by = REF && e > 0.f && r.cross != 0.f ? fmaf(r.cross, (float)(((double)hv - (double)zv) * a.inv_tau), r.scale) : r.scale;
+        const float by = REF && e > 0.f && r.cross != 0.f ? fmaf(r.cross, (float)(((double)hv - (double)zv - (double)r.shift) * a.inv_tau), r.scale) : r.scale;
         st_elem<DT>(g, i, e * by + (i == token ? r.at_token : 0.f));
     }
 }
@@ -541,12 +573,19 @@ __device__ __forceinline__ double token_logprob(const Rows& a, bool far, int tok
     if (far) return ((double)h - (double)E) * a.inv_tau - log(s);
     return ((double)h * a.c64 - reference<PARTS>(a, E) - log2(s)) * kLn2;
 }
-// log-sum-exp of the policy's row less that of the reference's
+// mean: E[h - z] / tau of a row; kl: that less the difference of the log-sum-exps
 template <int PARTS>
-__device__ __forceinline__ double lse_difference(const Rows& a, bool far, const Total<SumRef>& s) {
+__device__ __forceinline__ void divergence(const Rows& a, bool far, const Total<SumRef>& s, double& mean, double& kl) {
     const double sums = log2(s.s) - log2(s.sz);
-    if (far) return ((double)s.E - (double)s.Ez) * a.inv_tau + sums * kLn2;
-    return (reference<PARTS>(a, s.E) - reference<PARTS>(a, s.Ez) + sums) * kLn2;
+    if (far) {
+        mean = s.x / s.s * a.inv_tau;
+        kl = mean - (((double)s.E - (double)s.Ez) * a.inv_tau + sums * kLn2);
+    } else {
+        const double x = s.x / s.s * (PARTS == 2 ? 1.0 : 1.0 + a.rest);  // c's rest counts in differences of exponents too
+        mean = (x + (reference<PARTS>(a, s.E) - reference<PARTS>(a, s.Ez))) * kLn2;
+        kl = (x - sums) * kLn2;
+    }
+    if (kl < 0.0) kl = 0.0;  // by rounding only
 }
 
 // The sum of x over the workgroup, in every lane of wave 0.  The order is fixed.
@@ -749,7 +788,7 @@ __global__ __launch_bounds__(kGradThreads) void grad_kernel(const GradArgs a) {
     if (y < 0 || y >= a.r.V) w = nan64();
     const float s = a.stats[2 * row + 1];
     const bool far = s < 0.f;
-    const RowGrad rg = row_grad<DT, false, 2>(a.r, far, a.stats[2 * row], fabsf(s), w, 0.0, 0.0, 0.0);
+    const RowGrad rg = row_grad<DT, false, 2>(a.r, far, a.stats[2 * row], fabsf(s), w, 0.0, 0.0);
     if (far) {
         if (slice == 0) far_grad<DT, false>(h, nullptr, g, a.r, rg, y, kGradThreads);
         return;
@@ -776,7 +815,7 @@ struct PolicyArgs {
 };
 
 struct RowLoss {
-    double lp, kl, term, g, k, diff;
+    double lp, kl, term, g, k, mean;
 };
 
 // What a token of the row counts, by any one wave.
@@ -792,16 +831,14 @@ __device__ __forceinline__ RowLoss row_loss(const PolicyArgs& a, bool far, long 
     RowLoss o;
     const double adv = advantage;
     o.lp = token_logprob<PARTS>(a.r, far, y, hy, s.E, s.s);
-    o.kl = o.k = o.diff = 0.0;
+    o.kl = o.k = o.mean = 0.0;
     const double ratio = exp(o.lp - (double)old);
     const double plain = ratio * adv, bound = fmin(fmax(ratio, a.clip_lo), a.clip_hi) * adv;
     const bool clipped = plain > bound;  // NaN: not clipped, and NaN below
     o.term = clipped ? -bound : -plain;
     o.g = clipped ? 0.0 : -plain;
     if constexpr (REF) {
-        o.diff = lse_difference<PARTS>(a.r, far, s);
-        o.kl = s.x / s.s * a.r.inv_tau - o.diff;
-        if (o.kl < 0.0) o.kl = 0.0;  // by rounding only
+        divergence<PARTS>(a.r, far, s, o.mean, o.kl);
         o.k = a.kl_coef;
     } else if (a.ref_logprobs) {
         const double d = (double)a.ref_logprobs[row] - o.lp, e = expm1(d);
@@ -829,7 +866,7 @@ __device__ __forceinline__ RowGrad finish_row(const PolicyArgs& a, bool far, lon
     const RowLoss o = row_loss<REF, 1>(a, far, row, y, hy, old, advantage, n, s);
     write_policy(a, row, o.lp, o.kl);
     a.terms[row] = o.term;
-    return row_grad<DT, REF, 1>(a.r, far, s.E, s.s, o.g, o.k, o.diff, o.kl);
+    return row_grad<DT, REF, 1>(a.r, far, s.E, s.s, o.g, o.k, o.mean);
 }
 
 // The compiler is not to keep anything it has formed of a held vector (its logits widened, twice the registers) for the next use.
@@ -919,14 +956,12 @@ __global__ __launch_bounds__(kMaxThreads) void policy_kernel(const PolicyArgs a)
                 unpack(r[u + v], x[v]);
                 if constexpr (REF) unpack(rz[u + v], w[v]);
             }
-            float none = 0.f;
             if constexpr (REF) {
-                raise(sums.E, sums.s, sums.x, fmaxf(largest(x[0]), largest(x[1])), a.r.c);
-                raise(sums.Ez, sums.sz, none, fmaxf(largest(w[0]), largest(w[1])), a.r.c);
+                raise(sums, fmaxf(largest(x[0]), largest(x[1])), fmaxf(largest(w[0]), largest(w[1])), a.r.c);
                 add_under<1>(sums, x[0], w[0], a.r.c);
                 add_under<1>(sums, x[1], w[1], a.r.c);
             } else {
-                raise(sums.E, sums.s, none, fmaxf(largest(x[0]), largest(x[1])), a.r.c);
+                raise(sums, fmaxf(largest(x[0]), largest(x[1])), a.r.c);
                 add_under<1>(sums, x[0], a.r.c);
                 add_under<1>(sums, x[1], a.r.c);
             }
@@ -1033,7 +1068,7 @@ __device__ __forceinline__ void policy_slices_loss(const PolicyArgs& a, const Sl
                                                 a.count ? counted : row_norm(a, row), s);
                 write_policy(a, row, o.lp, o.kl);
                 loss += o.term;
-                shared_grad = row_grad<DT, REF, 2>(a.r, true, s.E, s.s, o.g, o.k, o.diff, o.kl);
+                shared_grad = row_grad<DT, REF, 2>(a.r, true, s.E, s.s, o.g, o.k, o.mean);
             }
             __syncthreads();
             const RowGrad rg = shared_grad;
@@ -1083,7 +1118,7 @@ __global__ __launch_bounds__(kSliceThreads) void policy_slices_kernel(const Poli
     if (a.r.far || is_far(s)) return;
     const int y = a.r.tokens[row];
     const RowLoss o = row_loss<REF, 2>(a, false, row, y, p.token_logits[row], a.old_logprobs[row], advantage_of(a, row), token_norm(a, row), s);
-    const RowGrad rg = row_grad<DT, REF, 2>(a.r, false, s.E, s.s, o.g, o.k, o.diff, o.kl);
+    const RowGrad rg = row_grad<DT, REF, 2>(a.r, false, s.E, s.s, o.g, o.k, o.mean);
     write_grad<DT, REF>(h, z, g, lay, rg, y, first, end, kSliceThreads, slice == 0, a.r.c, kAhead, r, rz);
 }
 
@@ -1238,7 +1273,8 @@ Rows make_rows(const void* logits, const void* ref, void* grad, const int32_t* t
     r.c.whole = (float)r.c64;
     // 1 / tau^2 is a factor otherwise, which fp32 may not hold, nor c's lower part
     r.far = !(p.temperature > 1e-12f && p.temperature < 1e12f);
-    r.inv_tau = 1.0 / (double)p.temperature;
+    r.tau = (double)p.temperature;
+    r.inv_tau = 1.0 / r.tau;
     r.scale = (double)p.grad_scale;
     r.rest = (r.c64 - (double)r.c.whole) / (double)r.c.whole;
     return r;

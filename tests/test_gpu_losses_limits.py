@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import loss_reference as R
-from test_gpu_losses import check_policy, check_preference, check_score, gen, losses, make  # noqa: F401
+from test_gpu_losses import U_of, check_policy, check_preference, check_score, close, gen, losses, make  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -130,3 +130,31 @@ def test_temperatures_far_from_1(losses, rows, tau, dtype):
     check_preference(losses, inp, g, tau=tau)
     for kl in ("none", "sampled", "full"):
         check_policy(losses, inp, g, kl=kl, tau=tau)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", [(2, 6, 97), (2, 5, 50257), (2, 60, 3001), (1, 101, 70003)])
+@pytest.mark.parametrize("shift", [100.0, -100.0, 700.0])
+@pytest.mark.parametrize("of", ["policy", "reference"])
+def test_a_common_offset_of_policy_or_reference(losses, rows, shift, of, dtype):
+    """Logits are defined up to a constant a row: whole-vocabulary KL and gradient are as near to their definition as without the offset,
+    by the bounds of the unshifted rows.  Logits on a grid of the type's steps at the offset, so that shifting rounds nothing."""
+    inp, g = make(*rows, dtype, sigma=1.0, ref=True)
+    x, y = inp["logits"], inp["tokens"]
+    grid = 2.0 ** math.floor(math.log2(abs(shift) + 64)) * torch.finfo(x.dtype).eps
+    h = (torch.randn(x.shape, generator=g, device="cuda").double() * max(1.0, 4 * grid) / grid).round() * grid
+    z = h + (torch.randn(x.shape, generator=g, device="cuda").double() * max(0.2, grid) / grid).round() * grid
+    tau = max(1.0, 2 * grid)
+    plain = R.Rows(h, y, tau, z)
+    h, z = (h + shift, z) if of == "policy" else (h, z + shift)
+    assert torch.equal(h.to(x.dtype).double(), h) and torch.equal(z.to(x.dtype).double(), z)
+    old = adv = torch.zeros(y.shape, device="cuda")  # the KL alone
+    out = losses.policy_loss(h.to(x.dtype), y, old, adv, ref_logits=z.to(x.dtype), kl_coef=1.0, temperature=tau)
+    close(out["kl"], plain.kl, plain.kl_err + U_of(plain.kl), "kl")
+    none = torch.zeros_like(plain.lp)
+    k = none + 1 / y.numel()
+    exact = plain.gradient(none, k)
+    bound = plain.gradient_bound(none, exact, x.dtype, k)
+    if dtype == "bf16":  # formed from whole differences in fp32: the offset's and the mean's roundings, a half step each, and the product's
+        bound = bound + 3 * R.U * abs(shift) / tau * (k[..., None] * plain.p) / tau
+    close(out["grad_logits"], exact, bound, "grad_logits")
