@@ -158,3 +158,44 @@ def test_a_common_offset_of_policy_or_reference(losses, rows, shift, of, dtype):
     if dtype == "bf16":  # formed from whole differences in fp32: the offset's and the mean's roundings, a half step each, and the product's
         bound = bound + 3 * R.U * abs(shift) / tau * (k[..., None] * plain.p) / tau
     close(out["grad_logits"], exact, bound, "grad_logits")
+
+
+@pytest.mark.parametrize("kl", ["none", "full"])
+@pytest.mark.parametrize("rows,V", [(100, 128256), (64, 50257), (300, 50257)])
+def test_rows_of_nan_take_no_sweeps_of_their_own(losses, rows, V, kl):
+    """What a diverged model gives: NaN wherever it reaches, at the time of other rows (those far from zero are swept one after the other, some
+    hundred times slower)."""
+    inp, g = make(1, rows, V, "bf16", ref=True)
+    x, y = inp["logits"], inp["tokens"]
+    more = {"ref_logits": inp["ref_logits"], "kl_coef": 0.1} if kl == "full" else {}
+    old = torch.full(y.shape, -10.0, device="cuda")
+
+    def call(t):
+        return losses.policy_loss(t, y, old, old, **more)
+
+    def time(t):
+        best = math.inf
+        for _ in range(5):
+            start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            start.record()
+            for _ in range(5):
+                call(t)
+            end.record()
+            end.synchronize()
+            best = min(best, start.elapsed_time(end))
+        return best
+
+    bad = torch.full_like(x, math.nan)
+    out = call(bad)
+    assert out["loss"].isnan() and out["logprobs"].isnan().all() and out["grad_logits"].isnan().all()
+    assert kl == "none" or out["kl"].isnan().all()
+    scored = losses.token_logprobs(bad, y, want_stats=True)
+    assert scored["logprobs"].isnan().all()
+    assert losses.token_logprobs_grad(bad, y, scored["stats"], old).isnan().all()
+    assert time(bad) <= 5 * time(x)
+    if kl == "full":  # NaN in the reference alone: the log-probs are what they are, also of rows far from zero
+        x[0, 3] = 3e6
+        want = losses.policy_loss(x, y, old, old)
+        out = losses.policy_loss(x, y, old, old, ref_logits=bad, kl_coef=0.1)
+        assert torch.allclose(out["logprobs"], want["logprobs"], rtol=0, atol=2e-6) and out["kl"].isnan().all() and out["loss"].isnan()
+        assert out["grad_logits"].isnan().all()
