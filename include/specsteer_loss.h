@@ -8,7 +8,8 @@
  *   specsteer_preference_loss      the loss of paired sequences' log ratios, and its gradient
  *
  * Logits are [B, T, V], vocabulary contiguous, row (b, t) scoring tokens[b][t]; P = Softmax(h / tau) over the
- * whole vocabulary, tau = params->temperature.  mask [B, T] says which positions count: the logits, tokens and
+ * whole vocabulary, tau = params->temperature.  As in specsteer.h a sequence's rows lie before those of the next: stride_t >= V and
+ * stride_b >= (T - 1) stride_t + V, with any gaps.  [T, B, V] logits, whose sequences interleave, are refused.  mask [B, T] says which positions count: the logits, tokens and
  * other inputs of a position that does not are never read, its outputs are 0 and so is its row of the gradient.
  *
  * Gradients are written, not accumulated: grad_logits has the logits' type, each element is rounded to it once.
@@ -45,8 +46,9 @@ typedef struct {
     int32_t length;        /* T, 0..SS_LOSS_MAX_LENGTH                                                 */
     int32_t vocab;         /* V, 1..SS_MAX_VOCAB                                                       */
     int32_t dtype;         /* ss_dtype of the logits and of their gradient                             */
-    int64_t stride_b;      /* element stride between sequences of the logits; 0 => length * stride_t   */
-    int64_t stride_t;      /* element stride between rows;                    0 => vocab               */
+    int64_t stride_b;      /* element stride between sequences of the logits; 0 => length * stride_t;  */
+                           /* at least (length - 1) * stride_t + vocab                                 */
+    int64_t stride_t;      /* element stride between rows, at least vocab;    0 => vocab               */
     int64_t grad_stride_b; /* the same of grad_logits                                                  */
     int64_t grad_stride_t;
     float temperature;     /* tau; finite, > 0, and 1.45 / tau < 3e38                                     */

@@ -1470,7 +1470,7 @@ const char* specsteer_loss_status_string(int status) {
         case SS_ERR_SHAPE: return "batch, length or vocab out of range, or an odd batch of pairs";
         case SS_ERR_DTYPE: return "unknown logits dtype";
         case SS_ERR_PARAM: return "temperature, coefficients or flags out of range, or two references";
-        case SS_ERR_STRIDE: return "strides negative, rows overlap, or a pointer off its element";
+        case SS_ERR_STRIDE: return "strides negative, rows that overlap, sequences that interleave, or a pointer off its element";
         case SS_ERR_WORKSPACE: return "workspace missing, misaligned or too small";
         case SS_ERR_DEVICE: return "HIP launch failed";
         default: return "unknown status";

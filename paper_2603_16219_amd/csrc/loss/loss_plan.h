@@ -16,7 +16,7 @@ struct LossShape {
     long gsb, gst;  // of their gradient
 };
 
-// Dense strides for those that are 0; false for rows that overlap.
+// Dense strides for those that are 0; false for rows that overlap and for sequences that interleave.
 inline bool loss_strides(int64_t sb, int64_t st, const ss_loss_params& p, long& out_sb, long& out_st) {
     if (sb < 0 || st < 0) return false;
     out_st = st ? st : (long)p.vocab;

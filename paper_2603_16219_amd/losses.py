@@ -10,8 +10,11 @@ A loss comes with the gradient of the logits it was given, which the model's own
     out = losses.policy_loss(logits, tokens, old_logprobs, advantages, mask=mask, ref_logprobs=ref, kl_coef=0.05)
     logits.backward(out["grad_logits"])
 
-The gradient may go to a tensor of the caller's, `grad_logits=`, which may be the logits themselves.  Autograd takes that for an operation in place:
-the backward pass of a model whose last operation keeps its output (a tanh, say) refuses logits that were replaced.
+Logits may have any strides with the vocabulary contiguous and each sequence's rows before the next one's (logits[:, :-1] of a padded
+vocabulary; not [T, B, V].transpose(0, 1)).
+
+The gradient may go to a tensor of the caller's, `grad_logits=`, which may be the logits themselves.  Autograd takes that for an operation in
+place: the backward pass of a model whose last operation keeps its output (a tanh, say) refuses logits that were replaced.
 """
 from __future__ import annotations
 

@@ -1,7 +1,7 @@
 """CPU checks of what the losses' calls accept, at the limits of strides."""
 import pytest
 
-from test_losses_host import CALLS, STRIDE, Call, losses  # noqa: F401
+from test_losses_host import CALLS, STRIDE, WORKSPACE, Call, losses  # noqa: F401
 
 
 @pytest.mark.parametrize("name", CALLS)
@@ -24,4 +24,14 @@ def test_the_largest_offsets_are_accepted(losses, field):
     # the last byte behind the last element at 2^63 - 4: refused for its workspace only, which is looked at after the strides
     shape = dict(batch=1, length=2) if field.endswith("t") else dict(batch=2, length=1)
     for name in ("token_logprobs", "policy_loss"):
-        assert Call(losses, name)(**shape, **{field: (1 << 61) - 101}, workspace=None) == 6
+        assert Call(losses, name)(**shape, **{field: (1 << 61) - 101}, workspace=None) == WORKSPACE
+
+
+@pytest.mark.parametrize("name", CALLS)
+@pytest.mark.parametrize("spoiled", [dict(stride_b=100, stride_t=400), dict(grad_stride_b=100, grad_stride_t=400), dict(stride_b=800 - 1)])
+def test_sequences_that_interleave_are_refused_by_name(losses, name, spoiled):
+    """[T, B, V] logits as [B, T, V]: rows of their own, but not one sequence behind the other."""
+    status = Call(losses, name)(**spoiled)
+    assert status == STRIDE and "interleave" in losses.status_string(status)
+    for b, t in ((807, 101), (800, 100), (1 << 40, 1 << 20)):  # gaps of any size between rows and sequences are fine
+        assert name == "token_logprobs_grad" or Call(losses, name)(stride_b=b, stride_t=t, grad_stride_b=b, grad_stride_t=t, workspace=None) == WORKSPACE
