@@ -631,8 +631,17 @@ struct ScoreArgs {
     float* logprobs;    // or NULL
     float* stats;       // or NULL
     double* logprob64;  // or NULL
-    long keep_from;     // rows from here on are read through the caches, for a gradient that reads them again soon
+    long keep_from;     // rows from here on are read through the caches, for a gradient that reads them again soon,
+    int if_sparse;      // if few enough of them count
 };
+
+// Whether few enough of the rows from keep_from on count, by 64 of them at multiples of the golden ratio, which fall anywhere in sequences of any
+// length and are the same for all workgroups.
+__device__ __forceinline__ bool sparse(const ScoreArgs& a) {
+    const unsigned long of = (unsigned)((threadIdx.x & 63) + 1) * 2654435769u;
+    const uint8_t m = a.r.mask[a.keep_from + (long)((unsigned long)(a.r.rows - a.keep_from) * of >> 32)];
+    return __popcll(__ballot(m != 0)) <= kSparse;
+}
 
 __device__ __forceinline__ void write_score(const ScoreArgs& a, long row, double lp, float E, double s) {
     if (a.logprobs) a.logprobs[row] = (float)lp;
@@ -671,8 +680,9 @@ __global__ __launch_bounds__(kMaxThreads) void score_kernel(const ScoreArgs a) {
     place(a.r, row, at, grad_at);
     const void* const h = row_ptr<DT>(a.r.logits, at);
     const Layout<DT> lay(h, a.r.V, threadIdx.x);
-    const Sum mine = row >= a.keep_from ? lane_sum<DT, Sum, 2, false>(h, nullptr, lay, threadIdx.x, lay.vecs, threads, true, a.r.c)
-                                        : lane_sum<DT, Sum, 2, true>(h, nullptr, lay, threadIdx.x, lay.vecs, threads, true, a.r.c);
+    const bool keep = row >= a.keep_from && (!a.if_sparse || sparse(a));
+    const Sum mine = keep ? lane_sum<DT, Sum, 2, false>(h, nullptr, lay, threadIdx.x, lay.vecs, threads, true, a.r.c)
+                          : lane_sum<DT, Sum, 2, true>(h, nullptr, lay, threadIdx.x, lay.vecs, threads, true, a.r.c);
     const Total<Sum> s = block_total(mine, threads, part);
     if (a.r.far || is_far(s)) {
         score_far_row<DT>(a, row, threads, part);
@@ -1355,7 +1365,8 @@ ss_status specsteer_token_logprobs(const void* logits, const int32_t* tokens, co
     if (off_element(logits, *params)) return SS_ERR_STRIDE;
     const LossScratch w = loss_scratch(*params);
     if (check_workspace(workspace, workspace_bytes, w.bytes) != SS_OK) return SS_ERR_WORKSPACE;
-    const ScoreArgs a{make_rows(logits, nullptr, nullptr, tokens, mask, *params, s), logprobs, stats, nullptr, s.rows - (stats ? cached_rows(*params, s.rows, false) : 0)};
+    const long kept = stats ? cached_rows(*params, s.rows, false).n : 0;
+    const ScoreArgs a{make_rows(logits, nullptr, nullptr, tokens, mask, *params, s), logprobs, stats, nullptr, s.rows - kept, 0};
     launch_score(*params, a, w, workspace, static_cast<hipStream_t>(stream));
     return launched();
 }
@@ -1445,7 +1456,8 @@ ss_status specsteer_preference_loss(const void* logits, const int32_t* tokens, c
     float* const stats = reinterpret_cast<float*>(base + w.stats);
     double *const weight = reinterpret_cast<double*>(base + w.seq), *const loss64 = weight + pairs;
     const Rows r = make_rows(logits, nullptr, grad_logits, tokens, mask, *params, s);
-    const ScoreArgs sa{r, logprobs, stats, lp64, s.rows - (grad_logits ? cached_rows(*params, s.rows, mask != nullptr) : 0)};
+    const CachedRows kept = grad_logits ? cached_rows(*params, s.rows, mask != nullptr) : CachedRows{0, false};
+    const ScoreArgs sa{r, logprobs, stats, lp64, s.rows - kept.n, kept.if_sparse ? 1 : 0};
     Slices c{nullptr, nullptr, 1, 0};
     const bool one = pairs_in_one(pairs, params->length), join = one && s.rows > 0 && s.rows <= kJoinRows && score_slices(s.rows, row_vecs(*params)) > 1;
     if (join) launch_slices<Sum>(*params, r, w, workspace, score_slices(s.rows, row_vecs(*params)), c, q);

@@ -95,12 +95,21 @@ inline int row_vecs(const ss_loss_params& p) { return p.vocab / (p.dtype == SS_B
 // How many of a call's last rows are read through the caches for a gradient behind it.  All where 256 MiB of last-level cache may hold them (2048
 // rows of V = 50257 bf16 scored and their gradient 108 us past the caches, 101 through them).  In larger calls the gradient, which begins
 // at the end, finds little, and reading past the caches is faster (4096 rows of V = 128256 515 us a preference loss, 531 with 300 MB through them) -- but
-// for a preference loss with a mask: of 600 MB of rows those that count are about what the caches hold (16 x 1024 tokens of V = 32000 with half of
-// them masked 389 and 372 us, 8 x 512 of V = 128256 405 and 385).
-inline long cached_rows(const ss_loss_params& p, long rows, bool masked) {
-    const double row = (double)p.vocab * (p.dtype == SS_BF16 ? 2 : 4), most = rows * row <= 268435456.0 ? rows * row : masked ? 600e6 : 0.0;
-    const long n = (long)(most / row);
-    return n < rows ? n : rows;
+// for a preference loss whose mask leaves out enough: of 600 MB of rows those that count are about what the caches hold then.  Only the GPU knows
+// what a mask keeps, so that its rows ask (kSparse of 64 of them).  Past the caches and through them, us, by the share of rows kept:
+//   16 x 1024 of V = 32000 bf16   a quarter 326, 289   half 423, 401   three quarters 466, 467   19 of 20 519, 536
+//   8 x 512 of V = 128256 bf16    a quarter 330, 294   half 380, 352   three quarters 461, 467   19 of 20 504, 531
+//   8 x 512 of V = 50257 fp32                          half 321, 301   five eighths 353, 339     19 of 20 414, 442
+struct CachedRows {
+    long n;
+    bool if_sparse;  // only if few enough of them count
+};
+constexpr int kSparse = 45;
+inline CachedRows cached_rows(const ss_loss_params& p, long rows, bool masked) {
+    const double row = (double)p.vocab * (p.dtype == SS_BF16 ? 2 : 4);
+    if (rows * row <= 268435456.0) return {rows, false};
+    const long n = masked ? (long)(600e6 / row) : 0;
+    return {n < rows ? n : rows, masked};
 }
 
 inline LossScratch loss_scratch(const ss_loss_params& p) {

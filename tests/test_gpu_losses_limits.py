@@ -199,3 +199,23 @@ def test_rows_of_nan_take_no_sweeps_of_their_own(losses, rows, V, kl):
         out = losses.policy_loss(x, y, old, old, ref_logits=bad, kl_coef=0.1)
         assert torch.allclose(out["logprobs"], want["logprobs"], rtol=0, atol=2e-6) and out["kl"].isnan().all() and out["loss"].isnan()
         assert out["grad_logits"].isnan().all()
+
+
+@pytest.mark.parametrize("B,T,V", [(16, 300, 32000), (4, 1025, 50257)])
+@pytest.mark.parametrize("kept", [0.0, 0.3, 0.68, 0.72, 1.0])
+def test_what_a_mask_keeps_decides_about_the_caches_only(losses, B, T, V, kept):
+    """Preference losses of more than the caches hold: the same log-probs and gradient whichever way the rows are read."""
+    inp, g = make(B, T, V, "bf16")
+    x, y = inp["logits"], inp["tokens"]
+    mask = torch.rand(B, T, generator=g, device="cuda") < kept
+    scored = losses.token_logprobs(x, y, mask=mask, want_stats=True)
+    out = losses.preference_loss(x, y, mask=mask, beta=0.01)
+    assert torch.equal(out["logprobs"], scored["logprobs"])
+    d = torch.where(mask, out["logprobs"], 0.0).double().sum(1)
+    margin = R.f32(0.01) * (d[:B // 2] - d[B // 2:])  # of sums of log-probs as they are before they are rounded, by half a step each
+    close(out["margin"], margin, 0.01 * 2 * T * R.U * 32 + U_of(margin), "margin")
+    w = (-R.f32(0.01) / (B // 2) * torch.sigmoid(-out["margin"].double()))
+    w = torch.cat([w, -w])[:, None].expand(B, T).float().contiguous()
+    grad = losses.token_logprobs_grad(x, y, scored["stats"], w, mask=mask)
+    # both round w (1[v = y] - p) to bf16 once, from weights that differ by a few steps of fp32
+    assert ((out["grad_logits"].float() - grad.float()).abs() <= 2.0 ** -7 * grad.float().abs() + 1e-30).all()

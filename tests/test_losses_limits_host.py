@@ -1,7 +1,10 @@
-"""CPU checks of what the losses' calls accept, at the limits of strides."""
+"""CPU checks of what the losses' calls accept, at the limits of strides, and of which rows are read through the caches."""
+import os
+import subprocess
+
 import pytest
 
-from test_losses_host import CALLS, STRIDE, WORKSPACE, Call, losses  # noqa: F401
+from test_losses_host import CALLS, ROOT, STRIDE, WORKSPACE, Call, losses  # noqa: F401
 
 
 @pytest.mark.parametrize("name", CALLS)
@@ -35,3 +38,23 @@ def test_sequences_that_interleave_are_refused_by_name(losses, name, spoiled):
     assert status == STRIDE and "interleave" in losses.status_string(status)
     for b, t in ((807, 101), (800, 100), (1 << 40, 1 << 20)):  # gaps of any size between rows and sequences are fine
         assert name == "token_logprobs_grad" or Call(losses, name)(stride_b=b, stride_t=t, grad_stride_b=b, grad_stride_t=t, workspace=None) == WORKSPACE
+
+
+def test_rows_read_through_the_caches(tmp_path):
+    """csrc/loss/loss_plan.h: all of a call's rows where the caches hold them, none of a larger one's without a mask; with one the last 600 MB,
+    if what the mask keeps of them turns out to be little enough, never without asking."""
+    calls = [(8, 64, 50257, 1), (8, 512, 128256, 1), (16, 1024, 32000, 1), (8, 512, 50257, 0), (4, 2, 1 << 20, 0)]
+    src = tmp_path / "rows.cpp"
+    src.write_text('#include <cstdio>\n#include "loss_plan.h"\nint main() { const int c[][4] = {' + ", ".join("{%d, %d, %d, %d}" % c for c in calls) +
+                   '}; for (const auto& v : c) for (int masked = 0; masked < 2; ++masked) { ss_loss_params p = {v[0], v[1], v[2], v[3], 0, 0, 0, 0, 1.f, 1.f};'
+                   ' const CachedRows r = cached_rows(p, (long)v[0] * v[1], masked); std::printf("%ld %d\\n", r.n, (int)r.if_sparse); } }\n')
+    exe = tmp_path / "rows"
+    subprocess.run(["g++", "-std=c++17", "-Wall", "-Wextra", "-Werror", "-Wno-unused-function", "-I", os.path.join(ROOT, "include"),
+                    "-I", os.path.join(ROOT, "paper_2603_16219_amd", "csrc", "loss"), "-o", exe, src], check=True)
+    got = [tuple(map(int, line.split())) for line in subprocess.run([exe], check=True, capture_output=True, text=True).stdout.splitlines()]
+    for (B, T, V, dtype), plain, masked in zip(calls, got[::2], got[1::2]):
+        rows, row = B * T, V * (2 if dtype else 4)
+        if rows * row <= 1 << 28:
+            assert plain == masked == (rows, 0)
+        else:
+            assert plain == (0, 0) and masked == (min(rows, 600_000_000 // row), 1)
