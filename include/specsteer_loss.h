@@ -27,7 +27,10 @@
  * (unless its P is below what fp32 holds).
  * A token outside [0, V) at a position that counts, or a row whose logits are all -inf, has the log-prob NaN, and
  * so have the loss and the gradient rows that depend on it.  A given token of probability zero has the log-prob
- * -inf.  +inf and NaN among the logits are unspecified but never fault.
+ * -inf: the KL estimated from it is +inf, its pair's margin +inf or -inf, of which the loss is 0 or +inf, and NaN only
+ * where both sequences of a pair hold one.  Weights that pass fp32 (of a huge grad_scale, say) make a row's
+ * gradient not finite.  +inf and NaN among the logits are unspecified but never fault.
+ * The same row's log-prob may differ in its last bits between calls of different kinds and numbers of rows.
  */
 #ifndef SPECSTEER_LOSS_H
 #define SPECSTEER_LOSS_H
