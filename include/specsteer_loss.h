@@ -23,8 +23,8 @@
  *
  * Values.  A logit of -inf, or of the type's lowest value, masks a token: probability zero (the lowest value in a
  * whole row is a uniform row).  In a whole-vocabulary KL a token that the policy masks counts nothing, whatever
- * the reference says of it; one that only the reference masks with -inf makes the row's KL and gradient not finite
- * (unless its P is below what fp32 holds).
+ * the reference says of it, and so does one whose P is far below what fp32 holds; another that only the reference
+ * masks makes the row's KL and gradient not finite (with the lowest value, or about as large as that).
  * A token outside [0, V) at a position that counts, or a row whose logits are all -inf, has the log-prob NaN, and
  * so have the loss and the gradient rows that depend on it.  A given token of probability zero has the log-prob
  * -inf: the KL estimated from it is +inf, its pair's margin +inf or -inf, of which the loss is 0 or +inf, and NaN only

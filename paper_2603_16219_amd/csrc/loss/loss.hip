@@ -110,9 +110,9 @@ __device__ __forceinline__ float exponent(float h, float E, Factor c) { return P
 template <int PARTS>
 __device__ __forceinline__ float term(float h, float E, Factor c) { return exp2_hw(exponent<PARTS>(h, E, c)); }
 
-// The difference of a token's exponents, and a number for one that the policy masks (-inf - -inf among them), whose term is 0 then.  +inf where
-// the reference alone masks one.
-__device__ __forceinline__ float exponent_diff(float t, float tz) { return fmaxf(t - tz, -3e38f); }
+// A product that is 0 if a factor is, whatever the other: the term of a token that the policy masks, or gives no probability in fp32, times the difference
+// of its exponents, which is infinite or NaN (-inf - -inf) then.  +inf remains where the reference alone masks a token.
+extern "C" __device__ float mul_or_zero(float a, float b) __asm("llvm.amdgcn.fmul.legacy");  // v_mul_legacy_f32, which has no builtin
 
 // A running sum: the reference E and sum 2^(h c - E).
 struct Sum {
@@ -125,9 +125,10 @@ struct SumRef {
 __device__ __forceinline__ void clear(Sum& a) { a.E = -kFar; a.s = 0.f; }
 __device__ __forceinline__ void clear(SumRef& a) { a.E = a.Ez = -kFar; a.s = a.x = a.sz = 0.f; }
 __device__ __forceinline__ float moved(float s, float from, float to) { return __builtin_ldexpf(s, (int)(from - to)); }
-// A cross term at other references, by and byz higher, from what it is with only its terms moved to them, and their sum.
-__device__ __forceinline__ float crossed(float x, float s, float by, float byz) { return fmaf(s, byz - by, x); }
-__device__ __forceinline__ double crossed(double x, double s, float by, float byz) { return x + s * (double)(byz - by); }
+// A cross term at other references, by and byz higher, from what it is with only its terms moved to them, and their sum.  Where that has become nothing, so
+// has the cross term, which stays infinite by itself if the reference masks one of the tokens (padding that the policy only holds far down).
+__device__ __forceinline__ float crossed(float x, float s, float by, float byz) { return s > 0.f ? fmaf(s, byz - by, x) : 0.f; }
+__device__ __forceinline__ double crossed(double x, double s, float by, float byz) { return s > 0.0 ? x + s * (double)(byz - by) : 0.0; }
 
 __device__ __forceinline__ void merge(Sum& a, const Sum& b) {
     const float E = fmaxf(a.E, b.E);
@@ -212,7 +213,7 @@ __device__ __forceinline__ void add_under(SumRef& a, const float (&h)[N], const 
     for (int i = 0; i < N; ++i) {
         const float t = exponent<PARTS>(h[i], a.E, c), tz = exponent<PARTS>(z[i], a.Ez, c);
         e[i] = exp2_hw(t);
-        x[i] = e[i] * exponent_diff(t, tz);
+        x[i] = mul_or_zero(e[i], t - tz);
         ez[i] = exp2_hw(tz);
     }
     a.s += tree_sum(e);
@@ -235,8 +236,7 @@ template <> struct Total<SumRef> {
 // NaN only by a logit that is, and so is whatever depends on it: 100 rows of NaN of V = 128256, a diverged model's, 23 ms swept again, 20 us so.
 __device__ __forceinline__ bool is_far(float E) { return !(E > 256.f - kFar && E < kFar); }
 __device__ __forceinline__ bool is_far(const Total<Sum>& a) { return a.s == a.s && is_far(a.E); }
-// (Nor do they where the reference alone masks a token whose term is 0: 0 times inf.)
-__device__ __forceinline__ bool is_far(const Total<SumRef>& a) { return a.s == a.s && (is_far(a.E) || (a.sz == a.sz && (is_far(a.Ez) || a.x != a.x))); }
+__device__ __forceinline__ bool is_far(const Total<SumRef>& a) { return a.s == a.s && (is_far(a.E) || (a.sz == a.sz && is_far(a.Ez))); }
 
 __device__ __forceinline__ double wave_sum_f64(double x) { return wave_last_f64(wave_incl_scan_f64(x)); }
 __device__ __forceinline__ double moved(double s, float from, float to) { return ldexp(s, (int)(from - to)); }
@@ -586,7 +586,6 @@ __device__ __forceinline__ void divergence(const Rows& a, bool far, const Total<
         mean = (x + (reference<PARTS>(a, s.E) - reference<PARTS>(a, s.Ez))) * kLn2;
         kl = (x - sums) * kLn2;
     }
-    if (sums != sums) mean = sums;  // NaN in the reference, which exponent_diff has bounded
     if (kl < 0.0) kl = 0.0;  // by rounding only
 }
 

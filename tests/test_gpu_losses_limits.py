@@ -5,7 +5,7 @@ import pytest
 import torch
 
 import loss_reference as R
-from test_gpu_losses import U_of, check_policy, check_preference, check_score, close, gen, losses, make  # noqa: F401
+from test_gpu_losses import U_of, check_policy, check_preference, check_score, close, gen, losses, make, ragged_mask  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -219,3 +219,51 @@ def test_what_a_mask_keeps_decides_about_the_caches_only(losses, B, T, V, kept):
     grad = losses.token_logprobs_grad(x, y, scored["stats"], w, mask=mask)
     # both round w (1[v = y] - p) to bf16 once, from weights that differ by a few steps of fp32
     assert ((out["grad_logits"].float() - grad.float()).abs() <= 2.0 ** -7 * grad.float().abs() + 1e-30).all()
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("low", ["-inf", "lowest"])
+@pytest.mark.parametrize("rows", [(1, 90, 50257), (1, 300, 3001)])
+def test_tokens_of_no_probability_that_the_reference_masks(losses, rows, low, dtype):
+    """Padding that the policy only holds far down and the reference masks: nothing of it counts, and no row is swept again for it."""
+    inp, g = make(*rows, dtype, ref=True)
+    x, z, y = inp["logits"], inp["ref_logits"], inp["tokens"]
+    old, adv = torch.zeros(y.shape, device="cuda") - 9, torch.randn(y.shape, generator=g, device="cuda")
+
+    def time():
+        best = math.inf
+        for _ in range(5):
+            start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            start.record()
+            for _ in range(5):
+                losses.policy_loss(x, y, old, adv, ref_logits=z, kl_coef=0.1)
+            end.record()
+            end.synchronize()
+            best = min(best, start.elapsed_time(end))
+        return best
+
+    plain = time()
+    x[..., :64] = -2000.0
+    z[..., :64] = -math.inf if low == "-inf" else torch.finfo(z.dtype).min
+    y.clamp_(min=64)
+    check_policy(losses, inp, g, kl="full")
+    check_policy(losses, inp, g, kl="full", mask=ragged_mask(*rows[:2], g, "lengths"), reduction="sum", scale=2.0 ** 16)
+    assert time() <= 5 * plain
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("rows", ROWS)
+def test_a_token_that_the_reference_alone_has_at_the_lowest_value(losses, rows, dtype):
+    """A KL as large as that value, or beyond fp32: no finite loss of ordinary size comes of it.  Other rows keep theirs."""
+    inp, g = make(*rows, dtype, ref=True)
+    x, z, y = inp["logits"], inp["ref_logits"], inp["tokens"]
+    old, adv = torch.zeros(y.shape, device="cuda") - 9, torch.randn(y.shape, generator=g, device="cuda")
+    want = losses.policy_loss(x, y, old, adv, ref_logits=z, kl_coef=0.1)
+    x7 = x[0, 1, 7].clone()
+    z[0, 1, 7] = torch.finfo(z.dtype).min
+    got = losses.policy_loss(x, y, old, adv, ref_logits=z, kl_coef=0.1)
+    assert x[0, 1, 7] == x7 and got["kl"][0, 1] > 1e30 and got["loss"] > 1e24
+    others = torch.ones(y.shape, dtype=torch.bool, device="cuda")
+    others[0, 1] = False
+    assert torch.equal(got["kl"][others], want["kl"][others]) and torch.equal(got["grad_logits"][others], want["grad_logits"][others])
+    assert torch.equal(got["logprobs"], want["logprobs"])
