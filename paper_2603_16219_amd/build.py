@@ -11,12 +11,12 @@ _ROOT = os.path.dirname(_PKG)
 SOURCES = [os.path.join(_PKG, "csrc", n) for n in ("specsteer.hip", "split.hip")]
 INCLUDE = os.path.join(_ROOT, "include")
 LIBRARY = os.path.join(_PKG, "libspecsteer.so")
-LOSS_SOURCES = [os.path.join(_PKG, "csrc", "loss", "loss.hip")]
+LOSS_SOURCES = [os.path.join(_PKG, "csrc", "loss", n) for n in ("loss.hip", "alternatives.hip")]
 LOSS_LIBRARY = os.path.join(_PKG, "libspecsteer_loss.so")
 CALLS_SOURCES = [os.path.join(_PKG, "csrc", "calls.cpp"), os.path.join(_PKG, "csrc", "calls_common.hpp"), os.path.join(_PKG, "csrc", "unbound.h"),
                  os.path.join(INCLUDE, "specsteer.h")]
 LOSS_CALLS_SOURCES = [os.path.join(_PKG, "csrc", "loss", "loss_calls.cpp"), os.path.join(_PKG, "csrc", "calls_common.hpp"),
-                      os.path.join(INCLUDE, "specsteer_loss.h"), os.path.join(INCLUDE, "specsteer.h")]
+                      *(os.path.join(INCLUDE, n) for n in ("specsteer_alternatives.h", "specsteer_loss.h", "specsteer.h"))]
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950",

@@ -8,7 +8,7 @@
 
 #include <c10/core/impl/DeviceGuardImplInterface.h>
 
-#include "specsteer_loss.h"
+#include "specsteer_alternatives.h"
 
 namespace {
 
@@ -19,6 +19,9 @@ struct Library {
     decltype(&specsteer_token_logprobs_grad) token_logprobs_grad;
     decltype(&specsteer_policy_loss) policy_loss;
     decltype(&specsteer_preference_loss) preference_loss;
+    decltype(&specsteer_token_alternatives_workspace_bytes) alternatives_workspace_bytes;
+    decltype(&specsteer_token_alternatives) token_alternatives;
+    decltype(&specsteer_token_alternatives_grad) token_alternatives_grad;
 } lib;
 
 // The strides of [B, T, V] with the vocabulary contiguous and no row twice, 0 where a size makes one meaningless.
@@ -228,12 +231,74 @@ PyObject* preference_loss(PyObject*, PyObject* const* a, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-// use(workspace_bytes, token_logprobs, token_logprobs_grad, policy_loss, preference_loss, current_raw_stream): the library's functions by their
-// addresses, and what gives torch's current stream on a device
+// token_alternatives(logits, tokens, topk, mask, temperature, want_stats, workspace)
+PyObject* token_alternatives(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 7) Py_RETURN_NONE;
+    const at::Tensor* x = gpu_tensor(a[0]);
+    ss_loss_params p;
+    bool ok = true, want;
+    if (!x || !describe(*x, p) || !PyLong_CheckExact(a[2])) Py_RETURN_NONE;
+    const at::Tensor *y = rows_of(a[1], at::kInt, *x, p, true, ok), *mask = mask_of(a[3], *x, p, ok);
+    int over = 0;
+    const long topk = PyLong_AsLongAndOverflow(a[2], &over);
+    if (!ok || over || topk < 0 || topk > SS_MAX_TOPK || !number(a[4], p.temperature) || !truth(a[5], want)) Py_RETURN_NONE;
+    at::Tensor ws;
+    if (a[6] == Py_None) {
+        const size_t need = lib.alternatives_workspace_bytes(&p, (int32_t)topk);
+        ws = make(*x, {(int64_t)(need > 256 ? need : 256)}, at::kByte);
+    } else if (!workspace_of(a[6], *x, p, ws)) {
+        Py_RETURN_NONE;
+    }
+    const at::Tensor lp = y ? make(*x, {p.batch, p.length}, at::kFloat) : at::Tensor(), entropy = make(*x, {p.batch, p.length}, at::kFloat);
+    const at::Tensor top = topk ? make(*x, {p.batch, p.length, topk}, at::kInt) : at::Tensor();
+    const at::Tensor top_lp = topk ? make(*x, {p.batch, p.length, topk}, at::kFloat) : at::Tensor();
+    const at::Tensor stats = want ? make(*x, {p.batch, p.length, 2}, at::kFloat) : at::Tensor();
+    void* stream;
+    if (!stream_of(*x, stream)) return nullptr;
+    const ss_status rc = unlocked([&] {
+        return lib.token_alternatives(data(x), data_as<int32_t>(y), data_as<uint8_t>(mask), &p, (int32_t)topk, ptr<float>(lp), ptr<float>(entropy),
+                                      ptr<int32_t>(top), ptr<float>(top_lp), ptr<float>(stats), ws.data_ptr(), ws.nbytes(), stream);
+    });
+    if (rc != SS_OK) return PyLong_FromLong(rc);
+    return result({{"logprobs", &lp}, {"entropy", &entropy}, {"top_tokens", &top}, {"top_logprobs", &top_lp}, {"stats", &stats}});
+    END_HANDLE_TH_ERRORS
+}
+
+// token_alternatives_grad(logits, tokens, stats, entropy, grad_logprobs, grad_entropy, mask, temperature, grad_scale, grad_logits)
+PyObject* token_alternatives_grad(PyObject*, PyObject* const* a, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (n != 10) Py_RETURN_NONE;
+    const at::Tensor* x = gpu_tensor(a[0]);
+    ss_loss_params p;
+    bool ok = true;
+    if (!x || !describe(*x, p)) Py_RETURN_NONE;
+    const at::Tensor *y = rows_of(a[1], at::kInt, *x, p, true, ok), *stats = ready(a[2], at::kFloat, *x), *entropy = rows_of(a[3], at::kFloat, *x, p, true, ok);
+    const at::Tensor *g = rows_of(a[4], at::kFloat, *x, p, true, ok), *k = rows_of(a[5], at::kFloat, *x, p, true, ok), *mask = mask_of(a[6], *x, p, ok);
+    if (!ok || !stats || stats->dim() != 3 || stats->size(0) != p.batch || stats->size(1) != p.length || stats->size(2) != 2) Py_RETURN_NONE;
+    if ((!g && !k) || (g && !y) || (k && !entropy)) Py_RETURN_NONE;
+    at::Tensor grad;
+    if (!number(a[7], p.temperature) || !number(a[8], p.grad_scale) || !gradient_of(a[9], true, *x, nullptr, p, grad)) Py_RETURN_NONE;
+    void* stream;
+    if (!stream_of(*x, stream)) return nullptr;
+    const ss_status rc = unlocked([&] {
+        return lib.token_alternatives_grad(data(x), data_as<int32_t>(y), data_as<uint8_t>(mask), data_as<float>(stats), data_as<float>(entropy),
+                                           data_as<float>(g), data_as<float>(k), &p, grad.data_ptr(), stream);
+    });
+    if (rc != SS_OK) return PyLong_FromLong(rc);
+    written(a[9], grad);
+    if (a[9] != Py_None) return Py_NewRef(a[9]);
+    return THPVariable_Wrap(grad);
+    END_HANDLE_TH_ERRORS
+}
+
+// use(workspace_bytes, token_logprobs, token_logprobs_grad, policy_loss, preference_loss, alternatives_workspace_bytes, token_alternatives,
+//     token_alternatives_grad, current_raw_stream): the library's functions by their addresses, and what gives torch's current stream on a device
 PyObject* use(PyObject*, PyObject* const* a, Py_ssize_t n) {
-    if (n != 6) return PyErr_Format(PyExc_TypeError, "six arguments");
-    void* f[5];
-    for (int i = 0; i < 5; ++i) {
+    constexpr int kFunctions = 8;
+    if (n != kFunctions + 1) return PyErr_Format(PyExc_TypeError, "nine arguments");
+    void* f[kFunctions];
+    for (int i = 0; i < kFunctions; ++i) {
         f[i] = PyLong_AsVoidPtr(a[i]);
         if (PyErr_Occurred()) return nullptr;
     }
@@ -242,8 +307,11 @@ PyObject* use(PyObject*, PyObject* const* a, Py_ssize_t n) {
     lib.token_logprobs_grad = reinterpret_cast<decltype(lib.token_logprobs_grad)>(f[2]);
     lib.policy_loss = reinterpret_cast<decltype(lib.policy_loss)>(f[3]);
     lib.preference_loss = reinterpret_cast<decltype(lib.preference_loss)>(f[4]);
-    Py_INCREF(a[5]);
-    Py_XSETREF(current_raw_stream, a[5]);
+    lib.alternatives_workspace_bytes = reinterpret_cast<decltype(lib.alternatives_workspace_bytes)>(f[5]);
+    lib.token_alternatives = reinterpret_cast<decltype(lib.token_alternatives)>(f[6]);
+    lib.token_alternatives_grad = reinterpret_cast<decltype(lib.token_alternatives_grad)>(f[7]);
+    Py_INCREF(a[kFunctions]);
+    Py_XSETREF(current_raw_stream, a[kFunctions]);
     Py_RETURN_NONE;
 }
 
@@ -253,6 +321,8 @@ PyMethodDef methods[] = {
     {"token_logprobs_grad", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(token_logprobs_grad)), METH_FASTCALL, nullptr},
     {"policy_loss", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(policy_loss)), METH_FASTCALL, nullptr},
     {"preference_loss", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(preference_loss)), METH_FASTCALL, nullptr},
+    {"token_alternatives", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(token_alternatives)), METH_FASTCALL, nullptr},
+    {"token_alternatives_grad", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(token_alternatives_grad)), METH_FASTCALL, nullptr},
     {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_loss_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

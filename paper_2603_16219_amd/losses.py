@@ -1,4 +1,5 @@
-"""Binding of the losses over full-vocabulary logits (include/specsteer_loss.h): argument marshalling only.
+"""Binding of the losses over full-vocabulary logits (include/specsteer_loss.h), and of their rows' entropies and likeliest tokens
+(include/specsteer_alternatives.h): argument marshalling only.
 
 As in ``binding``, arguments that need nothing done to them go to native code (csrc/loss/loss_calls.cpp), others through ctypes here.
 
@@ -76,14 +77,19 @@ def library() -> ctypes.CDLL:
         lib.specsteer_token_logprobs_grad.argtypes = [p] * 5 + [params] + [p] * 2
         lib.specsteer_policy_loss.argtypes = [p] * 7 + [params, ctypes.POINTER(SSPolicyParams)] + [p] * 5 + [ctypes.c_size_t, p]
         lib.specsteer_preference_loss.argtypes = [p] * 4 + [params, ctypes.POINTER(SSPreferenceParams)] + [p] * 6 + [ctypes.c_size_t, p]
-        for name in ("token_logprobs", "token_logprobs_grad", "policy_loss", "preference_loss"):
+        lib.specsteer_token_alternatives_workspace_bytes.restype = ctypes.c_size_t
+        lib.specsteer_token_alternatives_workspace_bytes.argtypes = [params, ctypes.c_int32]
+        lib.specsteer_token_alternatives.argtypes = [p] * 3 + [params, ctypes.c_int32] + [p] * 6 + [ctypes.c_size_t, p]
+        lib.specsteer_token_alternatives_grad.argtypes = [p] * 7 + [params] + [p] * 2
+        for name in ("token_logprobs", "token_logprobs_grad", "policy_loss", "preference_loss", "token_alternatives", "token_alternatives_grad"):
             getattr(lib, "specsteer_" + name).restype = ctypes.c_int
         lib.specsteer_loss_status_string.restype = ctypes.c_char_p
         lib.specsteer_loss_status_string.argtypes = [ctypes.c_int]
         _lib = lib
         _calls = load_wrappers("_loss_calls", _build.loss_calls_path, _build.build_loss_calls, lambda: (
             lib.specsteer_loss_workspace_bytes, lib.specsteer_token_logprobs, lib.specsteer_token_logprobs_grad, lib.specsteer_policy_loss,
-            lib.specsteer_preference_loss))
+            lib.specsteer_preference_loss, lib.specsteer_token_alternatives_workspace_bytes, lib.specsteer_token_alternatives,
+            lib.specsteer_token_alternatives_grad))
     return _lib
 
 
@@ -196,9 +202,9 @@ def _written(grad_logits: Optional[torch.Tensor]) -> None:
         torch.autograd.graph.increment_version(grad_logits)
 
 
-def _scratch(workspace: Optional[torch.Tensor], params: SSLossParams, device: torch.device) -> torch.Tensor:
+def _scratch(workspace: Optional[torch.Tensor], params: SSLossParams, device: torch.device, need=None) -> torch.Tensor:
     if workspace is None:
-        return torch.empty(max(workspace_bytes(params), 256), dtype=torch.uint8, device=device)
+        return torch.empty(max(workspace_bytes(params) if need is None else need, 256), dtype=torch.uint8, device=device)
     if not workspace.is_contiguous() or workspace.device != device:
         raise ValueError("workspace must be a contiguous tensor on the logits' device")
     return workspace
@@ -245,6 +251,73 @@ def token_logprobs_grad(logits: torch.Tensor, tokens: torch.Tensor, stats: torch
     tokens, stats = _ready_tokens(tokens, dev), stats.contiguous()
     _call(library().specsteer_token_logprobs_grad, dev, _ptr(logits), _ptr(tokens), _ptr(mask), _ptr(stats), _ptr(grad_logprobs),
           ctypes.byref(params), _ptr(grad_logits))
+    _written(grad_logits)
+    return grad_logits
+
+
+MAX_TOPK = 64
+
+
+def alternatives_workspace_bytes(params: SSLossParams, topk: int) -> int:
+    return int(library().specsteer_token_alternatives_workspace_bytes(ctypes.byref(params), topk))
+
+
+def token_alternatives(logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, *, topk: int = 0, mask: Optional[torch.Tensor] = None,
+                       temperature: float = 1.0, want_stats: bool = False, workspace: Optional[torch.Tensor] = None) -> dict:
+    """specsteer_token_alternatives on logits [B, T, V] and, if given, tokens [B, T]: {"logprobs" [B, T] float32 or None without tokens,
+    "entropy" [B, T] float32, "top_tokens" [B, T, topk] int32 and "top_logprobs" [B, T, topk] float32 or None for topk 0, "stats" [B, T, 2]
+    or None}.  Alternatives come by decreasing logit, ties by increasing id; -1 and -inf where there is none."""
+    out = _native("token_alternatives", logits, tokens, topk, mask, temperature, want_stats, workspace)
+    if out is not None:
+        return out
+    if isinstance(topk, bool) or not isinstance(topk, int) or not 0 <= topk <= MAX_TOPK:
+        raise ValueError(f"topk must be an integer in 0..{MAX_TOPK}, got {topk!r}")
+    if logits.dim() != 3:
+        raise ValueError("logits must be [B, T, V]")
+    dev, rows = logits.device, logits.shape[:2]
+    like = torch.empty(rows, dtype=torch.int32, device="meta") if tokens is None else tokens
+    params = _make_params(logits, like, temperature)
+    mask = _ready_mask(mask, like, dev)
+    tokens = None if tokens is None else _ready_tokens(tokens, dev)
+    workspace = _scratch(workspace, params, dev, alternatives_workspace_bytes(params, topk))
+    logprobs = None if tokens is None else torch.empty(rows, dtype=torch.float32, device=dev)
+    entropy = torch.empty(rows, dtype=torch.float32, device=dev)
+    top_tokens = torch.empty(*rows, topk, dtype=torch.int32, device=dev) if topk else None
+    top_logprobs = torch.empty(*rows, topk, dtype=torch.float32, device=dev) if topk else None
+    stats = torch.empty(*rows, 2, dtype=torch.float32, device=dev) if want_stats else None
+    _call(library().specsteer_token_alternatives, dev, _ptr(logits), _ptr(tokens), _ptr(mask), ctypes.byref(params), topk, _ptr(logprobs), _ptr(entropy),
+          _ptr(top_tokens), _ptr(top_logprobs), _ptr(stats), _ptr(workspace), _bytes(workspace))
+    return {"logprobs": logprobs, "entropy": entropy, "top_tokens": top_tokens, "top_logprobs": top_logprobs, "stats": stats}
+
+
+def token_alternatives_grad(logits: torch.Tensor, tokens: Optional[torch.Tensor], stats: torch.Tensor, entropy: Optional[torch.Tensor],
+                            grad_logprobs: Optional[torch.Tensor], grad_entropy: Optional[torch.Tensor], *, mask: Optional[torch.Tensor] = None,
+                            temperature: float = 1.0, grad_scale: float = 1.0, grad_logits: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """specsteer_token_alternatives_grad: the gradient [B, T, V] with respect to the logits, in their type, of a loss whose gradients with
+    respect to their log-probs and entropies are grad_logprobs and grad_entropy [B, T] (None: 0, not both).  stats and entropy are what
+    token_alternatives(..., want_stats=True) returned.  It goes to `grad_logits` if given, which may be the logits."""
+    out = _native("token_alternatives_grad", logits, tokens, stats, entropy, grad_logprobs, grad_entropy, mask, temperature, grad_scale, grad_logits)
+    if out is not None:
+        return out
+    if grad_logprobs is None and grad_entropy is None:
+        raise ValueError("give grad_logprobs, grad_entropy or both")
+    if (grad_logprobs is not None and tokens is None) or (grad_entropy is not None and entropy is None):
+        raise ValueError("grad_logprobs needs the tokens, grad_entropy the entropy")
+    if logits.dim() != 3:
+        raise ValueError("logits must be [B, T, V]")
+    grad_logits = _gradient(logits, True, grad_logits)
+    dev, rows = logits.device, logits.shape[:2]
+    like = torch.empty(rows, dtype=torch.int32, device="meta") if tokens is None else tokens
+    params = _make_params(logits, like, temperature, grad_scale, grad_logits)
+    if tuple(stats.shape) != (*rows, 2) or stats.dtype is not torch.float32 or stats.device != dev:
+        raise ValueError("stats must be what token_alternatives(..., want_stats=True) returned for these logits")
+    mask = _ready_mask(mask, like, dev)
+    grad_logprobs = _ready_rows(grad_logprobs, "grad_logprobs", like, dev)
+    grad_entropy = _ready_rows(grad_entropy, "grad_entropy", like, dev)
+    entropy = _ready_rows(entropy, "entropy", like, dev)
+    tokens, stats = None if tokens is None else _ready_tokens(tokens, dev), stats.contiguous()
+    _call(library().specsteer_token_alternatives_grad, dev, _ptr(logits), _ptr(tokens), _ptr(mask), _ptr(stats), _ptr(entropy), _ptr(grad_logprobs),
+          _ptr(grad_entropy), ctypes.byref(params), _ptr(grad_logits))
     _written(grad_logits)
     return grad_logits
 
