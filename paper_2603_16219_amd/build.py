@@ -13,10 +13,14 @@ INCLUDE = os.path.join(_ROOT, "include")
 LIBRARY = os.path.join(_PKG, "libspecsteer.so")
 LOSS_SOURCES = [os.path.join(_PKG, "csrc", "loss", n) for n in ("loss.hip", "alternatives.hip")]
 LOSS_LIBRARY = os.path.join(_PKG, "libspecsteer_loss.so")
+TREE_SOURCES = [os.path.join(_PKG, "csrc", "tree", n) for n in ("attention.hip", "verify.hip", "commit.hip")]
+TREE_LIBRARY = os.path.join(_PKG, "libspecsteer_tree.so")
 CALLS_SOURCES = [os.path.join(_PKG, "csrc", "calls.cpp"), os.path.join(_PKG, "csrc", "calls_common.hpp"), os.path.join(_PKG, "csrc", "unbound.h"),
                  os.path.join(INCLUDE, "specsteer.h")]
 LOSS_CALLS_SOURCES = [os.path.join(_PKG, "csrc", "loss", "loss_calls.cpp"), os.path.join(_PKG, "csrc", "calls_common.hpp"),
                       *(os.path.join(INCLUDE, n) for n in ("specsteer_alternatives.h", "specsteer_loss.h", "specsteer.h"))]
+TREE_CALLS_SOURCES = [os.path.join(_PKG, "csrc", "tree", "tree_calls.cpp"), os.path.join(_PKG, "csrc", "calls_common.hpp"),
+                      *(os.path.join(INCLUDE, n) for n in ("specsteer_tree.h", "specsteer.h"))]
 
 HIPCC_FLAGS = [
     "-O3", "-std=c++17", "--offload-arch=gfx950",
@@ -42,8 +46,10 @@ def _run(cmd: list, verbose: bool) -> None:
 def build(verbose: bool = False) -> str:
     build_library(verbose)
     build_loss_library(verbose)
+    build_tree_library(verbose)
     build_calls(verbose)
     build_loss_calls(verbose)
+    build_tree_calls(verbose)
     return LIBRARY
 
 
@@ -60,6 +66,13 @@ def build_loss_library(verbose: bool = False) -> str:
     return LOSS_LIBRARY
 
 
+def build_tree_library(verbose: bool = False) -> str:
+    """Trees of drafts, a library of their own too."""
+    hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
+    _run([hipcc, *HIPCC_FLAGS, "-I", INCLUDE, "-o", TREE_LIBRARY, *TREE_SOURCES], verbose)
+    return TREE_LIBRARY
+
+
 def calls_path() -> str:
     """Where the native wrappers for this torch and these sources lie: what they are compiled against is in the name, so that one
     built for another torch, whose tensors may be laid out differently, or from other sources is never loaded."""
@@ -69,6 +82,11 @@ def calls_path() -> str:
 def loss_calls_path() -> str:
     """The same for those of the losses."""
     return _calls_path("_loss_calls", LOSS_CALLS_SOURCES)
+
+
+def tree_calls_path() -> str:
+    """The same for those of trees."""
+    return _calls_path("_tree_calls", TREE_CALLS_SOURCES)
 
 
 def _calls_path(name: str, sources: list) -> str:
@@ -87,6 +105,10 @@ def build_calls(verbose: bool = False) -> str:
 
 def build_loss_calls(verbose: bool = False) -> str:
     return _build_calls(loss_calls_path(), LOSS_CALLS_SOURCES[0], verbose)
+
+
+def build_tree_calls(verbose: bool = False) -> str:
+    return _build_calls(tree_calls_path(), TREE_CALLS_SOURCES[0], verbose)
 
 
 def _build_calls(path: str, source: str, verbose: bool) -> str:
