@@ -1,79 +1,559 @@
-// Attention of a tree's rows over a paged cache and their ancestors, for MI355X (gfx950); include/specsteer_tree.h says what it computes.
+// Attention of a tree's rows over a paged cache and their ancestors, for MI355X (gfx950); include/specsteer_tree.h says what it computes,
+// tree_schedule.h how the work is dealt out.
 //
-// A wave a row and query head: it goes over the keys with a running maximum m and sum l of the weights 2^(s - m), s = scale log2(e) q.k, and
-// holds the weighted sum of the values, two elements a lane (one of head_dim 64).
+// For a block of columns (a tree row and a query head of the group each) and a tile of keys
+//     S^T = K Q^T,    P^T = 2^(c S^T - m),    l += sum P,    O^T += V^T P^T,    c = scale log2(e),
+// all products by 32x32x16 matrix instructions.  With columns along the lanes, a column's maximum and sum take one exchange between the wave's
+// halves, and the lanes that hold P^T's elements are those that have to give them to the second product: rows 8 a + 4 h + i of S^T lie in
+// half h, so that the keys of V^T are read in that order.  The reference m rises only when a score passes it by 2^kSlack, and O is rescaled then.
+//
+// Keys and values go from memory to LDS without registers, a tile ahead; in pieces of 16 bytes whose place in the row depends on the row, which
+// spreads both the keys' reads and the values' transposed ones over the banks.
+//
+// Bytes: the cache once a call for up to MB columns, whose products take 4 D MB flop for 4 D bytes a key.
+#include <type_traits>
+
 #include "tree_common.h"
+#include "tree_schedule.h"
 
 namespace {
+
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef float f32v4 __attribute__((ext_vector_type(4)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32v4 __attribute__((ext_vector_type(4)));
+
+template <int DT> struct Half;
+template <> struct Half<SS_BF16> {
+    typedef __bf16 T;
+    typedef __bf16 x8 __attribute__((ext_vector_type(8)));
+    // a weight is at most 2^kSlack
+    static constexpr float kSlack = 8.f, kLift = 0.f;
+    static constexpr unsigned kExponent = 0x7F80u;
+};
+template <> struct Half<SS_TREE_F16> {
+    typedef _Float16 T;
+    typedef _Float16 x8 __attribute__((ext_vector_type(8)));
+    // weights are 2^10 times as large, so that those 2^-24 below the largest are normal numbers still, and at most 2^15
+    static constexpr float kSlack = 5.f, kLift = 10.f;
+    static constexpr unsigned kExponent = 0x7C00u;
+};
+template <int DT>
+__device__ __forceinline__ f32x16 mfma(typename Half<DT>::x8 a, typename Half<DT>::x8 b, f32x16 c) {
+    if constexpr (DT == SS_BF16) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+
+// 16 bytes a lane from memory to LDS, lane i's to `to` + 16 i.  By the builtin the compiler waits for all such loads before the next read of LDS, those a
+// tile ahead among them; here the wait stands before the barrier that hands the tile over.  No register is written.  m0, which nothing else in these
+// kernels uses, is read one wait state behind its write.
+__device__ __forceinline__ void load_lds(unsigned to, const char* from) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(to), "v"(from) : "memory");
+}
+__device__ __forceinline__ unsigned lds_offset(const void* p) { return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) char*)p; }
 
 struct AttnArgs {
     const char *q, *k, *v, *kc, *vc;
     const int32_t *table, *cache_len, *parents, *tree_len;
     char* out;
+    float* part_o;   // [2 * shares][columns][D]: sums of values of parts
+    float2* part_ml; // [2 * shares][columns]: their references and sums of weights
     Strides3 qs, ks, os, cs;
     long ts;
-    int B, N, heads, group, pages, page_size, width;
-    float scale;  // times log2(e)
+    int B, N, group, kv_heads, pages, page_size, width, shares;
+    float scale;  // |scale| log2(e)
+    int negative; // scale < 0
 };
 
-template <int DT>
-__device__ __forceinline__ float ld_half(const char* p) {
-    if (DT == SS_BF16) return __uint_as_float((unsigned)*reinterpret_cast<const unsigned short*>(p) << 16);
-    return (float)*reinterpret_cast<const _Float16*>(p);
-}
-template <int DT>
-__device__ __forceinline__ void st_half(char* p, float x) {
-    if (DT == SS_BF16) *reinterpret_cast<unsigned short*>(p) = __builtin_bit_cast(unsigned short, (__bf16)x);
-    else *reinterpret_cast<_Float16*>(p) = (_Float16)x;
+struct Sequence {
+    int L, N;
+    bool bad;
+};
+__device__ __forceinline__ Sequence sequence(const AttnArgs& a, int b) {
+    Sequence s;
+    s.L = a.cache_len[b];
+    s.N = a.tree_len ? a.tree_len[b] : a.N;
+    s.bad = s.L < 0 || s.L > (long)a.width * a.page_size || s.N < 0 || s.N > a.N;
+    return s;
 }
 
-template <int DT, int D>
-__global__ __launch_bounds__(kWave) void attention_kernel(const AttnArgs a) {
-    constexpr int E = D / kWave;
-    const int lane = threadIdx.x, row = blockIdx.x, head = blockIdx.y, b = blockIdx.z, kv = head / a.group;
-    const int L = a.cache_len[b], N = a.tree_len ? a.tree_len[b] : a.N;
-    char* const out = a.out + 2 * (b * a.os.a + row * a.os.b + head * a.os.c + lane * E);
-    bool bad = L < 0 || L > (long)a.width * a.page_size || N < 0 || N > a.N;
-    if (!bad && a.parents)
-        for (int i = lane; i < N; i += kWave) {
-            const int p = a.parents[(long)b * a.N + i];
-            bad = bad || p < -1 || p >= i;
-        }
-    if (!bad)
-        for (int i = lane; i < (L + a.page_size - 1) / a.page_size; i += kWave) {
-            const int p = a.table[b * a.ts + i];
-            bad = bad || p < 0 || p >= a.pages;
-        }
-    const bool mine = row <= N;
-    if (__ballot(bad) || !mine) {
-        for (int e = 0; e < E; ++e) st_half<DT>(out + 2 * e, __ballot(bad) ? __builtin_nanf("") : 0.f);
-        return;
-    }
-    float q[E], o[E], m = -__builtin_huge_valf(), l = 0.f;
-    for (int e = 0; e < E; ++e) {
-        q[e] = ld_half<DT>(a.q + 2 * (b * a.qs.a + row * a.qs.b + head * a.qs.c + lane * E + e));
-        o[e] = 0.f;
-    }
-    const auto take = [&](const char* k, const char* v) {
-        float s = 0.f;
-        for (int e = 0; e < E; ++e) s = fmaf(q[e], ld_half<DT>(k + 2 * e), s);
-        s = wave_sum_f32(s) * a.scale;
-        const float top = fmaxf(m, s), by = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top), p = __builtin_amdgcn_exp2f(s - top);
-        l = fmaf(l, by, p);
-        for (int e = 0; e < E; ++e) o[e] = fmaf(o[e], by, p * ld_half<DT>(v + 2 * e));
-        m = top;
+// Where a unit lies: its sequence, and the units before that.
+struct Place {
+    int b;
+    long before, total;
+};
+// The sums over all sequences, by a workgroup; the unit asked for follows from them.
+template <int NT, typename F>
+__device__ __forceinline__ Place find_place(const AttnArgs& a, const TreeTiles& tiles, long* sh, F unit) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    constexpr int kWaves = NT / kWave;
+    const auto of = [&](int b) {
+        if (b >= a.B) return 0l;
+        const Sequence s = sequence(a, b);
+        return tree_items(tiles, s.L, s.N, s.bad, a.N).units(a.kv_heads);
     };
-    for (int t = 0; t < L; ++t) {
-        const long at = 2 * (a.table[b * a.ts + t / a.page_size] * a.cs.a + t % a.page_size * a.cs.b + kv * a.cs.c + lane * E);
-        take(a.kc + at, a.vc + at);
+    const long first = of(tid);
+    long sum = first;
+    for (int b = tid + NT; b < a.B; b += NT) sum += of(b);
+    for (int d = 1; d < kWave; d <<= 1) sum += __shfl_xor(sum, d, kWave);
+    __syncthreads();
+    if (lane == 0) sh[wave] = sum;
+    __syncthreads();
+    Place p;
+    p.total = 0;
+    for (int w = 0; w < kWaves; ++w) p.total += sh[w];
+    p.b = 0;
+    p.before = 0;
+    const long u = unit(p.total);
+    if (u < 0 || u >= p.total) return p;
+    long before = 0;
+    for (int b0 = 0; b0 < a.B; b0 += NT) {
+        const long mine = b0 == 0 ? first : of(b0 + tid);
+        long incl = mine;
+        for (int d = 1; d < kWave; d <<= 1) {
+            const long o = __shfl_up(incl, d, kWave);
+            if (lane >= d) incl += o;
+        }
+        __syncthreads();
+        if (lane == 63) sh[wave] = incl;
+        __syncthreads();
+        long start = before;
+        for (int w = 0; w < kWaves; ++w) {
+            if (w < wave) start += sh[w];
+            before += sh[w];
+        }
+        if (u >= start + incl - mine && u < start + incl) {
+            sh[kWaves] = b0 + tid;
+            sh[kWaves + 1] = start + incl - mine;
+        }
+        if (u < before) break;
     }
-    for (int j = row;;) {
-        const long at = 2 * (b * a.ks.a + j * a.ks.b + kv * a.ks.c + lane * E);
-        take(a.k + at, a.v + at);
-        if (j == 0) break;
-        j = a.parents ? a.parents[(long)b * a.N + j - 1] + 1 : j - 1;
+    __syncthreads();
+    p.b = (int)sh[kWaves];
+    p.before = sh[kWaves + 1];
+    return p;
+}
+
+template <int D_, int WM_, int WK_>
+struct Shape {
+    static constexpr int D = D_, WM = WM_, WK = WK_;
+    static constexpr int kWaves = WM * WK, kThreads = kWaves * kWave, kColumns = 32 * WM;
+    static constexpr int kSub = 128 / D;             // 32 keys each, of a wave's in a tile
+    static constexpr int kTile = 32 * WK * kSub;     // keys
+    static constexpr int kLanes = D / 8;             // of 16 bytes each, a row
+    static constexpr int kRows = kWave / kLanes;     // rows a load instruction
+    static constexpr int kLoads = kTile / (kRows * kWaves);  // of a wave for the keys of a tile, and for its values
+    static constexpr int kRowBytes = 2 * D, kTileBytes = kTile * kRowBytes, kStage = 2 * kTileBytes;
+    static constexpr int kPad = D + 4;               // floats of a column that waves hand over
+    static constexpr int kHand = (WK - 1) * kColumns * kPad * 4;
+    static constexpr int kBuffers = 2 * kStage > kHand ? 2 * kStage : kHand;
+};
+
+// By how much the 16-byte pieces of a row are turned round: 4 rows next to each other that a transposed read takes, and 16 whose same piece is
+// read at once, lie in different banks.
+template <int D>
+__device__ __forceinline__ int turn(int row) {
+    if constexpr (D == 128) return ((row & 3) << 2) | ((row >> 2) & 3);
+    else return (((row >> 1) & 1) << 2) | ((row >> 2) & 3);
+}
+
+template <int DT, typename C>
+__global__ __launch_bounds__(C::kThreads) void attention_kernel(const AttnArgs a) {
+    using H = Half<DT>;
+    using x8 = typename H::x8;
+    constexpr int D = C::D, kBlocks = D / 32, kSteps = D / 16;
+    __shared__ __attribute__((aligned(1024))) char lds[C::kBuffers];
+    __shared__ float2 hand_ml[C::WK][C::kColumns];
+    __shared__ unsigned short up[SS_MAX_K + 1];
+    __shared__ long sh[C::kWaves + 2];
+    __shared__ int sh_bad;
+    const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave % C::WM, wk = wave / C::WM;
+    const TreeTiles tiles{C::kTile, C::kColumns, a.group, a.kv_heads};
+
+    if (a.tree_len) {  // rows that belong to nobody are 0
+        const int pieces = a.group * a.kv_heads * (D / 8);
+        for (long r = blockIdx.x; r < (long)a.B * (a.N + 1); r += gridDim.x) {
+            const int b = (int)(r / (a.N + 1)), row = (int)(r % (a.N + 1));
+            const Sequence s = sequence(a, b);
+            if (s.bad || row <= s.N) continue;
+            for (int i = tid; i < pieces; i += C::kThreads)
+                *reinterpret_cast<uint4*>(a.out + 2 * (b * a.os.a + row * a.os.b + (i / (D / 8)) * a.os.c) + 16 * (i % (D / 8))) = make_uint4(0, 0, 0, 0);
+        }
     }
-    for (int e = 0; e < E; ++e) st_half<DT>(out + 2 * e, o[e] / l);
+
+    long u = 0;
+    const Place place = find_place<C::kThreads>(a, tiles, sh, [&](long total) { return u = share_begin(total, shares_of(a.shares, total), blockIdx.x); });
+    if (u >= place.total) return;
+    const long u_end = share_begin(place.total, shares_of(a.shares, place.total), blockIdx.x + 1);
+    int b = place.b;
+    long rel = u - place.before;  // within the sequence
+    Sequence s = sequence(a, b);
+    TreeItems items = tree_items(tiles, s.L, s.N, s.bad, a.N);
+    bool first_item = true;
+    while (u < u_end) {
+        if (rel >= items.units(a.kv_heads)) {
+            ++b;
+            rel = 0;
+            s = sequence(a, b);
+            items = tree_items(tiles, s.L, s.N, s.bad, a.N);
+        }
+        const int nt = items.tiles();
+        const int item = (int)(rel / nt), t0 = (int)(rel - (long)item * nt), t1 = (int)min((long)nt, t0 + (u_end - u));
+        const int head = item / items.blocks, block = item - head * items.blocks;
+        // this lane's column
+        const int column = block * C::kColumns + wm * 32 + (lane & 31);
+        const int rows = (s.bad ? a.N : s.N) + 1, row = column / a.group, of_group = column - row * a.group;
+        const bool valid = row < rows;
+        const bool whole = t0 == 0 && t1 == nt;
+        bool bad = s.bad;
+
+        f32x16 o[kBlocks];
+        float m = -1e30f, l = 0.f;
+#pragma unroll
+        for (int i = 0; i < kBlocks; ++i) o[i] = f32x16{};
+        __syncthreads();  // the last item's hand-over is done with
+        if (tid == 0) sh_bad = 0;
+        if (!s.bad) {
+            x8 q[kSteps];
+            const char* const qp = a.q + 2 * (b * a.qs.a + min(row, s.N) * a.qs.b + (head * a.group + of_group) * a.qs.c) + 16 * half;
+#pragma unroll
+            for (int i = 0; i < kSteps; ++i) {
+                u32v4 w = *reinterpret_cast<const u32v4*>(qp + 32 * i);
+                if (a.negative) w ^= 0x80008000u;
+                q[i] = __builtin_bit_cast(x8, w);
+            }
+            if (t1 > items.cached && a.parents)
+                for (int i = tid; i < s.N; i += C::kThreads) {
+                    int p = a.parents[(long)b * a.N + i];
+                    if (p < -1 || p >= i) {
+                        bad = true;
+                        p = -1;
+                    }
+                    up[i + 1] = (unsigned short)(p + 1);
+                }
+
+            // The loads of a tile: this wave's are rows load_row(j).
+            const auto load_row = [&](int j) { return (wave * C::kLoads + j) * C::kRows + lane / C::kLanes; };
+            int page[C::kLoads];
+            const auto look_up = [&](int t) {
+                if (t < items.cached)
+#pragma unroll
+                    for (int j = 0; j < C::kLoads; ++j) page[j] = a.table[b * a.ts + min(t * C::kTile + load_row(j), s.L - 1) / a.page_size];
+            };
+            const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_offset(lds)) + wave * C::kLoads * 1024;
+            const auto load = [&](int t, int stage) {
+#pragma unroll
+                for (int j = 0; j < C::kLoads; ++j) {
+                    const int r = load_row(j), piece = (lane % C::kLanes) ^ turn<D>(r);
+                    const char *k, *v;
+                    if (t < items.cached) {
+                        const int at = min(t * C::kTile + r, s.L - 1);
+                        int p = page[j];
+                        if (p < 0 || p >= a.pages) {
+                            bad = true;
+                            p = 0;
+                        }
+                        const long off = 2 * (p * a.cs.a + at % a.page_size * a.cs.b + head * a.cs.c) + 16 * piece;
+                        k = a.kc + off;
+                        v = a.vc + off;
+                    } else {
+                        const int at = min((t - items.cached) * C::kTile + r, s.N);
+                        const long off = 2 * (b * a.ks.a + at * a.ks.b + head * a.ks.c) + 16 * piece;
+                        k = a.k + off;
+                        v = a.v + off;
+                    }
+                    load_lds(lds0 + stage * C::kStage + j * 1024, k);
+                    load_lds(lds0 + stage * C::kStage + j * 1024 + C::kTileBytes, v);
+                }
+            };
+
+            const auto products = [&](auto tree_rows, int t, const char* stage) {
+                constexpr bool own = decltype(tree_rows)::value;  // a tile of the block's own rows, not of the cache
+#pragma unroll
+                for (int sub = 0; sub < C::kSub; ++sub) {
+                    const int key0 = (wk * C::kSub + sub) * 32;  // of the tile
+                    const char* const kt = stage + key0 * C::kRowBytes;
+                    const char* const vt = kt + C::kTileBytes;
+                    const int base = own ? (t - items.cached) * C::kTile + key0 : t * C::kTile + key0;  // of the block's rows, of the cache
+                    const int limit = own ? s.N + 1 : s.L;
+                    if (base >= limit) continue;
+                    f32x16 sc = {};
+                    {
+                        const int r = lane & 31;
+                        const char* const kr = kt + r * C::kRowBytes;
+                        const int x = half ^ turn<D>(r);
+#pragma unroll
+                        for (int i = 0; i < kSteps; ++i) sc = mfma<DT>(*reinterpret_cast<const x8*>(kr + ((2 * i) ^ x) * 16), q[i], sc);
+                    }
+                    unsigned seen = ~0u;  // keys of these 32
+                    if (own) {
+                        seen = 0;
+                        if (!a.parents) {
+                            if (row >= base) seen = row - base >= 31 ? ~0u : (2u << (row - base)) - 1;
+                        } else {
+                            int j = min(row, s.N);
+                            while (j > base + 31) j = up[j];
+                            while (j >= base && j > 0) {
+                                seen |= 1u << (j - base);
+                                j = up[j];
+                            }
+                            if (base == 0) seen |= 1u;
+                        }
+                    } else if (base + 32 > limit) {
+                        seen = (1u << (limit - base)) - 1;
+                    }
+                    if (own || base + 32 > limit) {
+                        const unsigned mine = seen >> (4 * half);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (!(mine >> (8 * (i / 4) + i % 4) & 1)) sc[i] = -__builtin_huge_valf();
+                    }
+                    float top = sc[0];
+#pragma unroll
+                    for (int i = 1; i < 16; ++i) top = fmaxf(top, sc[i]);
+                    top = fmaxf(top, __shfl_xor(top, 32, kWave)) * a.scale;
+                    const bool rise = top > m + H::kSlack;
+                    if (__ballot(rise)) {
+                        const float to = rise ? top : m, by = __builtin_amdgcn_exp2f(m - to);
+                        m = to;
+                        l *= by;
+#pragma unroll
+                        for (int i = 0; i < kBlocks; ++i) o[i] *= by;
+                    }
+                    const float ref = H::kLift - m;
+                    float p[16];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) {
+                        p[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], a.scale, ref));
+                        l += p[i];
+                    }
+                    x8 pb[2];
+#pragma unroll
+                    for (int i = 0; i < 16; ++i) pb[i / 8][i % 8] = (typename H::T)p[i];
+                    // the values, transposed: 4 keys of a column each read
+                    const int q4 = (lane & 15) >> 2, wide = lane >> 4 & 1;
+#pragma unroll
+                    for (int db = 0; db < kBlocks; ++db) {
+#pragma unroll
+                        for (int kb = 0; kb < 2; ++kb) {
+                            union {
+                                s16x4 h[2];
+                                x8 all;
+                                unsigned short e[8];
+                            } vf;
+#pragma unroll
+                            for (int j = 0; j < 2; ++j) {
+                                const int r = 16 * kb + 8 * j + 4 * half + q4, piece = db * 4 + 2 * wide + ((lane & 3) >> 1);
+                                vf.h[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(vt + r * C::kRowBytes + (piece ^ turn<D>(r)) * 16 + (lane & 1) * 8));
+                            }
+                            if (own) {  // what is not finite is taken apart, below
+#pragma unroll
+                                for (int j = 0; j < 8; ++j)
+                                    if ((vf.e[j] & H::kExponent) == H::kExponent) vf.e[j] = 0;
+                            }
+                            o[db] = mfma<DT>(vf.all, pb[kb], o[db]);
+                        }
+                    }
+                    if (own) {
+                        // Values of the block that are not finite count for the rows that see them alone: a product with a weight of 0 is none
+                        for (int r = 0; r < 32; ++r) {
+                            const char* const vr = vt + r * C::kRowBytes;
+                            bool odd = false;
+                            if (lane < D / 2) {
+                                const unsigned w = reinterpret_cast<const unsigned*>(vr)[lane];
+                                odd = (w & H::kExponent) == H::kExponent || (w >> 16 & H::kExponent) == H::kExponent;
+                            }
+                            if (!__ballot(odd) || base + r >= limit) continue;
+                            float w = 0.f;
+#pragma unroll
+                            for (int i = 0; i < 16; ++i) w = (8 * (i / 4) + i % 4) == (r & ~4) ? p[i] : w;
+                            w = __shfl(w, (lane & 31) + ((r & 4) << 3), kWave);
+#pragma unroll
+                            for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+                                for (int i = 0; i < 16; ++i) {
+                                    const int d = db * 32 + 8 * (i / 4) + 4 * half + i % 4;
+                                    const typename H::T e = *reinterpret_cast<const typename H::T*>(vr + ((d / 8) ^ turn<D>(r)) * 16 + (d % 8) * 2);
+                                    const bool finite = (__builtin_bit_cast(unsigned short, e) & H::kExponent) != H::kExponent;
+                                    if (!finite && (seen >> r & 1)) o[db][i] += w * (float)e;
+                                }
+                        }
+                    }
+                }
+            };
+
+            look_up(t0);
+            load(t0, 0);
+            look_up(min(t0 + 1, t1 - 1));
+            const auto step = [&](auto tree_rows, int t) {
+                const int at = (t - t0) & 1;
+                asm volatile("" ::: "memory");
+                __builtin_amdgcn_s_waitcnt(0);
+                __builtin_amdgcn_s_barrier();
+                asm volatile("" ::: "memory");
+                if (t + 1 < t1) {
+                    load(t + 1, at ^ 1);
+                    if (t + 2 < t1) look_up(t + 2);
+                }
+                products(tree_rows, t, lds + at * C::kStage);
+            };
+            int t = t0;
+            for (; t < min(t1, items.cached); ++t) step(std::false_type{}, t);
+            for (; t < t1; ++t) step(std::true_type{}, t);
+            l += __shfl_xor(l, 32, kWave);
+        }
+        if (bad) sh_bad = 1;
+        // the waves' sums over their keys to those of the first
+        __syncthreads();
+        float* const hand = reinterpret_cast<float*>(lds);
+        if (C::WK > 1) {
+            if (half == 0) hand_ml[wk][wm * 32 + (lane & 31)] = make_float2(m, l);
+            if (wk > 0) {
+                float* const to = hand + ((wk - 1) * C::kColumns + wm * 32 + (lane & 31)) * C::kPad;
+#pragma unroll
+                for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        *reinterpret_cast<f32v4*>(to + db * 32 + 8 * i + 4 * half) = f32v4{o[db][4 * i], o[db][4 * i + 1], o[db][4 * i + 2], o[db][4 * i + 3]};
+            }
+            __syncthreads();
+        }
+        if (wk == 0) {
+            if (C::WK > 1) {
+                float top = m;
+                for (int w = 1; w < C::WK; ++w) top = fmaxf(top, hand_ml[w][wm * 32 + (lane & 31)].x);
+                const float by = __builtin_amdgcn_exp2f(m - top);
+                l *= by;
+                m = top;
+#pragma unroll
+                for (int db = 0; db < kBlocks; ++db) o[db] *= by;
+                for (int w = 1; w < C::WK; ++w) {
+                    const float2 ml = hand_ml[w][wm * 32 + (lane & 31)];
+                    const float f = __builtin_amdgcn_exp2f(ml.x - m);
+                    l = fmaf(ml.y, f, l);
+                    const float* const from = hand + ((w - 1) * C::kColumns + wm * 32 + (lane & 31)) * C::kPad;
+#pragma unroll
+                    for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            const f32v4 x = *reinterpret_cast<const f32v4*>(from + db * 32 + 8 * i + 4 * half);
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) o[db][4 * i + j] = fmaf(x[j], f, o[db][4 * i + j]);
+                        }
+                }
+            }
+            if (sh_bad) l = __builtin_nanf("");
+            if (valid) {
+                if (whole) {
+                    const float by = 1.f / l;
+                    char* const to = a.out + 2 * (b * a.os.a + row * a.os.b + (head * a.group + of_group) * a.os.c + 4 * half);
+#pragma unroll
+                    for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            typename H::T r[4];
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) r[j] = (typename H::T)(o[db][4 * i + j] * by);
+                            __builtin_memcpy(__builtin_assume_aligned(to + 2 * (db * 32 + 8 * i), 8), r, 8);
+                        }
+                } else {
+                    const long slot = 2l * blockIdx.x + (first_item ? 0 : 1), c = slot * C::kColumns + wm * 32 + (lane & 31);
+                    if (half == 0) a.part_ml[c] = make_float2(m, l);
+                    float* const to = a.part_o + c * D + 4 * half;
+#pragma unroll
+                    for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            *reinterpret_cast<f32v4*>(to + db * 32 + 8 * i) = f32v4{o[db][4 * i], o[db][4 * i + 1], o[db][4 * i + 2], o[db][4 * i + 3]};
+                }
+            }
+        }
+        first_item = false;
+        rel += t1 - t0;
+        u += t1 - t0;
+    }
+}
+
+// The parts of the item that share blockIdx.x + 1 begins inside of, if no share before it does.
+constexpr int kJoinThreads = 256, kJoinColumns = 16;
+template <int DT, typename C>
+__global__ __launch_bounds__(kJoinThreads) void attention_join_kernel(const AttnArgs a) {
+    using H = Half<DT>;
+    constexpr int D = C::D, kLanes = D / 4, kAtOnce = kJoinThreads / kLanes;
+    __shared__ long sh[kJoinThreads / kWave + 2];
+    const int w = blockIdx.x + 1, tid = threadIdx.x;
+    const TreeTiles tiles{C::kTile, C::kColumns, a.group, a.kv_heads};
+    long u = 0;
+    const Place place = find_place<kJoinThreads>(a, tiles, sh, [&](long total) { return u = share_begin(total, shares_of(a.shares, total), w); });
+    if (u >= place.total) return;
+    const int shares = shares_of(a.shares, place.total);
+    const int b = place.b;
+    const Sequence s = sequence(a, b);
+    const TreeItems items = tree_items(tiles, s.L, s.N, s.bad, a.N);
+    const int nt = items.tiles();
+    const long rel = u - place.before;
+    const int item = (int)(rel / nt), t0 = (int)(rel - (long)item * nt);
+    const long start = u - t0, end = start + nt;
+    if (t0 == 0 || share_begin(place.total, shares, w - 1) > start) return;  // it is cut before this already
+    const int head = item / items.blocks, block = item - head * items.blocks;
+    const int rows = (s.bad ? a.N : s.N) + 1;
+    for (int i = tid / kLanes; i < kJoinColumns; i += kAtOnce) {
+        const int of_block = blockIdx.y * kJoinColumns + i, column = block * C::kColumns + of_block, row = column / a.group;
+        if (of_block >= C::kColumns || row >= rows) break;
+        float m = -1e30f, l = 0.f;
+        f32v4 o = {};
+        for (int x = w - 1; x < shares; ++x) {
+            const long from = share_begin(place.total, shares, x);
+            if (from >= end) break;
+            const long c = (2l * x + (from >= start ? 0 : 1)) * C::kColumns + of_block;
+            const float2 ml = a.part_ml[c];
+            const f32v4 v = *reinterpret_cast<const f32v4*>(a.part_o + c * D + 4 * (tid % kLanes));
+            const float top = fmaxf(m, ml.x), by = __builtin_amdgcn_exp2f(m - top), f = __builtin_amdgcn_exp2f(ml.x - top);
+            l = fmaf(l, by, ml.y * f);
+            o = o * by + v * f;
+            m = top;
+        }
+        typename H::T r[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) r[j] = (typename H::T)(o[j] / l);
+        char* const to = a.out + 2 * (b * a.os.a + row * a.os.b + (head * a.group + (column - row * a.group)) * a.os.c + 4 * (tid % kLanes));
+        __builtin_memcpy(__builtin_assume_aligned(to, 8), r, 8);
+    }
+}
+
+// What a call takes: its shares, one a workgroup that runs at once, and no more than it may have units.
+struct AttnPlan {
+    int columns, shares;
+    size_t off_ml, bytes;
+};
+template <typename C>
+AttnPlan plan_for(const ss_tree_params& p, int groups_a_unit) {
+    const TreeTiles tiles{C::kTile, C::kColumns, p.heads / p.kv_heads, p.kv_heads};
+    TreeItems most = tree_items(tiles, 0, p.nodes, false, p.nodes);
+    most.cached = (int)(((long)p.table_width * p.page_size + C::kTile - 1) / C::kTile);
+    const double units = (double)most.units(p.kv_heads) * p.batch;
+    AttnPlan r;
+    r.columns = C::kColumns;
+    r.shares = device_cu_count() * groups_a_unit;
+    if (units < r.shares) r.shares = units < 1 ? 1 : (int)units;
+    const size_t slots = 2 * (size_t)r.shares * C::kColumns;
+    r.off_ml = slots * C::D * 4;
+    r.bytes = (r.off_ml + slots * 8 + 255) / 256 * 256;
+    return r;
+}
+
+template <typename F>
+auto with_shape(const ss_tree_params& p, F f) {
+    const int columns = (p.nodes + 1) * (p.heads / p.kv_heads);
+    if (p.head_dim == 64) {
+        if (columns <= 32) return f(Shape<64, 1, 2>{}, 2);
+        if (columns <= 64) return f(Shape<64, 2, 2>{}, 2);
+        return f(Shape<64, 4, 2>{}, 1);
+    }
+    if (columns <= 32) return f(Shape<128, 1, 2>{}, 2);
+    if (columns <= 64) return f(Shape<128, 2, 2>{}, 2);
+    return f(Shape<128, 4, 2>{}, 1);
 }
 
 }  // namespace
@@ -82,7 +562,8 @@ extern "C" {
 
 size_t specsteer_tree_attention_workspace_bytes(const ss_tree_params* params) {
     TreeShape s;
-    return tree_shape(params, true, s) == SS_OK ? 256 : 0;
+    if (tree_shape(params, true, s) != SS_OK) return 0;
+    return with_shape(*params, [&](auto shape, int groups) { return plan_for<decltype(shape)>(*params, groups).bytes; });
 }
 
 ss_status specsteer_tree_attention(const void* q, const void* k, const void* v, const void* k_cache, const void* v_cache, const int32_t* block_table,
@@ -95,17 +576,48 @@ ss_status specsteer_tree_attention(const void* q, const void* k, const void* v, 
     const bool cached = params->pages > 0 && params->table_width > 0;
     if (!q || !k || !v || !cache_len || !out || (cached && (!k_cache || !v_cache || !block_table))) return SS_ERR_NULL;
     if (off_16(q) || off_16(k) || off_16(v) || off_16(out) || (cached && (off_16(k_cache) || off_16(v_cache)))) return SS_ERR_STRIDE;
-    if (bad_workspace(workspace, workspace_bytes, 256)) return SS_ERR_WORKSPACE;
-    const auto in = [](const void* p) { return static_cast<const char*>(p); };
-    AttnArgs a{in(q), in(k), in(v), in(k_cache), in(v_cache), block_table, cache_len, params->nodes ? parents : nullptr, tree_len, static_cast<char*>(out),
-               s.q, s.k, s.out, s.cache, s.table, params->batch, params->nodes, params->heads, params->heads / params->kv_heads, params->pages,
-               params->page_size, params->table_width, params->scale * 1.4426950408889634f};
-    if (!cached) a.width = 0;
-    const dim3 grid((unsigned)(params->nodes + 1), (unsigned)params->heads, (unsigned)params->batch);
-    hipStream_t st = static_cast<hipStream_t>(stream);
-    if (params->dtype == SS_BF16) launch(params->head_dim == 64 ? attention_kernel<SS_BF16, 64> : attention_kernel<SS_BF16, 128>, grid, dim3(kWave), 0, st, (const AttnArgs)a);
-    else launch(params->head_dim == 64 ? attention_kernel<SS_TREE_F16, 64> : attention_kernel<SS_TREE_F16, 128>, grid, dim3(kWave), 0, st, (const AttnArgs)a);
-    return tree_launched();
+    return with_shape(*params, [&](auto shape, int groups) {
+        using C = decltype(shape);
+        const AttnPlan plan = plan_for<C>(*params, groups);
+        if (bad_workspace(workspace, workspace_bytes, plan.bytes)) return SS_ERR_WORKSPACE;
+        const auto in = [](const void* p) { return static_cast<const char*>(p); };
+        AttnArgs a{};
+        a.q = in(q);
+        a.k = in(k);
+        a.v = in(v);
+        a.kc = in(k_cache);
+        a.vc = in(v_cache);
+        a.table = block_table;
+        a.cache_len = cache_len;
+        a.parents = params->nodes ? parents : nullptr;
+        a.tree_len = tree_len;
+        a.out = static_cast<char*>(out);
+        a.part_o = static_cast<float*>(workspace);
+        a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + plan.off_ml);
+        a.qs = s.q;
+        a.ks = s.k;
+        a.os = s.out;
+        a.cs = s.cache;
+        a.ts = s.table;
+        a.B = params->batch;
+        a.N = params->nodes;
+        a.kv_heads = params->kv_heads;
+        a.group = params->heads / params->kv_heads;
+        a.pages = params->pages;
+        a.page_size = params->page_size;
+        a.width = cached ? params->table_width : 0;
+        a.shares = plan.shares;
+        // a factor of 0 would make masked scores NaN; under this one all that can be told apart is the mask
+        a.scale = std::fmax(std::fabs(params->scale) * 1.4426950408889634f, 1e-30f);
+        a.negative = params->scale < 0.f;
+        hipStream_t st = static_cast<hipStream_t>(stream);
+        const bool bf = params->dtype == SS_BF16;
+        launch(bf ? attention_kernel<SS_BF16, C> : attention_kernel<SS_TREE_F16, C>, dim3((unsigned)plan.shares), dim3(C::kThreads), 0, st, (const AttnArgs)a);
+        if (plan.shares > 1)
+            launch(bf ? attention_join_kernel<SS_BF16, C> : attention_join_kernel<SS_TREE_F16, C>,
+                   dim3((unsigned)plan.shares - 1, (unsigned)((C::kColumns + kJoinColumns - 1) / kJoinColumns)), dim3(kJoinThreads), 0, st, (const AttnArgs)a);
+        return tree_launched();
+    });
 }
 
 const char* specsteer_tree_status_string(int status) {
