@@ -1,7 +1,7 @@
 // The verify-and-recover step down a tree of drafts, for MI355X (gfx950); include/specsteer_tree.h says what it computes.
 //
 // The rows that the walk comes through are known only as it goes, and a row is read by many workgroups.  A tree is therefore taken in stages
-// (verify_plan.h): one sums some rows at and below the cursor, of G and S_noctx, whichever way the walk may take there; the next one's workgroups
+// (verify_plan.h), two at most: one sums some rows at and below the cursor, of G and S_noctx, whichever way the walk may take there; the next one's workgroups
 // each walk over those sums for themselves, from what lies in LDS by then, and sum the rows that follow.  The last launch walks to the
 // end, forms the recovery row's masses a chunk of 4 vectors a lane at a time, and the workgroup of a sequence that comes last draws the token.
 //
@@ -41,7 +41,8 @@ struct VerifyArgs {
     int B, N, V;
     Factor c;
     double c64, inv_tau, lambda, beta;
-    int far, greedy, plain;  // plain: beta is 0
+    float steer_hi, steer_lo;  // beta c in two parts
+    int far, greedy, plain;    // plain: beta is 0
     int slices, slice_vecs, chunks, parts, part_chunks;
 };
 
@@ -224,22 +225,187 @@ __device__ __forceinline__ int reach(const VerifyArgs& a, int b, int stage, int 
     return N;
 }
 
-// Stage `stage`: the sums of one slice of some of its rows.
+// ------------------------------------------------------------------ trees of up to 63 nodes
+
+// The same for a tree whose rows are the bits of a word: a lane a node, children and descendants by ballots.  Everything that memory holds of the walk
+// so far, the sums of rows that were not summed among it, is on its way at once; what bounds a stage's beginning is that one round trip and the
+// two logarithms of a row.  By the general walk, whose loads wait for one another and whose steps for barriers, the rows' launches of 64 trees of up to 31 nodes
+// took 12 to 28 us and the draw 27.
+constexpr int kSmall = 63;
+struct SmallShared {
+    double diff[kSmall + 1];
+    unsigned long long far[kVerifyGroup / kWave], inner, set, rows;
+    signed char parent[kSmall + 1];
+    Total<Sum> part[kVerifyGroup / kWave];
+    int scan[kVerifyGroup / kWave];
+    double table[SS_MAX_K + 1];
+    Cursor at;
+};
+
+__device__ __forceinline__ unsigned long long lowest_bits(unsigned long long m, int n) {
+    while (__popcll(m) > n) m &= ~(1ull << (63 - __clzll((long long)m)));
+    return m;
+}
+// Rows at and below the cursor, by a wave whose lane i has node i's parent (or one that no row is).
+__device__ __forceinline__ unsigned long long rows_below(int cur, int parent) {
+    unsigned long long m = 1ull << (cur + 1);
+    for (;;) {
+        const unsigned long long more = m | __ballot(parent >= -1 && (m >> (parent + 1) & 1)) << 1;
+        if (more == m) return m;
+        m = more;
+    }
+}
+
 template <int DT>
+__device__ __forceinline__ int reach(const VerifyArgs& a, int b, int stage, int rows_before, int rows, bool leader, SmallShared& w) {
+    constexpr int kLanes = 4, kMine = 16 / kLanes;  // lanes a row
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int r = tid / kLanes, l = tid % kLanes;
+    Total<Sum> s[2][kMine];
+#pragma unroll
+    for (int x = 0; x < 2; ++x)
+#pragma unroll
+        for (int k = 0; k < kMine; ++k) {
+            clear_total(s[x][k]);
+            const int i = k * kLanes + l;
+            if (stage > 0 && r <= a.N && i < a.slices) s[x][k] = a.sums[(((long)b * (a.N + 1) + r) * 2 + x) * a.slices + i];
+        }
+    Cursor c{-1, 0, 0, 0};
+    if (stage > 0) c = a.cursors[(long)(stage - 1) * a.B + b];
+    int N = nodes_of(a, b), parent = -5, token = 0;
+    float2 h = make_float2(0.f, 0.f);
+    double u = 0.0;
+    if (wave == 0 && lane < a.N) {
+        parent = a.parents ? a.parents[(long)b * a.N + lane] : lane - 1;
+        if (stage == 0) token = a.tokens[(long)b * a.N + lane];
+        else {
+            h = a.logits[(long)b * a.N + lane];
+            u = a.uniforms[(long)b * (a.N + 1) + lane];
+        }
+    }
+    if (tid == 0) w.inner = 0;
+    if (stage > 0) {
+        double lse[2];
+        bool far = false;
+#pragma unroll
+        for (int x = 0; x < 2; ++x) {
+            Total<Sum> t;
+            t.E = fmaxf(fmaxf(s[x][0].E, s[x][1].E), fmaxf(s[x][2].E, s[x][3].E));
+            t.s = 0.0;
+#pragma unroll
+            for (int k = 0; k < kMine; ++k) t.s += moved(s[x][k].s, s[x][k].E, t.E);
+            t = join_group(t, kLanes);
+            far = far || a.far || is_far(t);
+            lse[x] = (double)t.E + log2(t.s);
+        }
+        if (l == 0) w.diff[r] = lse[0] - lse[1];
+        unsigned long long mask = 0;
+        const unsigned long long ballot = __ballot(far && l == 0 && r <= a.N);
+        for (int k = 0; k < kWave / kLanes; ++k) mask |= (ballot >> (kLanes * k) & 1) << (wave * (kWave / kLanes) + k);
+        if (lane == 0) w.far[wave] = mask;
+    }
+    __syncthreads();
+    unsigned long long set = 0, inner = 0;
+    if (wave == 0) {
+        if (stage == 0) {
+            const bool bad = N < 0 || N > a.N || (lane < N && (parent < -1 || parent >= lane || token < 0 || token >= a.V));
+            c.done = __ballot(bad) ? 2 : N == 0 ? 1 : 0;
+        }
+        if (c.done || lane >= N) parent = -5;
+        if (parent >= -1) atomicOr(&w.inner, 1ull << (parent + 1));
+        w.parent[lane] = (signed char)parent;
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        inner = *const_cast<volatile unsigned long long*>(&w.inner);
+        if (stage > 0 && !c.done) set = lowest_bits(rows_below(c.cur, parent) & inner, rows_before);
+        if (lane == 0) {
+            w.at = c;
+            w.set = set;
+        }
+    }
+    if (stage > 0) {
+        __syncthreads();
+        const unsigned long long all = w.set, far = all & (w.far[0] | w.far[1] | w.far[2] | w.far[3]);
+        if (far) {  // rows far from zero, by the whole workgroup
+            for (unsigned long long m = far; m; m &= m - 1) {
+                const int fr = first_lane(m);
+                double lse[2];
+                for (int x = 0; x < 2; ++x) {
+                    const void* const row = row_ptr<DT>(x ? a.Sm : a.G, b * a.sb + fr * a.st);
+                    __syncthreads();
+                    const Total<Sum> t = far_sum<DT, Sum>(row, nullptr, a.V, a.c64, kVerifyGroup, w.part);
+                    lse[x] = (double)t.E * a.c64 + log2(t.s);
+                }
+                if (tid == 0) w.diff[fr] = lse[0] - lse[1];
+            }
+            __syncthreads();
+        }
+    }
+    if (wave == 0) {
+        if (stage > 0 && !c.done) {
+            bool accept = false;
+            if (parent >= -1 && (set >> (parent + 1) & 1)) {
+                // masked by G: never accepted; by S_noctx alone: always
+                const double alpha = h.x == -__builtin_huge_valf() ? -1.0 : exp2(((double)h.x - (double)h.y) * a.c64 - w.diff[parent + 1]) / a.lambda;
+                accept = u <= 1.0 && !(u > alpha);
+            }
+            for (;;) {
+                const int row = c.cur + 1;
+                if (!(inner >> row & 1)) c.done = 1;
+                else if (!(set >> row & 1)) break;
+                const unsigned long long taken = c.done ? 0 : __ballot(accept && parent == c.cur);
+                if (!taken) {
+                    c.done = 1;
+                    break;
+                }
+                c.cur = first_lane(taken);
+                if (leader && lane == 0) a.path[(long)b * a.N + c.n] = c.cur;
+                ++c.n;
+            }
+        }
+        const unsigned long long next = c.done ? 0 : lowest_bits(rows_below(c.cur, parent) & inner, rows);
+        if (lane == 0) {
+            w.at = c;
+            w.rows = next;
+        }
+    }
+    __syncthreads();
+    return N;
+}
+
+// The same by the general walk.
+template <int DT>
+__device__ __forceinline__ int reach(const VerifyArgs& a, int b, int stage, int rows_before, int rows, bool leader, WalkShared& w) {
+    const int N = reach<DT>(a, b, stage, rows_before, leader, w);
+    if (!w.at.done && rows) pick_rows(a, N, w.at.cur, rows, w);
+    return N;
+}
+__device__ __forceinline__ int row_count(const WalkShared& w) { return w.count; }
+__device__ __forceinline__ int row_count(const SmallShared& w) { return __popcll(w.rows); }
+__device__ __forceinline__ int nth_row(const WalkShared& w, int k) { return w.rows[k]; }
+__device__ __forceinline__ int nth_row(const SmallShared& w, int k) {
+    unsigned long long m = w.rows;
+    for (; k > 0; --k) m &= m - 1;
+    return first_lane(m);
+}
+__device__ __forceinline__ double* space_of(WalkShared& w) { return w.diff; }
+__device__ __forceinline__ double* space_of(SmallShared& w) { return w.table; }
+
+// Stage `stage`: the sums of one slice of some of its rows.
+template <int DT, typename W>
 __global__ __launch_bounds__(kVerifyGroup) void rows_kernel(const VerifyArgs a, const int stage, const int rows_before, const int rows, const int groups) {
-    __shared__ WalkShared w;
+    __shared__ W w;
     const int per = groups * 2 * a.slices, b = (int)(blockIdx.x / (unsigned)per), id = (int)(blockIdx.x - (unsigned)(b * per));
     const int slice = id % a.slices, x = id / a.slices & 1, group = id / (2 * a.slices);
     const bool leader = id == 0;
-    const int N = reach<DT>(a, b, stage, rows_before, leader, w);
+    const int N = reach<DT>(a, b, stage, rows_before, rows, leader, w);
     if (leader && threadIdx.x == 0) {
         a.cursors[(long)stage * a.B + b] = w.at;
         if (stage == 0 && a.parts > 1) *reinterpret_cast<int*>(a.arrive + (long)b * kArriveBytes) = 0;
     }
     if (w.at.done) return;
-    pick_rows(a, N, w.at.cur, rows, w);
-    for (int k = group; k < w.count; k += groups) {
-        const int r = w.rows[k];
+    const int count = row_count(w);
+    for (int k = group; k < count; k += groups) {
+        const int r = nth_row(w, k);
         const void* const h = row_ptr<DT>(x ? a.Sm : a.G, b * a.sb + r * a.st);
         const Layout<DT> lay(h, a.V, threadIdx.x);
         const int begin = min(lay.vecs, slice * a.slice_vecs), end = slice + 1 == a.slices ? lay.vecs : min(lay.vecs, begin + a.slice_vecs);
@@ -260,50 +426,93 @@ template <int DT>
 struct RecoveryRow {
     const void *g, *sp, *sm;
 };
-// Eq. 8's exponent, in double
-__device__ __forceinline__ double rec_exponent(const VerifyArgs& a, float g, float sp, float sm) {
-    return a.plain ? (double)g * a.c64 : fma((double)g, a.c64, steer(sp, sm) * (a.beta * a.c64));
+// Eq. 8's exponent less E, in fp32: g c first, whose upper part is exact for bf16 (loss_rows.h), so that what is rounded is of the difference's size.
+// In double the masses of 64 rows of V = 128256 took 14 us, most of it arithmetic.
+__device__ __forceinline__ float rec_exponent(const VerifyArgs& a, float g, float d, float E) {
+    const float t = exponent<2>(g, E, a.c);
+    return a.plain ? t : fmaf(d, a.steer_lo, fmaf(d, a.steer_hi, t));
 }
+// and in double, for the token drawn
+__device__ __forceinline__ double rec_exponent64(const VerifyArgs& a, double g, double d) { return fma(g, a.c64, d * (a.beta * a.c64)); }
 
-// Chunk `c` of a row by a wave: each lane's logits, -inf where there are none, and the first one's id.  The last chunk has the elements behind the
-// last vector, one a lane.
+// A step of chunk `c` of a row by a wave: each lane's logits of G, -inf where there are none, and the steering term's differences; returns the
+// first one's id.  The last chunk has the elements behind the last vector, one a lane.
 template <int DT>
-__device__ __forceinline__ int load_chunk(const VerifyArgs& a, const RecoveryRow<DT>& row, int c, int step, float (&g)[Row<DT>::kVec],
-                                          float (&sp)[Row<DT>::kVec], float (&sm)[Row<DT>::kVec]) {
+struct Chunk {
+    typename Row<DT>::Raw g, sp, sm;
+    int id;
+};
+template <int DT>
+__device__ __forceinline__ Chunk<DT> load_chunk(const VerifyArgs& a, const RecoveryRow<DT>& row, int c, int step) {
     constexpr int kVec = Row<DT>::kVec;
     const int lane = threadIdx.x & 63, vecs = a.V / kVec;
-#pragma unroll
-    for (int i = 0; i < kVec; ++i) {
-        g[i] = -__builtin_huge_valf();
-        sp[i] = sm[i] = 0.f;
-    }
+    Chunk<DT> k;
+    k.g = neg_inf_raw<DT, kVec>();
+    k.sp = k.sm = typename Row<DT>::Raw{};
     if (c + 1 < a.chunks) {
         const int v = c * kMassVecs + step * kWave + lane;
         if (v < vecs) {
-            unpack(ld_raw<DT, kVec>(row.g, v), g);
+            k.g = ld_raw<DT, kVec>(row.g, v);
             if (!a.plain) {
-                unpack(ld_raw<DT, kVec>(row.sp, v), sp);
-                unpack(ld_raw<DT, kVec>(row.sm, v), sm);
+                k.sp = ld_raw<DT, kVec>(row.sp, v);
+                k.sm = ld_raw<DT, kVec>(row.sm, v);
             }
         }
-        return v * kVec;
+        k.id = v * kVec;
+        return k;
     }
-    const int at = vecs * kVec + lane;
-    if (step == 0 && at < a.V) {
-        g[0] = ld_elem<DT>(row.g, at);
+    k.id = vecs * kVec + lane;
+    if (step == 0 && k.id < a.V) {
+        const auto first = [&](typename Row<DT>::Raw& r, const void* p) {
+            if constexpr (DT == SS_BF16) r.x = (r.x & 0xFFFF0000u) | reinterpret_cast<const unsigned short*>(p)[k.id];
+            else r.x = reinterpret_cast<const float*>(p)[k.id];
+        };
+        first(k.g, row.g);
         if (!a.plain) {
-            sp[0] = ld_elem<DT>(row.sp, at);
-            sm[0] = ld_elem<DT>(row.sm, at);
+            first(k.sp, row.sp);
+            first(k.sm, row.sm);
         }
     }
-    return at;
+    return k;
+}
+// a token that both of the specialist's rows mask has no steering term
+template <int DT>
+__device__ __forceinline__ void unpack_chunk(const Chunk<DT>& k, float (&g)[Row<DT>::kVec], float (&d)[Row<DT>::kVec]) {
+    constexpr int kVec = Row<DT>::kVec;
+    float sp[kVec], sm[kVec];
+    unpack(k.g, g);
+    unpack(k.sp, sp);
+    unpack(k.sm, sm);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) d[i] = sp[i] == sm[i] ? 0.f : sp[i] - sm[i];
 }
 constexpr int kMassSteps = kMassVecs / kWave;
 
-template <int DT>
+// What workgroups hand over inside a launch goes past the caches of one die with stores and loads at device scope; a wave has delivered when its
+// stores are acknowledged.  Fences, which write a die's whole cache back, took 100 us of a launch of 512 workgroups.
+__device__ __forceinline__ void put(unsigned long long* p, unsigned long long v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ unsigned long long get(const unsigned long long* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
+__device__ __forceinline__ void put(Mass* p, Mass m) { put(reinterpret_cast<unsigned long long*>(p), __builtin_bit_cast(unsigned long long, m)); }
+__device__ __forceinline__ Mass get(const Mass* p) { return __builtin_bit_cast(Mass, get(reinterpret_cast<const unsigned long long*>(p))); }
+__device__ __forceinline__ void put(Best* p, Best v) {
+    unsigned long long* const q = reinterpret_cast<unsigned long long*>(p);
+    put(q, __builtin_bit_cast(unsigned long long, v.h));
+    put(q + 1, (unsigned long long)(unsigned)v.id);
+}
+__device__ __forceinline__ Best get(const Best* p) {
+    const unsigned long long* const q = reinterpret_cast<const unsigned long long*>(p);
+    return Best{__builtin_bit_cast(double, get(q)), (int)(unsigned)get(q + 1), 0};
+}
+__device__ __forceinline__ void delivered() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(0);
+    asm volatile("" ::: "memory");
+}
+
+template <int DT, typename W>
 __global__ __launch_bounds__(kVerifyGroup) void draw_kernel(const VerifyArgs a, const int stages, const int rows_before) {
     constexpr int kVec = Row<DT>::kVec, kWaves = kVerifyGroup / kWave;
-    __shared__ WalkShared w;
+    __shared__ W w;
     __shared__ Best best[kWaves];
     __shared__ double sum[kWaves];
     __shared__ int pick[4];
@@ -311,7 +520,7 @@ __global__ __launch_bounds__(kVerifyGroup) void draw_kernel(const VerifyArgs a, 
     const int b = (int)(blockIdx.x / (unsigned)a.parts), part = (int)(blockIdx.x - (unsigned)(b * a.parts));
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const bool leader = part == 0;
-    reach<DT>(a, b, stages, rows_before, leader, w);
+    reach<DT>(a, b, stages, rows_before, 0, leader, w);
     const Cursor at = w.at;
     const bool marked = at.done == 2;
     if (leader) {
@@ -329,37 +538,41 @@ __global__ __launch_bounds__(kVerifyGroup) void draw_kernel(const VerifyArgs a, 
     Best top{-__builtin_huge_val(), kNever, 0};
     const int c1 = min(a.chunks, (part + 1) * a.part_chunks);
     for (int c = part * a.part_chunks + wave; c < c1; c += kWaves) {
-        double y[kMassSteps][kVec];
+        Chunk<DT> k[kMassSteps];
+#pragma unroll
+        for (int s = 0; s < kMassSteps; ++s) k[s] = load_chunk<DT>(a, row, c, s);
         float most = -__builtin_huge_valf();
 #pragma unroll
         for (int s = 0; s < kMassSteps; ++s) {
-            float g[kVec], sp[kVec], sm[kVec];
-            const int id = load_chunk<DT>(a, row, c, s, g, sp, sm);
+            float g[kVec], d[kVec];
+            unpack_chunk<DT>(k[s], g, d);
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) {
-                y[s][i] = rec_exponent(a, g[i], sp[i], sm[i]);
-                most = fmaxf(most, (float)y[s][i]);
-            }
-            if (a.greedy)
+            for (int i = 0; i < kVec; ++i) most = fmaxf(most, rec_exponent(a, g[i], d[i], 0.f));
+            if (a.greedy) {
+                float sp[kVec], sm[kVec];
+                unpack(k[s].sp, sp);
+                unpack(k[s].sm, sm);
 #pragma unroll
                 for (int i = 0; i < kVec; ++i) {
                     const double h = a.plain ? (double)g[i] : __dadd_rn((double)g[i], __dmul_rn(a.beta, steer(sp[i], sm[i])));
-                    if (h > top.h) top = Best{h, id + i, 0};
+                    if (h > top.h) top = Best{h, k[s].id + i, 0};
                 }
+            }
         }
         for (int d = 1; d < kWave; d <<= 1) most = fmaxf(most, __shfl_xor(most, d, kWave));
         // a reference near the largest exponent; a chunk of masked tokens has any
         const float E = fmaxf(fminf(ceilf(most), 3e38f), -3e38f);
         float s = 0.f;
 #pragma unroll
-        for (int k = 0; k < kMassSteps; ++k) {
-            float e[kVec];
+        for (int u = 0; u < kMassSteps; ++u) {
+            float g[kVec], d[kVec], e[kVec];
+            unpack_chunk<DT>(k[u], g, d);
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) e[i] = exp2_hw((float)(y[k][i] - (double)E));
+            for (int i = 0; i < kVec; ++i) e[i] = exp2_hw(rec_exponent(a, g[i], d[i], E));
             s += tree_sum(e);
         }
         const double all = wave_sum_f64((double)s);
-        if (lane == 0) masses[c] = Mass{E, (float)all};
+        if (lane == 0) put(masses + c, Mass{E, (float)all});
     }
     if (a.greedy) {
         for (int d = 1; d < kWave; d <<= 1) {
@@ -372,32 +585,34 @@ __global__ __launch_bounds__(kVerifyGroup) void draw_kernel(const VerifyArgs a, 
         if (tid == 0) {
             for (int v = 1; v < kWaves; ++v)
                 if (best[v].h > top.h || (best[v].h == top.h && best[v].id < top.id)) top = best[v];
-            a.best[(long)b * a.parts + part] = top;
+            put(a.best + (long)b * a.parts + part, top);
         }
     }
-    __threadfence();
+    delivered();
     __syncthreads();
     if (a.parts > 1) {  // the last of the sequence's workgroups goes on
         if (tid == 0) pick[0] = atomicAdd(reinterpret_cast<int*>(a.arrive + (long)b * kArriveBytes), 1);
         __syncthreads();
         if (pick[0] + 1 < a.parts) return;
-        __threadfence();
     }
     // all masses at the largest reference
+    static_assert(sizeof(Mass) <= sizeof(double) && SS_MAX_VOCAB / 4 / kMassVecs + 1 <= SS_MAX_K + 1, "space for a row's masses");
+    Mass* const table = reinterpret_cast<Mass*>(space_of(w));
     float E = -__builtin_huge_valf();
     for (int c = tid; c < a.chunks; c += kVerifyGroup) {
-        const Mass m = masses[c];
+        const Mass m = get(masses + c);
+        table[c] = m;
         if (m.s > 0.f) E = fmaxf(E, m.E);
     }
     for (int d = 1; d < kWave; d <<= 1) E = fmaxf(E, __shfl_xor(E, d, kWave));
     if (lane == 0) sum[wave] = (double)E;
     __syncthreads();
     for (int v = 0; v < kWaves; ++v) E = fmaxf(E, (float)sum[v]);
-    const auto mass = [&](Mass m) { return m.s > 0.f ? (double)m.s * exp2((double)m.E - (double)E) : 0.0; };
+    const auto mass = [&](Mass m) { return m.s > 0.f ? moved((double)m.s, m.E, E) : 0.0; };
     // a lane's chunks lie next to each other, so that the lanes' sums are in order
     const int each = (a.chunks + kVerifyGroup - 1) / kVerifyGroup, lo = min(a.chunks, tid * each), hi = min(a.chunks, lo + each);
     double mine = 0.0;
-    for (int c = lo; c < hi; ++c) mine += mass(masses[c]);
+    for (int c = lo; c < hi; ++c) mine += mass(table[c]);
     const double incl = wave_incl_scan_f64(mine);
     __syncthreads();
     if (lane == 63) sum[wave] = incl;
@@ -411,9 +626,9 @@ __global__ __launch_bounds__(kVerifyGroup) void draw_kernel(const VerifyArgs a, 
     const double log2Z = (double)E + log2(Z);
     if (a.greedy) {
         if (tid == 0) {
-            Best t = a.best[(long)b * a.parts];
+            Best t = get(a.best + (long)b * a.parts);
             for (int v = 1; v < a.parts; ++v) {
-                const Best o = a.best[(long)b * a.parts + v];
+                const Best o = get(a.best + (long)b * a.parts + v);
                 if (o.h > t.h || (o.h == t.h && o.id < t.id)) t = o;
             }
             a.next_token[b] = min(t.id, a.V - 1);
@@ -428,7 +643,7 @@ __global__ __launch_bounds__(kVerifyGroup) void draw_kernel(const VerifyArgs a, 
         int found = kNever, last = -1;
         double start = 0.0;
         for (int c = lo; c < hi; ++c) {
-            const double m = mass(masses[c]);
+            const double m = mass(table[c]);
             if (m > 0.0) last = c;
             if (found == kNever && m > 0.0 && cum + m > target) {
                 found = c;
@@ -460,33 +675,42 @@ __global__ __launch_bounds__(kVerifyGroup) void draw_kernel(const VerifyArgs a, 
     const bool take_last = chunk == kNever;
     if (take_last) chunk = last_chunk;
     if (wave != 0) return;
-    // wave 0 goes over the chunk again, a vector a lane at a time
-    const double cE = (double)masses[chunk].E, scale = exp2(cE - (double)E);
+    // wave 0 goes over the chunk again, in the order of its tokens
+    const float cE = table[chunk].E;
+    const double scale = moved(1.0, cE, E);
+    Chunk<DT> k[kMassSteps];
+#pragma unroll
+    for (int s = 0; s < kMassSteps; ++s) k[s] = load_chunk<DT>(a, row, chunk, s);
     int token = -1, last = 0;
     double y_token = 0.0, y_last = 0.0;
     for (int s = 0; s < kMassSteps && token < 0; ++s) {
-        float g[kVec], sp[kVec], sm[kVec];
-        const int id = load_chunk<DT>(a, row, chunk, s, g, sp, sm);
-        double y[kVec], e[kVec], own = 0.0;
+        Chunk<DT> now = k[0];
+#pragma unroll
+        for (int v = 1; v < kMassSteps; ++v)
+            if (s == v) now = k[v];
+        float g[kVec], d[kVec], e[kVec];
+        double own = 0.0;
+        unpack_chunk<DT>(now, g, d);
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
-            y[i] = rec_exponent(a, g[i], sp[i], sm[i]);
-            e[i] = (double)exp2_hw((float)(y[i] - cE)) * scale;
-            own += e[i];
+            e[i] = exp2_hw(rec_exponent(a, g[i], d[i], cE));
+            own += (double)e[i];
         }
-        const double in = wave_incl_scan_f64(own);
-        double cum = start + (in - own);
+        const double in = wave_incl_scan_f64(own * scale);
+        double cum = start + wave_shift_up_f64(in);
         int hit = -1, some = -1;
-        double y_hit = 0.0, y_some = 0.0;
+        float g_hit = 0.f, g_some = 0.f, d_hit = 0.f, d_some = 0.f;
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
-            cum += e[i];
-            if (e[i] > 0.0) {
-                some = id + i;
-                y_some = y[i];
+            cum += (double)e[i] * scale;
+            if (e[i] > 0.f) {
+                some = now.id + i;
+                g_some = g[i];
+                d_some = d[i];
                 if (hit < 0 && !take_last && cum > target) {
-                    hit = id + i;
-                    y_hit = y[i];
+                    hit = some;
+                    g_hit = g[i];
+                    d_hit = d[i];
                 }
             }
         }
@@ -494,12 +718,12 @@ __global__ __launch_bounds__(kVerifyGroup) void draw_kernel(const VerifyArgs a, 
         if (hits) {
             const int L = first_lane(hits);
             token = __shfl(hit, L, kWave);
-            y_token = __shfl(y_hit, L, kWave);
+            y_token = rec_exponent64(a, (double)__shfl(g_hit, L, kWave), (double)__shfl(d_hit, L, kWave));
         }
         if (somes) {
             const int L = 63 - __clzll((long long)somes);
             last = __shfl(some, L, kWave);
-            y_last = __shfl(y_some, L, kWave);
+            y_last = rec_exponent64(a, (double)__shfl(g_some, L, kWave), (double)__shfl(d_some, L, kWave));
         }
         start += wave_last_f64(in);
     }
@@ -571,6 +795,8 @@ ss_status specsteer_tree_verify(const void* G, const void* S_ctx, const void* S_
     a.inv_tau = r.inv_tau;
     a.lambda = (double)params->lambda;
     a.beta = (double)params->beta;
+    a.steer_hi = (float)(a.beta * a.c64);
+    a.steer_lo = (float)(a.beta * a.c64 - (double)a.steer_hi);
     a.far = r.far;
     a.greedy = (params->flags & SS_FLAG_GREEDY) ? 1 : 0;
     a.plain = params->beta == 0.f ? 1 : 0;
@@ -580,13 +806,14 @@ ss_status specsteer_tree_verify(const void* G, const void* S_ctx, const void* S_
     a.parts = p.parts;
     a.part_chunks = p.part_chunks;
     hipStream_t q = static_cast<hipStream_t>(stream);
-    const bool bf = params->dtype == SS_BF16;
-    if (p.stages == 0 && p.parts > 1)
-        launch(clear_kernel, dim3((unsigned)((a.B + 255) / 256)), dim3(256), 0, q, a.arrive, a.B);
+    if (p.stages == 0 && p.parts > 1) launch(clear_kernel, dim3((unsigned)((a.B + 255) / 256)), dim3(256), 0, q, a.arrive, a.B);
+    const bool bf = params->dtype == SS_BF16, small = params->k_max <= kSmall;
+    const auto rows = bf ? small ? rows_kernel<SS_BF16, SmallShared> : rows_kernel<SS_BF16, WalkShared> : small ? rows_kernel<SS_F32, SmallShared> : rows_kernel<SS_F32, WalkShared>;
+    const auto draw = bf ? small ? draw_kernel<SS_BF16, SmallShared> : draw_kernel<SS_BF16, WalkShared> : small ? draw_kernel<SS_F32, SmallShared> : draw_kernel<SS_F32, WalkShared>;
     for (int k = 0; k < p.stages; ++k)
-        launch(bf ? rows_kernel<SS_BF16> : rows_kernel<SS_F32>, dim3((unsigned)a.B * (unsigned)(p.groups[k] * 2 * p.slices)), dim3(kVerifyGroup), 0, q, (const VerifyArgs)a, (const int)k,
+        launch(rows, dim3((unsigned)a.B * (unsigned)(p.groups[k] * 2 * p.slices)), dim3(kVerifyGroup), 0, q, (const VerifyArgs)a, (const int)k,
                (const int)(k ? p.rows[k - 1] : 0), (const int)p.rows[k], (const int)p.groups[k]);
-    launch(bf ? draw_kernel<SS_BF16> : draw_kernel<SS_F32>, dim3((unsigned)a.B * (unsigned)p.parts), dim3(kVerifyGroup), 0, q, (const VerifyArgs)a, (const int)p.stages,
+    launch(draw, dim3((unsigned)a.B * (unsigned)p.parts), dim3(kVerifyGroup), 0, q, (const VerifyArgs)a, (const int)p.stages,
            (const int)(p.stages ? p.rows[p.stages - 1] : 0));
     return tree_launched();
 }

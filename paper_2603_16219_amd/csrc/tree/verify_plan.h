@@ -7,7 +7,7 @@ namespace {
 
 // A stage sums the first `rows` rows with children at and below the cursor, in the order of the nodes; the next one walks on over them, and
 // goes on from there.  The last one takes all that are left.
-constexpr int kMaxStages = 5;
+constexpr int kMaxStages = 2;
 struct VerifyPlan {
     int stages;
     int rows[kMaxStages];
@@ -20,35 +20,35 @@ struct VerifyPlan {
 
 constexpr int kVerifyGroup = 256;                      // threads
 constexpr int kMassVecs = 4 * 64;                     // of a wave
-constexpr long kStageBytes = 24l << 20;                // about what a launch costs by itself
+constexpr long kAllBytes = 160l << 20, kFirstBytes = 36l << 20;
+constexpr int kMaxParts = 16;                          // slices of a row
 constexpr int kArriveBytes = 256;                      // between the counters of two sequences
 inline VerifyPlan verify_plan(const ss_params& p, int units) {
     const auto up = [](size_t n) { return (n + 255) / 256 * 256; };
     VerifyPlan r{};
     const long B = p.batch > 0 ? p.batch : 1, N = p.k_max, esz = p.dtype == SS_BF16 ? 2 : 4, vec = 16 / esz, vecs = p.vocab / vec;
     const double pair = 2.0 * B * p.vocab * esz;  // a row of every sequence
-    // about half of a tree's rows have children
+    // About half of a tree's rows have children.  All at once where that is less than two stages and the second one's launch: 16 trees of 31 nodes,
+    // V = 128256 bf16 (130 MB) 39 us a call, 45 in two stages; of 60 nodes (250 MB) 79 and 62; 64 trees of 15 84 and 68.  The first stage's rows are two
+    // of each sequence or kFirstBytes of them (64 trees: one 76, two 68, four 75; 16 trees: two 65, four 62); three stages are slower throughout.
+    double tasks = 2.0 * B;  // rows of a stage
     if (N == 0) {
         r.stages = 0;
-    } else if (pair * (N + 1) * 0.5 <= 2.0 * kStageBytes) {
+    } else if (pair * (N + 1) * 0.5 <= (double)kAllBytes) {
         r.stages = 1;
         r.rows[0] = (int)N + 1;
+        tasks *= (N + 1) * 0.25;
     } else {
-        const int first = pair < kStageBytes ? (int)(kStageBytes / pair) : 1;
-        int left = (int)N + 1, w = first;
-        while (left > 0 && r.stages < kMaxStages - 1 && left > w) {
-            r.rows[r.stages++] = w;
-            left -= w;
-            w = r.stages == 1 ? 2 * first : 2 * w;
-            if (pair < kStageBytes && r.stages == 2) break;
-        }
-        r.rows[r.stages++] = (int)N + 1;
+        const double first = (double)kFirstBytes / pair;
+        r.stages = 2;
+        r.rows[0] = first < 2 ? 2 : first > N ? (int)N : (int)first;
+        r.rows[1] = (int)N + 1;
+        tasks *= r.rows[0];
     }
-    // slices: two workgroups a unit or more from the first stage's rows, 512 vectors each at least
-    const long tasks = 2 * B * (r.stages ? r.rows[0] > 1 && r.stages == 1 ? (r.rows[0] + 1) / 2 : r.rows[0] : 1);
-    long want = (4l * units + tasks - 1) / tasks;
-    const long most = vecs / 512 > 0 ? vecs / 512 : 1;
-    r.slices = (int)(want < 1 ? 1 : want > most ? most : want > 16 ? 16 : want);
+    // about four workgroups a unit in a stage of a few rows, eight in one of all, of 512 vectors each at least (64 trees, two rows first: 4 slices 68 us, 8 75;
+    // 4 trees in one stage: 4 32, 8 29.5)
+    const long want = (long)(4.0 * units / tasks + 0.999), most = vecs / 512 > 0 ? vecs / 512 : 1;
+    r.slices = (int)(want < 1 ? 1 : want > most ? most : want > kMaxParts ? kMaxParts : want);
     r.slice_vecs = (int)((vecs + r.slices - 1) / r.slices);
     for (int k = 0; k < r.stages; ++k) {
         const int rows = r.rows[k] < N + 1 ? r.rows[k] : (int)N + 1;
