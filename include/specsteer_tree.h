@@ -49,7 +49,8 @@ typedef struct {
     int64_t q_stride[3];     /* sequence, row, head of q                                                */
     int64_t k_stride[3];     /* of k; v has the same                                                    */
     int64_t out_stride[3];   /* of out                                                                  */
-    int64_t cache_stride[3]; /* page, slot, head of k_cache; v_cache has the same                       */
+    int64_t cache_stride[3]; /* page, slot, head of k_cache; v_cache has the same.  attention: pages    */
+                             /* and slots less than 2^31 apart                                          */
     int64_t table_stride;    /* of block_table's rows                                                   */
 } ss_tree_params;
 

@@ -52,13 +52,21 @@ __device__ __forceinline__ void load_lds(unsigned to, const char* from) {
 }
 __device__ __forceinline__ unsigned lds_offset(const void* p) { return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) char*)p; }
 
+// The larger of a lane's value and that of the same lane of the other half.
+__device__ __forceinline__ float halves_max(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
 struct AttnArgs {
     const char *q, *k, *v, *kc, *vc;
     const int32_t *table, *cache_len, *parents, *tree_len;
     char* out;
     float* part_o;   // [2 * shares][columns][D]: sums of values of parts
     float2* part_ml; // [2 * shares][columns]: their references and sums of weights
-    Strides3 qs, ks, os, cs;
+    Strides3 qs, ks, os;
+    unsigned page_step, slot_step;  // bytes
+    long head_step;
     long ts;
     int B, N, group, kv_heads, pages, page_size, width, shares;
     float scale;  // |scale| log2(e)
@@ -134,11 +142,11 @@ __device__ __forceinline__ Place find_place(const AttnArgs& a, const TreeTiles& 
     return p;
 }
 
-template <int D_, int WM_, int WK_>
+template <int D_, int WM_, int WK_, int SUB_>
 struct Shape {
     static constexpr int D = D_, WM = WM_, WK = WK_;
     static constexpr int kWaves = WM * WK, kThreads = kWaves * kWave, kColumns = 32 * WM;
-    static constexpr int kSub = 128 / D;             // 32 keys each, of a wave's in a tile
+    static constexpr int kSub = SUB_;                // 32 keys each, of a wave's in a tile
     static constexpr int kTile = 32 * WK * kSub;     // keys
     static constexpr int kLanes = D / 8;             // of 16 bytes each, a row
     static constexpr int kRows = kWave / kLanes;     // rows a load instruction
@@ -233,41 +241,65 @@ __global__ __launch_bounds__(C::kThreads) void attention_kernel(const AttnArgs a
                     up[i + 1] = (unsigned short)(p + 1);
                 }
 
-            // The loads of a tile: this wave's are rows load_row(j).
+            // The loads of a tile: this wave's are rows load_row(j).  Where they lie in the cache goes on from tile to tile without a division.
             const auto load_row = [&](int j) { return (wave * C::kLoads + j) * C::kRows + lane / C::kLanes; };
-            int page[C::kLoads];
-            const auto look_up = [&](int t) {
+            const auto piece_of = [&](int r) { return 16u * ((lane % C::kLanes) ^ turn<D>(r)); };
+            const char *const kc = a.kc + head * a.head_step, *const vc = a.vc + head * a.head_step;
+            const int32_t* const table = a.table + b * a.ts;
+            const int last = s.L > 0 ? (s.L - 1) / a.page_size : 0, last_slot = s.L - 1 - last * a.page_size;
+            const int step_pages = C::kTile / a.page_size, step_slots = C::kTile - step_pages * a.page_size;
+            int column_of[C::kLoads], slot[C::kLoads], page[C::kLoads];  // of the table, of the page, and the page
+#pragma unroll
+            for (int j = 0; j < C::kLoads; ++j) {
+                const int at = t0 * C::kTile + load_row(j);
+                column_of[j] = at / a.page_size;
+                slot[j] = at - column_of[j] * a.page_size;
+            }
+            const auto look_up = [&](int t) {  // once for every tile, in their order
                 if (t < items.cached)
 #pragma unroll
-                    for (int j = 0; j < C::kLoads; ++j) page[j] = a.table[b * a.ts + min(t * C::kTile + load_row(j), s.L - 1) / a.page_size];
+                    for (int j = 0; j < C::kLoads; ++j) page[j] = table[min(column_of[j], last)];
+            };
+            const auto go_on = [&] {
+#pragma unroll
+                for (int j = 0; j < C::kLoads; ++j) {
+                    column_of[j] += step_pages;
+                    slot[j] += step_slots;
+                    if (slot[j] >= a.page_size) {
+                        slot[j] -= a.page_size;
+                        ++column_of[j];
+                    }
+                }
             };
             const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_offset(lds)) + wave * C::kLoads * 1024;
             const auto load = [&](int t, int stage) {
+                const bool cached = t < items.cached;
 #pragma unroll
                 for (int j = 0; j < C::kLoads; ++j) {
-                    const int r = load_row(j), piece = (lane % C::kLanes) ^ turn<D>(r);
+                    const int r = load_row(j);
                     const char *k, *v;
-                    if (t < items.cached) {
-                        const int at = min(t * C::kTile + r, s.L - 1);
-                        int p = page[j];
-                        if (p < 0 || p >= a.pages) {
+                    if (cached) {
+                        // past the end the last key again, which is masked
+                        const int at = t * C::kTile + r < s.L ? slot[j] : last_slot;
+                        unsigned p = (unsigned)page[j];
+                        if (p >= (unsigned)a.pages) {
                             bad = true;
                             p = 0;
                         }
-                        const long off = 2 * (p * a.cs.a + at % a.page_size * a.cs.b + head * a.cs.c) + 16 * piece;
-                        k = a.kc + off;
-                        v = a.vc + off;
+                        const unsigned long off = (unsigned long)p * a.page_step + ((unsigned long)(unsigned)at * a.slot_step + piece_of(r));
+                        k = kc + off;
+                        v = vc + off;
                     } else {
                         const int at = min((t - items.cached) * C::kTile + r, s.N);
-                        const long off = 2 * (b * a.ks.a + at * a.ks.b + head * a.ks.c) + 16 * piece;
+                        const long off = 2 * (b * a.ks.a + at * a.ks.b + head * a.ks.c) + piece_of(r);
                         k = a.k + off;
                         v = a.v + off;
                     }
                     load_lds(lds0 + stage * C::kStage + j * 1024, k);
                     load_lds(lds0 + stage * C::kStage + j * 1024 + C::kTileBytes, v);
                 }
+                if (cached) go_on();
             };
-
             const auto products = [&](auto tree_rows, int t, const char* stage) {
                 constexpr bool own = decltype(tree_rows)::value;  // a tile of the block's own rows, not of the cache
 #pragma unroll
@@ -312,7 +344,7 @@ __global__ __launch_bounds__(C::kThreads) void attention_kernel(const AttnArgs a
                     float top = sc[0];
 #pragma unroll
                     for (int i = 1; i < 16; ++i) top = fmaxf(top, sc[i]);
-                    top = fmaxf(top, __shfl_xor(top, 32, kWave)) * a.scale;
+                    top = halves_max(top) * a.scale;
                     const bool rise = top > m + H::kSlack;
                     if (__ballot(rise)) {
                         const float to = rise ? top : m, by = __builtin_amdgcn_exp2f(m - to);
@@ -385,7 +417,7 @@ __global__ __launch_bounds__(C::kThreads) void attention_kernel(const AttnArgs a
 
             look_up(t0);
             load(t0, 0);
-            look_up(min(t0 + 1, t1 - 1));
+            look_up(t0 + 1);
             const auto step = [&](auto tree_rows, int t) {
                 const int at = (t - t0) & 1;
                 asm volatile("" ::: "memory");
@@ -394,7 +426,7 @@ __global__ __launch_bounds__(C::kThreads) void attention_kernel(const AttnArgs a
                 asm volatile("" ::: "memory");
                 if (t + 1 < t1) {
                     load(t + 1, at ^ 1);
-                    if (t + 2 < t1) look_up(t + 2);
+                    look_up(t + 2);
                 }
                 products(tree_rows, t, lds + at * C::kStage);
             };
@@ -547,13 +579,15 @@ template <typename F>
 auto with_shape(const ss_tree_params& p, F f) {
     const int columns = (p.nodes + 1) * (p.heads / p.kv_heads);
     if (p.head_dim == 64) {
-        if (columns <= 32) return f(Shape<64, 1, 2>{}, 2);
-        if (columns <= 64) return f(Shape<64, 2, 2>{}, 2);
-        return f(Shape<64, 4, 2>{}, 1);
+        if (columns <= 32) return f(Shape<64, 1, 2, 2>{}, 2);
+        if (columns <= 64) return f(Shape<64, 2, 2, 2>{}, 2);
+        if (columns <= 128) return f(Shape<64, 4, 2, 2>{}, 1);
+        return f(Shape<64, 8, 1, 4>{}, 1);
     }
-    if (columns <= 32) return f(Shape<128, 1, 2>{}, 2);
-    if (columns <= 64) return f(Shape<128, 2, 2>{}, 2);
-    return f(Shape<128, 4, 2>{}, 1);
+    if (columns <= 32) return f(Shape<128, 1, 2, 1>{}, 2);
+    if (columns <= 64) return f(Shape<128, 2, 2, 1>{}, 2);
+    if (columns <= 128) return f(Shape<128, 4, 2, 1>{}, 1);
+    return f(Shape<128, 8, 1, 2>{}, 1);
 }
 
 }  // namespace
@@ -597,7 +631,9 @@ ss_status specsteer_tree_attention(const void* q, const void* k, const void* v, 
         a.qs = s.q;
         a.ks = s.k;
         a.os = s.out;
-        a.cs = s.cache;
+        a.page_step = (unsigned)(2 * s.cache.a);
+        a.slot_step = (unsigned)(2 * s.cache.b);
+        a.head_step = 2 * s.cache.c;
         a.ts = s.table;
         a.B = params->batch;
         a.N = params->nodes;

@@ -73,6 +73,7 @@ inline ss_status tree_shape(const ss_tree_params* p, bool attention, TreeShape& 
     const long rows = p->nodes + 1;
     if (!tree_strides(p->k_stride, p->batch, rows, p->kv_heads, p->head_dim, false, s.k)) return SS_ERR_STRIDE;
     if (!tree_strides(p->cache_stride, p->pages, p->page_size, p->kv_heads, p->head_dim, !attention, s.cache)) return SS_ERR_STRIDE;
+    if (attention && ((p->pages > 1 && s.cache.a >= 1l << 31) || (p->page_size > 1 && s.cache.b >= 1l << 31))) return SS_ERR_STRIDE;
     if (attention && (!tree_strides(p->q_stride, p->batch, rows, p->heads, p->head_dim, false, s.q) ||
                       !tree_strides(p->out_stride, p->batch, rows, p->heads, p->head_dim, true, s.out)))
         return SS_ERR_STRIDE;
