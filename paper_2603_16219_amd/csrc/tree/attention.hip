@@ -7,12 +7,10 @@
 // halves, and the lanes that hold P^T's elements are those that have to give them to the second product: rows 8 a + 4 h + i of S^T lie in
 // half h, so that the keys of V^T are read in that order.  The reference m rises only when a score passes it by 2^kSlack, and O is rescaled then.
 //
-// Keys and values go from memory to LDS without registers, a tile ahead; in pieces of 16 bytes whose place in the row depends on the row, which
+// Keys and values go from memory to LDS without registers, half a tile at a time; in pieces of 16 bytes whose place in the row depends on the row, which
 // spreads both the keys' reads and the values' transposed ones over the banks.
 //
 // Bytes: the cache once a call for up to MB columns, whose products take 4 D MB flop for 4 D bytes a key.
-#include <type_traits>
-
 #include "tree_common.h"
 #include "tree_schedule.h"
 
@@ -51,6 +49,43 @@ __device__ __forceinline__ void load_lds(unsigned to, const char* from) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, off" : : "s"(to), "v"(from) : "memory");
 }
 __device__ __forceinline__ unsigned lds_offset(const void* p) { return (unsigned)(uintptr_t)(const __attribute__((address_space(3))) char*)p; }
+
+// Keys or values of a tile are there for all waves when each wave's loads are, of which those of up to HELD - 1 tiles may be on their way still that
+// were asked for behind them: `later` tiles follow this one.
+template <int N>
+__device__ __forceinline__ void wait_loads() {
+    asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
+}
+template <int LOADS, int HELD>
+__device__ __forceinline__ void arrived(int later) {
+    static_assert(2 * LOADS * (HELD - 1) < 64, "what the counter counts");
+    if (later >= HELD - 1) wait_loads<2 * LOADS*(HELD - 1)>();
+    else if (HELD > 4 && later >= 3) wait_loads<2 * LOADS * 3>();
+    else if (HELD > 3 && later >= 2) wait_loads<2 * LOADS * 2>();
+    else if (HELD > 2 && later >= 1) wait_loads<2 * LOADS>();
+    else wait_loads<0>();
+    asm volatile("s_barrier" : : : "memory");
+}
+__device__ __forceinline__ float tree_sum16(const float (&p)[16]) {
+    float s[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) s[i] = p[i] + p[i + 8];
+    return ((s[0] + s[4]) + (s[2] + s[6])) + ((s[1] + s[5]) + (s[3] + s[7]));
+}
+
+// Which of the 32 keys from `base` on a row sees: of the block's own rows itself and its ancestors, of the cache those there are.
+__device__ __forceinline__ unsigned seen_keys(bool own, bool tree, int base, int limit, int row, int N, const unsigned short* up) {
+    if (!own) return limit - base >= 32 ? ~0u : (1u << (limit - base)) - 1;
+    int j = min(row, N);
+    if (!tree) return j < base ? 0u : j - base >= 31 ? ~0u : (2u << (j - base)) - 1;
+    unsigned seen = base == 0 ? 1u : 0u;
+    while (j > base + 31) j = up[j];
+    while (j >= base && j > 0) {
+        seen |= 1u << (j - base);
+        j = up[j];
+    }
+    return seen;
+}
 
 // The larger of a lane's value and that of the same lane of the other half.
 __device__ __forceinline__ float halves_max(float x) {
@@ -142,7 +177,7 @@ __device__ __forceinline__ Place find_place(const AttnArgs& a, const TreeTiles& 
     return p;
 }
 
-template <int D_, int WM_, int WK_, int SUB_>
+template <int D_, int WM_, int WK_, int SUB_, int HELD_>
 struct Shape {
     static constexpr int D = D_, WM = WM_, WK = WK_;
     static constexpr int kWaves = WM * WK, kThreads = kWaves * kWave, kColumns = 32 * WM;
@@ -152,9 +187,11 @@ struct Shape {
     static constexpr int kRows = kWave / kLanes;     // rows a load instruction
     static constexpr int kLoads = kTile / (kRows * kWaves);  // of a wave for the keys of a tile, and for its values
     static constexpr int kRowBytes = 2 * D, kTileBytes = kTile * kRowBytes, kStage = 2 * kTileBytes;
+    static constexpr int kTable = 1024;              // entries of the table in LDS
     static constexpr int kPad = D + 4;               // floats of a column that waves hand over
+    static constexpr int kHeld = HELD_;              // tiles in LDS
     static constexpr int kHand = (WK - 1) * kColumns * kPad * 4;
-    static constexpr int kBuffers = 2 * kStage > kHand ? 2 * kStage : kHand;
+    static constexpr int kBuffers = kHeld * kStage > kHand ? kHeld * kStage : kHand;
 };
 
 // By how much the 16-byte pieces of a row are turned round: 4 rows next to each other that a transposed read takes, and 16 whose same piece is
@@ -173,6 +210,7 @@ __global__ __launch_bounds__(C::kThreads) void attention_kernel(const AttnArgs a
     __shared__ __attribute__((aligned(1024))) char lds[C::kBuffers];
     __shared__ float2 hand_ml[C::WK][C::kColumns];
     __shared__ unsigned short up[SS_MAX_K + 1];
+    __shared__ int table[C::kTable];
     __shared__ long sh[C::kWaves + 2];
     __shared__ int sh_bad;
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -190,10 +228,14 @@ __global__ __launch_bounds__(C::kThreads) void attention_kernel(const AttnArgs a
         }
     }
 
-    long u = 0;
-    const Place place = find_place<C::kThreads>(a, tiles, sh, [&](long total) { return u = share_begin(total, shares_of(a.shares, total), blockIdx.x); });
-    if (u >= place.total) return;
-    const long u_end = share_begin(place.total, shares_of(a.shares, place.total), blockIdx.x + 1);
+    Shares deals{};
+    const Place place = find_place<C::kThreads>(a, tiles, sh, [&](long total) {
+        deals = deal(total, a.shares);
+        return (int)blockIdx.x < deals.shares ? deals.begin(blockIdx.x) : -1l;
+    });
+    if ((int)blockIdx.x >= deals.shares) return;
+    long u = deals.begin(blockIdx.x);
+    const long u_end = deals.begin(blockIdx.x + 1);
     int b = place.b;
     long rel = u - place.before;  // within the sequence
     Sequence s = sequence(a, b);
@@ -231,7 +273,7 @@ __global__ __launch_bounds__(C::kThreads) void attention_kernel(const AttnArgs a
                 if (a.negative) w ^= 0x80008000u;
                 q[i] = __builtin_bit_cast(x8, w);
             }
-            if (t1 > items.cached && a.parents)
+            if (t1 > items.cached && a.parents) {
                 for (int i = tid; i < s.N; i += C::kThreads) {
                     int p = a.parents[(long)b * a.N + i];
                     if (p < -1 || p >= i) {
@@ -240,129 +282,170 @@ __global__ __launch_bounds__(C::kThreads) void attention_kernel(const AttnArgs a
                     }
                     up[i + 1] = (unsigned short)(p + 1);
                 }
+                __syncthreads();
+            }
 
-            // The loads of a tile: this wave's are rows load_row(j).  Where they lie in the cache goes on from tile to tile without a division.
+            // The loads of a tile: this wave's are rows load_row(j).  Where they lie in the cache goes on from tile to tile without a division; the
+            // pages come from a piece of the table in LDS.
             const auto load_row = [&](int j) { return (wave * C::kLoads + j) * C::kRows + lane / C::kLanes; };
             const auto piece_of = [&](int r) { return 16u * ((lane % C::kLanes) ^ turn<D>(r)); };
-            const char *const kc = a.kc + head * a.head_step, *const vc = a.vc + head * a.head_step;
-            const int32_t* const table = a.table + b * a.ts;
             const int last = s.L > 0 ? (s.L - 1) / a.page_size : 0, last_slot = s.L - 1 - last * a.page_size;
             const int step_pages = C::kTile / a.page_size, step_slots = C::kTile - step_pages * a.page_size;
-            int column_of[C::kLoads], slot[C::kLoads], page[C::kLoads];  // of the table, of the page, and the page
+            int column_of[C::kLoads], slot[C::kLoads];  // of the table, of the page
 #pragma unroll
             for (int j = 0; j < C::kLoads; ++j) {
                 const int at = t0 * C::kTile + load_row(j);
                 column_of[j] = at / a.page_size;
                 slot[j] = at - column_of[j] * a.page_size;
             }
-            const auto look_up = [&](int t) {  // once for every tile, in their order
-                if (t < items.cached)
-#pragma unroll
-                    for (int j = 0; j < C::kLoads; ++j) page[j] = table[min(column_of[j], last)];
-            };
-            const auto go_on = [&] {
-#pragma unroll
-                for (int j = 0; j < C::kLoads; ++j) {
-                    column_of[j] += step_pages;
-                    slot[j] += step_slots;
-                    if (slot[j] >= a.page_size) {
-                        slot[j] -= a.page_size;
-                        ++column_of[j];
+            int table_from = 0, table_until = t0;  // the column that table[0] is, the tile up to which they are there
+            const auto look_up = [&](int t) {
+                if (t >= items.cached || t < table_until) return;
+                __syncthreads();
+                table_from = (int)((long)t * C::kTile / a.page_size);
+                const int until = min(last, (int)(((long)min(t1, items.cached) * C::kTile - 1) / a.page_size));
+                for (int i = tid; i < C::kTable && table_from + i <= until; i += C::kThreads) {
+                    int p = a.table[b * a.ts + table_from + i];
+                    if (p < 0 || p >= a.pages) {
+                        bad = true;
+                        p = 0;
                     }
+                    table[i] = p;
                 }
+                const long more = ((long)(table_from + C::kTable) * a.page_size - (long)t * C::kTile) / C::kTile;
+                table_until = more < items.cached ? t + (int)more : items.cached;
+                __syncthreads();
             };
+            const char* from[C::kLoads];  // of the keys that were asked for last; their values lie as far from the values' array
             const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_offset(lds)) + wave * C::kLoads * 1024;
-            const auto load = [&](int t, int stage) {
+            const auto load_keys = [&](int t, int stage) {
                 const bool cached = t < items.cached;
+                if (cached) {
+                    const char* const base = a.kc + head * a.head_step;
 #pragma unroll
-                for (int j = 0; j < C::kLoads; ++j) {
-                    const int r = load_row(j);
-                    const char *k, *v;
-                    if (cached) {
+                    for (int j = 0; j < C::kLoads; ++j) {
                         // past the end the last key again, which is masked
-                        const int at = t * C::kTile + r < s.L ? slot[j] : last_slot;
-                        unsigned p = (unsigned)page[j];
-                        if (p >= (unsigned)a.pages) {
-                            bad = true;
-                            p = 0;
+                        const bool in = t * C::kTile + load_row(j) < s.L;
+                        const unsigned p = (unsigned)table[(in ? column_of[j] : last) - table_from], at = (unsigned)(in ? slot[j] : last_slot);
+                        from[j] = base + ((unsigned long)p * a.page_step + ((unsigned long)at * a.slot_step + piece_of(load_row(j))));
+                        column_of[j] += step_pages;
+                        slot[j] += step_slots;
+                        if (slot[j] >= a.page_size) {
+                            slot[j] -= a.page_size;
+                            ++column_of[j];
                         }
-                        const unsigned long off = (unsigned long)p * a.page_step + ((unsigned long)(unsigned)at * a.slot_step + piece_of(r));
-                        k = kc + off;
-                        v = vc + off;
-                    } else {
-                        const int at = min((t - items.cached) * C::kTile + r, s.N);
-                        const long off = 2 * (b * a.ks.a + at * a.ks.b + head * a.ks.c) + piece_of(r);
-                        k = a.k + off;
-                        v = a.v + off;
                     }
-                    load_lds(lds0 + stage * C::kStage + j * 1024, k);
-                    load_lds(lds0 + stage * C::kStage + j * 1024 + C::kTileBytes, v);
+                } else {
+                    const char* const base = a.k + 2 * (b * a.ks.a + head * a.ks.c);
+#pragma unroll
+                    for (int j = 0; j < C::kLoads; ++j)
+                        from[j] = base + 2 * (min((t - items.cached) * C::kTile + load_row(j), s.N) * a.ks.b) + piece_of(load_row(j));
                 }
-                if (cached) go_on();
+#pragma unroll
+                for (int j = 0; j < C::kLoads; ++j) load_lds(lds0 + stage * C::kStage + j * 1024, from[j]);
             };
-            const auto products = [&](auto tree_rows, int t, const char* stage) {
-                constexpr bool own = decltype(tree_rows)::value;  // a tile of the block's own rows, not of the cache
+            const auto load_values = [&](int t, int stage) {
+                const long by = t < items.cached ? a.vc - a.kc : a.v - a.k;
+#pragma unroll
+                for (int j = 0; j < C::kLoads; ++j) load_lds(lds0 + stage * C::kStage + j * 1024 + C::kTileBytes, from[j] + by);
+            };
+
+            // kHeld tiles are held, and half a tile is asked for as soon as its place is free: values of t + kHeld - 1 behind the products with the
+            // values of t - 1, keys of t + kHeld behind those with the keys of t.  All but one of the halves are on their way at any time.
+            constexpr int kAhead = C::kHeld - 1;
+#pragma unroll
+            for (int i = 0; i < C::kHeld; ++i)
+                if (t0 + i < t1) {
+                    look_up(t0 + i);
+                    load_keys(t0 + i, i);
+                    if (i < kAhead) load_values(t0 + i, i);
+                }
+            int at = 0;  // the place of tile t
+            for (int t = t0; t < t1; ++t) {
+                const bool own = t >= items.cached;  // a tile of the block's own rows, not of the cache
+                const char* const stage = lds + at * C::kStage;
+                const int limit = own ? s.N + 1 : s.L, base0 = (own ? t - items.cached : t) * C::kTile + wk * C::kSub * 32;
+                arrived<C::kLoads, C::kHeld>(t1 - 1 - t);
+                if (t + kAhead < t1) load_values(t + kAhead, at > 0 ? at - 1 : kAhead);
+                x8 weights[C::kSub][2];
+                f32x16 sc[C::kSub];
+                float top = -__builtin_huge_valf();
 #pragma unroll
                 for (int sub = 0; sub < C::kSub; ++sub) {
-                    const int key0 = (wk * C::kSub + sub) * 32;  // of the tile
-                    const char* const kt = stage + key0 * C::kRowBytes;
-                    const char* const vt = kt + C::kTileBytes;
-                    const int base = own ? (t - items.cached) * C::kTile + key0 : t * C::kTile + key0;  // of the block's rows, of the cache
-                    const int limit = own ? s.N + 1 : s.L;
+                    const int base = base0 + sub * 32;  // of the block's rows, or of the cache
                     if (base >= limit) continue;
-                    f32x16 sc = {};
-                    {
-                        const int r = lane & 31;
-                        const char* const kr = kt + r * C::kRowBytes;
-                        const int x = half ^ turn<D>(r);
+                    sc[sub] = f32x16{};
+                    const int r = lane & 31;
+                    const char* const kr = stage + ((wk * C::kSub + sub) * 32 + r) * C::kRowBytes;
+                    const int x = half ^ turn<D>(r);
 #pragma unroll
-                        for (int i = 0; i < kSteps; ++i) sc = mfma<DT>(*reinterpret_cast<const x8*>(kr + ((2 * i) ^ x) * 16), q[i], sc);
-                    }
-                    unsigned seen = ~0u;  // keys of these 32
-                    if (own) {
-                        seen = 0;
-                        if (!a.parents) {
-                            if (row >= base) seen = row - base >= 31 ? ~0u : (2u << (row - base)) - 1;
-                        } else {
-                            int j = min(row, s.N);
-                            while (j > base + 31) j = up[j];
-                            while (j >= base && j > 0) {
-                                seen |= 1u << (j - base);
-                                j = up[j];
-                            }
-                            if (base == 0) seen |= 1u;
-                        }
-                    } else if (base + 32 > limit) {
-                        seen = (1u << (limit - base)) - 1;
-                    }
+                    for (int i = 0; i < kSteps; ++i) sc[sub] = mfma<DT>(*reinterpret_cast<const x8*>(kr + ((2 * i) ^ x) * 16), q[i], sc[sub]);
                     if (own || base + 32 > limit) {
-                        const unsigned mine = seen >> (4 * half);
+                        const unsigned mine = seen_keys(own, a.parents != nullptr, base, limit, row, s.N, up) >> (4 * half);
 #pragma unroll
                         for (int i = 0; i < 16; ++i)
-                            if (!(mine >> (8 * (i / 4) + i % 4) & 1)) sc[i] = -__builtin_huge_valf();
+                            if (!(mine >> (8 * (i / 4) + i % 4) & 1)) sc[sub][i] = -__builtin_huge_valf();
                     }
-                    float top = sc[0];
 #pragma unroll
-                    for (int i = 1; i < 16; ++i) top = fmaxf(top, sc[i]);
-                    top = halves_max(top) * a.scale;
-                    const bool rise = top > m + H::kSlack;
-                    if (__ballot(rise)) {
-                        const float to = rise ? top : m, by = __builtin_amdgcn_exp2f(m - to);
-                        m = to;
-                        l *= by;
+                    for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[sub][i]);
+                }
+                // one reference for all weights of the tile, which are products only later
+                top = halves_max(top) * a.scale;
+                const bool rise = top > m + H::kSlack;
+                if (__ballot(rise)) {
+                    const float to = rise ? top : m, by = __builtin_amdgcn_exp2f(m - to);
+                    m = to;
+                    l *= by;
 #pragma unroll
-                        for (int i = 0; i < kBlocks; ++i) o[i] *= by;
-                    }
-                    const float ref = H::kLift - m;
+                    for (int i = 0; i < kBlocks; ++i) o[i] *= by;
+                }
+                const float ref = H::kLift - m;
+#pragma unroll
+                for (int sub = 0; sub < C::kSub; ++sub) {
+                    if (base0 + sub * 32 >= limit) continue;
                     float p[16];
 #pragma unroll
                     for (int i = 0; i < 16; ++i) {
-                        p[i] = __builtin_amdgcn_exp2f(fmaf(sc[i], a.scale, ref));
-                        l += p[i];
+                        p[i] = __builtin_amdgcn_exp2f(fmaf(sc[sub][i], a.scale, ref));
+                        weights[sub][i / 8][i % 8] = (typename H::T)p[i];
                     }
-                    x8 pb[2];
+                    l += tree_sum16(p);
+                }
+                arrived<C::kLoads, C::kHeld>(t1 - 1 - t);
+                if (own) {
+                    // Values of the block that are not finite count for the rows that see them alone, which have NaN; a product with a weight of 0 is none
+                    unsigned odd[C::kSub] = {};
 #pragma unroll
-                    for (int i = 0; i < 16; ++i) pb[i / 8][i % 8] = (typename H::T)p[i];
+                    for (int sub = 0; sub < C::kSub; ++sub) {
+                        const char* const vr = stage + C::kTileBytes + ((wk * C::kSub + sub) * 32 + (lane & 31)) * C::kRowBytes + half * D;
+                        bool is = false;
+                        for (int i = 0; i < D / 4; ++i) {
+                            const unsigned w = reinterpret_cast<const unsigned*>(vr)[i];
+                            is = is || (w & H::kExponent) == H::kExponent || (w >> 16 & H::kExponent) == H::kExponent;
+                        }
+                        const unsigned long long ballot = __ballot(is);
+                        odd[sub] = (unsigned)ballot | (unsigned)(ballot >> 32);
+                        if (odd[sub] && base0 + sub * 32 < limit &&
+                            (odd[sub] & seen_keys(true, a.parents != nullptr, base0 + sub * 32, limit, row, s.N, up)))
+                            l = __builtin_nanf("");
+                    }
+                    __syncthreads();  // other waves look at the same values
+#pragma unroll
+                    for (int sub = 0; sub < C::kSub; ++sub)
+                        if (odd[sub] >> (lane & 31) & 1) {
+                            char* const vr = lds + at * C::kStage + C::kTileBytes + ((wk * C::kSub + sub) * 32 + (lane & 31)) * C::kRowBytes + half * D;
+                            for (int i = 0; i < D / 4; ++i) reinterpret_cast<unsigned*>(vr)[i] = 0;
+                        }
+                    __syncthreads();
+                }
+                if (t + C::kHeld < t1) {
+                    look_up(t + C::kHeld);
+                    load_keys(t + C::kHeld, at);
+                }
+#pragma unroll
+                for (int sub = 0; sub < C::kSub; ++sub) {
+                    if (base0 + sub * 32 >= limit) continue;
+                    const char* const vt = stage + C::kTileBytes + (wk * C::kSub + sub) * 32 * C::kRowBytes;
                     // the values, transposed: 4 keys of a column each read
                     const int q4 = (lane & 15) >> 2, wide = lane >> 4 & 1;
 #pragma unroll
@@ -372,67 +455,18 @@ __global__ __launch_bounds__(C::kThreads) void attention_kernel(const AttnArgs a
                             union {
                                 s16x4 h[2];
                                 x8 all;
-                                unsigned short e[8];
                             } vf;
 #pragma unroll
                             for (int j = 0; j < 2; ++j) {
                                 const int r = 16 * kb + 8 * j + 4 * half + q4, piece = db * 4 + 2 * wide + ((lane & 3) >> 1);
                                 vf.h[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(vt + r * C::kRowBytes + (piece ^ turn<D>(r)) * 16 + (lane & 1) * 8));
                             }
-                            if (own) {  // what is not finite is taken apart, below
-#pragma unroll
-                                for (int j = 0; j < 8; ++j)
-                                    if ((vf.e[j] & H::kExponent) == H::kExponent) vf.e[j] = 0;
-                            }
-                            o[db] = mfma<DT>(vf.all, pb[kb], o[db]);
-                        }
-                    }
-                    if (own) {
-                        // Values of the block that are not finite count for the rows that see them alone: a product with a weight of 0 is none
-                        for (int r = 0; r < 32; ++r) {
-                            const char* const vr = vt + r * C::kRowBytes;
-                            bool odd = false;
-                            if (lane < D / 2) {
-                                const unsigned w = reinterpret_cast<const unsigned*>(vr)[lane];
-                                odd = (w & H::kExponent) == H::kExponent || (w >> 16 & H::kExponent) == H::kExponent;
-                            }
-                            if (!__ballot(odd) || base + r >= limit) continue;
-                            float w = 0.f;
-#pragma unroll
-                            for (int i = 0; i < 16; ++i) w = (8 * (i / 4) + i % 4) == (r & ~4) ? p[i] : w;
-                            w = __shfl(w, (lane & 31) + ((r & 4) << 3), kWave);
-#pragma unroll
-                            for (int db = 0; db < kBlocks; ++db)
-#pragma unroll
-                                for (int i = 0; i < 16; ++i) {
-                                    const int d = db * 32 + 8 * (i / 4) + 4 * half + i % 4;
-                                    const typename H::T e = *reinterpret_cast<const typename H::T*>(vr + ((d / 8) ^ turn<D>(r)) * 16 + (d % 8) * 2);
-                                    const bool finite = (__builtin_bit_cast(unsigned short, e) & H::kExponent) != H::kExponent;
-                                    if (!finite && (seen >> r & 1)) o[db][i] += w * (float)e;
-                                }
+                            o[db] = mfma<DT>(vf.all, weights[sub][kb], o[db]);
                         }
                     }
                 }
-            };
-
-            look_up(t0);
-            load(t0, 0);
-            look_up(t0 + 1);
-            const auto step = [&](auto tree_rows, int t) {
-                const int at = (t - t0) & 1;
-                asm volatile("" ::: "memory");
-                __builtin_amdgcn_s_waitcnt(0);
-                __builtin_amdgcn_s_barrier();
-                asm volatile("" ::: "memory");
-                if (t + 1 < t1) {
-                    load(t + 1, at ^ 1);
-                    look_up(t + 2);
-                }
-                products(tree_rows, t, lds + at * C::kStage);
-            };
-            int t = t0;
-            for (; t < min(t1, items.cached); ++t) step(std::false_type{}, t);
-            for (; t < t1; ++t) step(std::true_type{}, t);
+                at = at == kAhead ? 0 : at + 1;
+            }
             l += __shfl_xor(l, 32, kWave);
         }
         if (bad) sh_bad = 1;
@@ -516,10 +550,13 @@ __global__ __launch_bounds__(kJoinThreads) void attention_join_kernel(const Attn
     __shared__ long sh[kJoinThreads / kWave + 2];
     const int w = blockIdx.x + 1, tid = threadIdx.x;
     const TreeTiles tiles{C::kTile, C::kColumns, a.group, a.kv_heads};
-    long u = 0;
-    const Place place = find_place<kJoinThreads>(a, tiles, sh, [&](long total) { return u = share_begin(total, shares_of(a.shares, total), w); });
-    if (u >= place.total) return;
-    const int shares = shares_of(a.shares, place.total);
+    Shares deals{};
+    const Place place = find_place<kJoinThreads>(a, tiles, sh, [&](long total) {
+        deals = deal(total, a.shares);
+        return w < deals.shares ? deals.begin(w) : -1l;
+    });
+    if (w >= deals.shares) return;
+    const long u = deals.begin(w);
     const int b = place.b;
     const Sequence s = sequence(a, b);
     const TreeItems items = tree_items(tiles, s.L, s.N, s.bad, a.N);
@@ -527,24 +564,27 @@ __global__ __launch_bounds__(kJoinThreads) void attention_join_kernel(const Attn
     const long rel = u - place.before;
     const int item = (int)(rel / nt), t0 = (int)(rel - (long)item * nt);
     const long start = u - t0, end = start + nt;
-    if (t0 == 0 || share_begin(place.total, shares, w - 1) > start) return;  // it is cut before this already
+    if (t0 == 0 || deals.begin(w - 1) > start) return;  // it is cut before this already
     const int head = item / items.blocks, block = item - head * items.blocks;
     const int rows = (s.bad ? a.N : s.N) + 1;
     for (int i = tid / kLanes; i < kJoinColumns; i += kAtOnce) {
         const int of_block = blockIdx.y * kJoinColumns + i, column = block * C::kColumns + of_block, row = column / a.group;
         if (of_block >= C::kColumns || row >= rows) break;
+        // the share before has the item's first part, in its second slot unless it begins with the item
+        const auto at = [&](int x) { return (2l * x + (x >= w || deals.begin(x) == start ? 0 : 1)) * C::kColumns + of_block; };
+        int x_end = w;
+        while (x_end < deals.shares && deals.begin(x_end) < end) ++x_end;
         float m = -1e30f, l = 0.f;
+#pragma unroll 4
+        for (int x = w - 1; x < x_end; ++x) m = fmaxf(m, a.part_ml[at(x)].x);
         f32v4 o = {};
-        for (int x = w - 1; x < shares; ++x) {
-            const long from = share_begin(place.total, shares, x);
-            if (from >= end) break;
-            const long c = (2l * x + (from >= start ? 0 : 1)) * C::kColumns + of_block;
-            const float2 ml = a.part_ml[c];
-            const f32v4 v = *reinterpret_cast<const f32v4*>(a.part_o + c * D + 4 * (tid % kLanes));
-            const float top = fmaxf(m, ml.x), by = __builtin_amdgcn_exp2f(m - top), f = __builtin_amdgcn_exp2f(ml.x - top);
-            l = fmaf(l, by, ml.y * f);
-            o = o * by + v * f;
-            m = top;
+#pragma unroll 4
+        for (int x = w - 1; x < x_end; ++x) {
+            const float2 ml = a.part_ml[at(x)];
+            const f32v4 v = *reinterpret_cast<const f32v4*>(a.part_o + at(x) * D + 4 * (tid % kLanes));
+            const float f = __builtin_amdgcn_exp2f(ml.x - m);
+            l = fmaf(ml.y, f, l);
+            o += v * f;
         }
         typename H::T r[4];
 #pragma unroll
@@ -568,6 +608,7 @@ AttnPlan plan_for(const ss_tree_params& p, int groups_a_unit) {
     AttnPlan r;
     r.columns = C::kColumns;
     r.shares = device_cu_count() * groups_a_unit;
+    if (r.shares > kMaxShares) r.shares = kMaxShares;
     if (units < r.shares) r.shares = units < 1 ? 1 : (int)units;
     const size_t slots = 2 * (size_t)r.shares * C::kColumns;
     r.off_ml = slots * C::D * 4;
@@ -579,15 +620,15 @@ template <typename F>
 auto with_shape(const ss_tree_params& p, F f) {
     const int columns = (p.nodes + 1) * (p.heads / p.kv_heads);
     if (p.head_dim == 64) {
-        if (columns <= 32) return f(Shape<64, 1, 2, 2>{}, 2);
-        if (columns <= 64) return f(Shape<64, 2, 2, 2>{}, 2);
-        if (columns <= 128) return f(Shape<64, 4, 2, 2>{}, 1);
-        return f(Shape<64, 8, 1, 4>{}, 1);
+        if (columns <= 32) return f(Shape<64, 1, 2, 1, 4>{}, 2);
+        if (columns <= 64) return f(Shape<64, 2, 2, 1, 4>{}, 2);
+        if (columns <= 128) return f(Shape<64, 4, 2, 1, 5>{}, 1);
+        return f(Shape<64, 8, 1, 2, 5>{}, 1);
     }
-    if (columns <= 32) return f(Shape<128, 1, 2, 1>{}, 2);
-    if (columns <= 64) return f(Shape<128, 2, 2, 1>{}, 2);
-    if (columns <= 128) return f(Shape<128, 4, 2, 1>{}, 1);
-    return f(Shape<128, 8, 1, 2>{}, 1);
+    if (columns <= 32) return f(Shape<128, 1, 2, 1, 2>{}, 2);
+    if (columns <= 64) return f(Shape<128, 2, 2, 1, 2>{}, 2);
+    if (columns <= 128) return f(Shape<128, 4, 2, 1, 4>{}, 1);
+    return f(Shape<128, 8, 1, 1, 5>{}, 1);
 }
 
 }  // namespace

@@ -8,6 +8,9 @@
 // launch joins those of the item that the share's beginning cuts, if it is the first to do so.
 #pragma once
 
+// begin() multiplies two numbers of shares in 32 bits
+constexpr int kMaxShares = 1 << 15;
+
 #ifdef __HIPCC__
 #define SS_TREE_BOTH __host__ __device__ __forceinline__
 #else
@@ -38,9 +41,18 @@ SS_TREE_BOTH TreeItems tree_items(const TreeTiles& t, int length, int nodes, boo
 }
 // No share is empty.
 SS_TREE_BOTH int shares_of(int most, long units) { return units < most ? (int)units : most; }
-SS_TREE_BOTH long share_begin(long units, int shares, int w) {
-    const long q = units / shares, r = units % shares;  // units * shares may pass 64 bits
-    return q * w + r * w / shares;
+struct Shares {
+    long each;   // units of a share,
+    int more;    // and one more of these of them, spread out
+    int shares;
+    SS_TREE_BOTH long begin(int w) const { return each * w + (long)((unsigned)more * (unsigned)w / (unsigned)shares); }
+};
+SS_TREE_BOTH Shares deal(long units, int most) {
+    Shares r;
+    r.shares = shares_of(most, units);
+    r.each = r.shares ? units / r.shares : 0;
+    r.more = (int)(units - r.each * r.shares);
+    return r;
 }
 
 }  // namespace

@@ -226,7 +226,7 @@ def test_bad_data_marks_its_sequence_alone(tree, what):
     for N, Hq, L in ((6, 4, 300), (50, 8, 1500)):
         i = make(3, N, Hq, 2, 128, [L, L - 50, L], 16, ragged=True, seed=9)
         i["tree_len"][1] = N
-        want = run(tree, i)
+        want, bound = R.attention(*(i[k] for k in ("q", "k", "v", "k_cache", "v_cache", "table", "cache_len", "parents", "tree_len")), 1 / math.sqrt(128))
         width = i["table"].shape[1]
         at, v = {"cache_len": ("cache_len", width * 16 + 1), "negative_len": ("cache_len", -1), "tree_len": ("tree_len", N + 1), "negative_tree": ("tree_len", -3),
                  "parent": ("parents", N - 1), "self_parent": ("parents", 2), "low_parent": ("parents", -2), "page": ("table", i["k_cache"].shape[0]),
@@ -236,7 +236,8 @@ def test_bad_data_marks_its_sequence_alone(tree, what):
         else:
             i[at][1, {"parent": N - 2, "late_page": (L - 51) // 16}.get(what, 2)] = v
         got = run(tree, i)
-        assert got[1].isnan().all() and torch.equal(got[0], want[0]) and torch.equal(got[2], want[2])
+        assert got[1].isnan().all()
+        close(got[::2], want[::2], bound[::2], "the others")  # lengths say where all sequences' sums are cut
 
 
 def test_pages_and_parents_that_are_not_needed_may_be_anything(tree):
