@@ -56,7 +56,7 @@ template <int N>
 __device__ __forceinline__ void wait_loads() {
     asm volatile("s_waitcnt vmcnt(%0)" : : "n"(N) : "memory");
 }
-template <int LOADS, int HELD>
+template <int LOADS, int HELD, bool SHARED>
 __device__ __forceinline__ void arrived(int later) {
     static_assert(2 * LOADS * (HELD - 1) < 64, "what the counter counts");
     if (later >= HELD - 1) wait_loads<2 * LOADS*(HELD - 1)>();
@@ -64,7 +64,7 @@ __device__ __forceinline__ void arrived(int later) {
     else if (HELD > 3 && later >= 2) wait_loads<2 * LOADS * 2>();
     else if (HELD > 2 && later >= 1) wait_loads<2 * LOADS>();
     else wait_loads<0>();
-    asm volatile("s_barrier" : : : "memory");
+    if (SHARED) asm volatile("s_barrier" : : : "memory");
 }
 __device__ __forceinline__ float tree_sum16(const float (&p)[16]) {
     float s[8];
@@ -101,6 +101,8 @@ struct AttnArgs {
     float2* part_ml; // [2 * shares][columns]: their references and sums of weights
     Strides3 qs, ks, os;
     unsigned page_step, slot_step;  // bytes
+    unsigned page_mul;              // a position's page: the upper half of its product with this, shifted; or 0 for pages of one
+    int page_shift;
     long head_step;
     long ts;
     int B, N, group, kv_heads, pages, page_size, width, shares;
@@ -177,19 +179,19 @@ __device__ __forceinline__ Place find_place(const AttnArgs& a, const TreeTiles& 
     return p;
 }
 
-template <int D_, int WM_, int WK_, int SUB_, int HELD_>
+// A workgroup of WM x WK waves: each takes NC blocks of 32 columns and 32 keys of a tile; waves of the same columns take turns at the keys.
+template <int D_, int NC_, int WM_, int WK_, int HELD_>
 struct Shape {
-    static constexpr int D = D_, WM = WM_, WK = WK_;
-    static constexpr int kWaves = WM * WK, kThreads = kWaves * kWave, kColumns = 32 * WM;
-    static constexpr int kSub = SUB_;                // 32 keys each, of a wave's in a tile
-    static constexpr int kTile = 32 * WK * kSub;     // keys
+    static constexpr int D = D_, NC = NC_, WM = WM_, WK = WK_;
+    static constexpr int kWaves = WM * WK, kThreads = kWaves * kWave, kColumns = 32 * NC * WM;
+    static constexpr int kTile = 32 * WK;            // keys
     static constexpr int kLanes = D / 8;             // of 16 bytes each, a row
     static constexpr int kRows = kWave / kLanes;     // rows a load instruction
-    static constexpr int kLoads = kTile / (kRows * kWaves);  // of a wave for the keys of a tile, and for its values
+    static constexpr int kLoads = 32 / (kRows * WM); // of a wave for the keys of a tile, and for its values; with one wave over the columns its own
     static constexpr int kRowBytes = 2 * D, kTileBytes = kTile * kRowBytes, kStage = 2 * kTileBytes;
+    static constexpr int kHeld = HELD_;              // tiles in LDS
     static constexpr int kTable = 1024;              // entries of the table in LDS
     static constexpr int kPad = D + 4;               // floats of a column that waves hand over
-    static constexpr int kHeld = HELD_;              // tiles in LDS
     static constexpr int kHand = (WK - 1) * kColumns * kPad * 4;
     static constexpr int kBuffers = kHeld * kStage > kHand ? kHeld * kStage : kHand;
 };
@@ -203,10 +205,10 @@ __device__ __forceinline__ int turn(int row) {
 }
 
 template <int DT, typename C>
-__global__ __launch_bounds__(C::kThreads) void attention_kernel(const AttnArgs a) {
+__global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void attention_kernel(const AttnArgs a) {
     using H = Half<DT>;
     using x8 = typename H::x8;
-    constexpr int D = C::D, kBlocks = D / 32, kSteps = D / 16;
+    constexpr int D = C::D, NC = C::NC, kBlocks = D / 32, kSteps = D / 16;
     __shared__ __attribute__((aligned(1024))) char lds[C::kBuffers];
     __shared__ float2 hand_ml[C::WK][C::kColumns];
     __shared__ unsigned short up[SS_MAX_K + 1];
@@ -251,27 +253,41 @@ __global__ __launch_bounds__(C::kThreads) void attention_kernel(const AttnArgs a
         const int nt = items.tiles();
         const int item = (int)(rel / nt), t0 = (int)(rel - (long)item * nt), t1 = (int)min((long)nt, t0 + (u_end - u));
         const int head = item / items.blocks, block = item - head * items.blocks;
-        // this lane's column
-        const int column = block * C::kColumns + wm * 32 + (lane & 31);
-        const int rows = (s.bad ? a.N : s.N) + 1, row = column / a.group, of_group = column - row * a.group;
-        const bool valid = row < rows;
+        // this lane's columns
+        const int rows = (s.bad ? a.N : s.N) + 1;
+        int row[NC], query[NC], place_of[NC];  // a tree's row, the query head, the column of the block
+#pragma unroll
+        for (int c = 0; c < NC; ++c) {
+            place_of[c] = (wm * NC + c) * 32 + (lane & 31);
+            const int column = block * C::kColumns + place_of[c];
+            row[c] = column / a.group;
+            query[c] = head * a.group + column - row[c] * a.group;
+        }
         const bool whole = t0 == 0 && t1 == nt;
         bool bad = s.bad;
 
-        f32x16 o[kBlocks];
-        float m = -1e30f, l = 0.f;
+        f32x16 o[NC][kBlocks];
+        float m[NC], l[NC];
 #pragma unroll
-        for (int i = 0; i < kBlocks; ++i) o[i] = f32x16{};
+        for (int c = 0; c < NC; ++c) {
+            m[c] = -1e30f;
+            l[c] = 0.f;
+#pragma unroll
+            for (int i = 0; i < kBlocks; ++i) o[c][i] = f32x16{};
+        }
         __syncthreads();  // the last item's hand-over is done with
         if (tid == 0) sh_bad = 0;
         if (!s.bad) {
-            x8 q[kSteps];
-            const char* const qp = a.q + 2 * (b * a.qs.a + min(row, s.N) * a.qs.b + (head * a.group + of_group) * a.qs.c) + 16 * half;
+            x8 q[NC][kSteps];
 #pragma unroll
-            for (int i = 0; i < kSteps; ++i) {
-                u32v4 w = *reinterpret_cast<const u32v4*>(qp + 32 * i);
-                if (a.negative) w ^= 0x80008000u;
-                q[i] = __builtin_bit_cast(x8, w);
+            for (int c = 0; c < NC; ++c) {
+                const char* const qp = a.q + 2 * (b * a.qs.a + min(row[c], s.N) * a.qs.b + query[c] * a.qs.c) + 16 * half;
+#pragma unroll
+                for (int i = 0; i < kSteps; ++i) {
+                    u32v4 w = *reinterpret_cast<const u32v4*>(qp + 32 * i);
+                    if (a.negative) w ^= 0x80008000u;
+                    q[c][i] = __builtin_bit_cast(x8, w);
+                }
             }
             if (t1 > items.cached && a.parents) {
                 for (int i = tid; i < s.N; i += C::kThreads) {
@@ -285,19 +301,11 @@ __global__ __launch_bounds__(C::kThreads) void attention_kernel(const AttnArgs a
                 __syncthreads();
             }
 
-            // The loads of a tile: this wave's are rows load_row(j).  Where they lie in the cache goes on from tile to tile without a division; the
-            // pages come from a piece of the table in LDS.
-            const auto load_row = [&](int j) { return (wave * C::kLoads + j) * C::kRows + lane / C::kLanes; };
-            const auto piece_of = [&](int r) { return 16u * ((lane % C::kLanes) ^ turn<D>(r)); };
-            const int last = s.L > 0 ? (s.L - 1) / a.page_size : 0, last_slot = s.L - 1 - last * a.page_size;
-            const int step_pages = C::kTile / a.page_size, step_slots = C::kTile - step_pages * a.page_size;
-            int column_of[C::kLoads], slot[C::kLoads];  // of the table, of the page
-#pragma unroll
-            for (int j = 0; j < C::kLoads; ++j) {
-                const int at = t0 * C::kTile + load_row(j);
-                column_of[j] = at / a.page_size;
-                slot[j] = at - column_of[j] * a.page_size;
-            }
+            // The rows of a tile that this wave loads are kMine from first_row on.  A lane finds where one of them lies, and those that load its pieces
+            // ask for that: the arithmetic once for all rows, whatever the pages' size.  The pages come from a piece of the table in LDS.
+            constexpr int kMine = C::kLoads * C::kRows;
+            const int first_row = wave * kMine, my_row = first_row + lane % kMine;
+            const int last = s.L > 0 ? (s.L - 1) / a.page_size : 0;
             int table_from = 0, table_until = t0;  // the column that table[0] is, the tile up to which they are there
             const auto look_up = [&](int t) {
                 if (t >= items.cached || t < table_until) return;
@@ -316,222 +324,222 @@ __global__ __launch_bounds__(C::kThreads) void attention_kernel(const AttnArgs a
                 table_until = more < items.cached ? t + (int)more : items.cached;
                 __syncthreads();
             };
-            const char* from[C::kLoads];  // of the keys that were asked for last; their values lie as far from the values' array
-            const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_offset(lds)) + wave * C::kLoads * 1024;
-            const auto load_keys = [&](int t, int stage) {
-                const bool cached = t < items.cached;
-                if (cached) {
-                    const char* const base = a.kc + head * a.head_step;
-#pragma unroll
-                    for (int j = 0; j < C::kLoads; ++j) {
-                        // past the end the last key again, which is masked
-                        const bool in = t * C::kTile + load_row(j) < s.L;
-                        const unsigned p = (unsigned)table[(in ? column_of[j] : last) - table_from], at = (unsigned)(in ? slot[j] : last_slot);
-                        from[j] = base + ((unsigned long)p * a.page_step + ((unsigned long)at * a.slot_step + piece_of(load_row(j))));
-                        column_of[j] += step_pages;
-                        slot[j] += step_slots;
-                        if (slot[j] >= a.page_size) {
-                            slot[j] -= a.page_size;
-                            ++column_of[j];
-                        }
-                    }
+            unsigned long of_row = 0;  // the address of this lane's row, of the keys of the tile that is asked for next or was last
+            const unsigned long first_key = reinterpret_cast<uintptr_t>(a.kc) + head * a.head_step, first_own = reinterpret_cast<uintptr_t>(a.k) + 2 * (b * a.ks.a + head * a.ks.c);
+            const auto locate = [&](int t) {
+                if (t < items.cached) {
+                    look_up(t);
+                    const unsigned pos = (unsigned)min(t * C::kTile + my_row, s.L - 1);  // past the end the last key again, which is masked
+                    const unsigned col = a.page_mul ? __umulhi(pos, a.page_mul) >> a.page_shift : pos, slot = pos - col * (unsigned)a.page_size;
+                    of_row = (unsigned long)(unsigned)table[col - table_from] * a.page_step + ((unsigned long)slot * a.slot_step + first_key);
                 } else {
-                    const char* const base = a.k + 2 * (b * a.ks.a + head * a.ks.c);
-#pragma unroll
-                    for (int j = 0; j < C::kLoads; ++j)
-                        from[j] = base + 2 * (min((t - items.cached) * C::kTile + load_row(j), s.N) * a.ks.b) + piece_of(load_row(j));
+                    of_row = first_own + 2 * (min((t - items.cached) * C::kTile + my_row, s.N) * a.ks.b);
                 }
-#pragma unroll
-                for (int j = 0; j < C::kLoads; ++j) load_lds(lds0 + stage * C::kStage + j * 1024, from[j]);
             };
-            const auto load_values = [&](int t, int stage) {
-                const long by = t < items.cached ? a.vc - a.kc : a.v - a.k;
+            const unsigned lds0 = __builtin_amdgcn_readfirstlane(lds_offset(lds)) + wave * C::kLoads * 1024;
+            const int asks = 4 * (lane / C::kLanes);
+            const auto load = [&](long by, unsigned to) {
 #pragma unroll
-                for (int j = 0; j < C::kLoads; ++j) load_lds(lds0 + stage * C::kStage + j * 1024 + C::kTileBytes, from[j] + by);
+                for (int j = 0; j < C::kLoads; ++j) {
+                    const unsigned lo = (unsigned)__builtin_amdgcn_ds_bpermute(asks + 4 * C::kRows * j, (int)(unsigned)of_row);
+                    const unsigned hi = (unsigned)__builtin_amdgcn_ds_bpermute(asks + 4 * C::kRows * j, (int)(unsigned)(of_row >> 32));
+                    const unsigned piece = 16u * ((lane % C::kLanes) ^ turn<D>(first_row + j * C::kRows + lane / C::kLanes));
+                    load_lds(to + j * 1024, reinterpret_cast<const char*>(((unsigned long)hi << 32 | lo) + (by + piece)));
+                }
             };
+            const auto load_keys = [&](int stage) { load(0, lds0 + stage * C::kStage); };
+            const auto load_values = [&](int t, int stage) { load(t < items.cached ? a.vc - a.kc : a.v - a.k, lds0 + stage * C::kStage + C::kTileBytes); };
 
             // kHeld tiles are held, and half a tile is asked for as soon as its place is free: values of t + kHeld - 1 behind the products with the
-            // values of t - 1, keys of t + kHeld behind those with the keys of t.  All but one of the halves are on their way at any time.
+            // values of t - 1, keys of t + kHeld behind those with the keys of t.  All but one of the halves are on their way at any time.  Waves that
+            // share their keys meet at every half; others go on by themselves.
             constexpr int kAhead = C::kHeld - 1;
+            constexpr bool kShared = C::WM > 1;
 #pragma unroll
             for (int i = 0; i < C::kHeld; ++i)
                 if (t0 + i < t1) {
-                    look_up(t0 + i);
-                    load_keys(t0 + i, i);
+                    locate(t0 + i);
+                    load_keys(i);
                     if (i < kAhead) load_values(t0 + i, i);
                 }
             int at = 0;  // the place of tile t
             for (int t = t0; t < t1; ++t) {
                 const bool own = t >= items.cached;  // a tile of the block's own rows, not of the cache
-                const char* const stage = lds + at * C::kStage;
-                const int limit = own ? s.N + 1 : s.L, base0 = (own ? t - items.cached : t) * C::kTile + wk * C::kSub * 32;
-                arrived<C::kLoads, C::kHeld>(t1 - 1 - t);
+                const char* const stage = lds + at * C::kStage + wk * 32 * C::kRowBytes;
+                const int limit = own ? s.N + 1 : s.L, base = (own ? t - items.cached : t) * C::kTile + wk * 32;  // of the block's rows, or of the cache
+                const bool some = base < limit;
+                arrived<C::kLoads, C::kHeld, kShared>(t1 - 1 - t);
+                // All reads of LDS before the first product: one by one, each waited for, they took most of a tile's time
+                x8 k[kSteps];
+                {
+                    const int r = lane & 31, x = half ^ turn<D>(r);
+                    const char* const kr = stage + r * C::kRowBytes;
+#pragma unroll
+                    for (int i = 0; i < kSteps; ++i) k[i] = *reinterpret_cast<const x8*>(kr + ((2 * i) ^ x) * 16);
+                }
+                __builtin_amdgcn_sched_barrier(0);
                 if (t + kAhead < t1) load_values(t + kAhead, at > 0 ? at - 1 : kAhead);
-                x8 weights[C::kSub][2];
-                f32x16 sc[C::kSub];
-                float top = -__builtin_huge_valf();
+                if (t + C::kHeld < t1) locate(t + C::kHeld);
+                x8 weights[NC][2];
+                if (some) {
+                    f32x16 sc[NC];
 #pragma unroll
-                for (int sub = 0; sub < C::kSub; ++sub) {
-                    const int base = base0 + sub * 32;  // of the block's rows, or of the cache
-                    if (base >= limit) continue;
-                    sc[sub] = f32x16{};
-                    const int r = lane & 31;
-                    const char* const kr = stage + ((wk * C::kSub + sub) * 32 + r) * C::kRowBytes;
-                    const int x = half ^ turn<D>(r);
+                    for (int c = 0; c < NC; ++c) sc[c] = f32x16{};
 #pragma unroll
-                    for (int i = 0; i < kSteps; ++i) sc[sub] = mfma<DT>(*reinterpret_cast<const x8*>(kr + ((2 * i) ^ x) * 16), q[i], sc[sub]);
-                    if (own || base + 32 > limit) {
-                        const unsigned mine = seen_keys(own, a.parents != nullptr, base, limit, row, s.N, up) >> (4 * half);
+                    for (int i = 0; i < kSteps; ++i)
 #pragma unroll
-                        for (int i = 0; i < 16; ++i)
-                            if (!(mine >> (8 * (i / 4) + i % 4) & 1)) sc[sub][i] = -__builtin_huge_valf();
+                        for (int c = 0; c < NC; ++c) sc[c] = mfma<DT>(k[i], q[c][i], sc[c]);
+                    if (own || base + 32 > limit)
+#pragma unroll
+                        for (int c = 0; c < NC; ++c) {
+                            const unsigned mine = seen_keys(own, a.parents != nullptr, base, limit, row[c], s.N, up) >> (4 * half);
+#pragma unroll
+                            for (int i = 0; i < 16; ++i)
+                                if (!(mine >> (8 * (i / 4) + i % 4) & 1)) sc[c][i] = -__builtin_huge_valf();
+                        }
+#pragma unroll
+                    for (int c = 0; c < NC; ++c) {
+                        float top = sc[c][0];
+#pragma unroll
+                        for (int i = 1; i < 16; ++i) top = fmaxf(top, sc[c][i]);
+                        top = halves_max(top) * a.scale;
+                        const bool rise = top > m[c] + H::kSlack;
+                        if (__ballot(rise)) {
+                            const float to = rise ? top : m[c], by = __builtin_amdgcn_exp2f(m[c] - to);
+                            m[c] = to;
+                            l[c] *= by;
+#pragma unroll
+                            for (int i = 0; i < kBlocks; ++i) o[c][i] *= by;
+                        }
+                        const float ref = H::kLift - m[c];
+                        float p[16];
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) {
+                            p[i] = __builtin_amdgcn_exp2f(fmaf(sc[c][i], a.scale, ref));
+                            weights[c][i / 8][i % 8] = (typename H::T)p[i];
+                        }
+                        l[c] += tree_sum16(p);
                     }
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) top = fmaxf(top, sc[sub][i]);
                 }
-                // one reference for all weights of the tile, which are products only later
-                top = halves_max(top) * a.scale;
-                const bool rise = top > m + H::kSlack;
-                if (__ballot(rise)) {
-                    const float to = rise ? top : m, by = __builtin_amdgcn_exp2f(m - to);
-                    m = to;
-                    l *= by;
-#pragma unroll
-                    for (int i = 0; i < kBlocks; ++i) o[i] *= by;
-                }
-                const float ref = H::kLift - m;
-#pragma unroll
-                for (int sub = 0; sub < C::kSub; ++sub) {
-                    if (base0 + sub * 32 >= limit) continue;
-                    float p[16];
-#pragma unroll
-                    for (int i = 0; i < 16; ++i) {
-                        p[i] = __builtin_amdgcn_exp2f(fmaf(sc[sub][i], a.scale, ref));
-                        weights[sub][i / 8][i % 8] = (typename H::T)p[i];
-                    }
-                    l += tree_sum16(p);
-                }
-                arrived<C::kLoads, C::kHeld>(t1 - 1 - t);
+                arrived<C::kLoads, C::kHeld, kShared>(t1 - 1 - t);
                 if (own) {
                     // Values of the block that are not finite count for the rows that see them alone, which have NaN; a product with a weight of 0 is none
-                    unsigned odd[C::kSub] = {};
-#pragma unroll
-                    for (int sub = 0; sub < C::kSub; ++sub) {
-                        const char* const vr = stage + C::kTileBytes + ((wk * C::kSub + sub) * 32 + (lane & 31)) * C::kRowBytes + half * D;
-                        bool is = false;
-                        for (int i = 0; i < D / 4; ++i) {
-                            const unsigned w = reinterpret_cast<const unsigned*>(vr)[i];
-                            is = is || (w & H::kExponent) == H::kExponent || (w >> 16 & H::kExponent) == H::kExponent;
-                        }
-                        const unsigned long long ballot = __ballot(is);
-                        odd[sub] = (unsigned)ballot | (unsigned)(ballot >> 32);
-                        if (odd[sub] && base0 + sub * 32 < limit &&
-                            (odd[sub] & seen_keys(true, a.parents != nullptr, base0 + sub * 32, limit, row, s.N, up)))
-                            l = __builtin_nanf("");
+                    char* const vr = lds + (stage - lds) + C::kTileBytes + (lane & 31) * C::kRowBytes + half * D;
+                    bool is = false;
+                    for (int i = 0; i < D / 4; ++i) {
+                        const unsigned w = reinterpret_cast<const unsigned*>(vr)[i];
+                        is = is || (w & H::kExponent) == H::kExponent || (w >> 16 & H::kExponent) == H::kExponent;
                     }
-                    __syncthreads();  // other waves look at the same values
+                    const unsigned long long ballot = __ballot(is);
+                    const unsigned odd = (unsigned)ballot | (unsigned)(ballot >> 32);
+                    if (odd && some)
 #pragma unroll
-                    for (int sub = 0; sub < C::kSub; ++sub)
-                        if (odd[sub] >> (lane & 31) & 1) {
-                            char* const vr = lds + at * C::kStage + C::kTileBytes + ((wk * C::kSub + sub) * 32 + (lane & 31)) * C::kRowBytes + half * D;
-                            for (int i = 0; i < D / 4; ++i) reinterpret_cast<unsigned*>(vr)[i] = 0;
-                        }
+                        for (int c = 0; c < NC; ++c)
+                            if (odd & seen_keys(true, a.parents != nullptr, base, limit, row[c], s.N, up)) l[c] = __builtin_nanf("");
+                    __syncthreads();  // other waves look at the same values
+                    if (odd >> (lane & 31) & 1)
+                        for (int i = 0; i < D / 4; ++i) reinterpret_cast<unsigned*>(vr)[i] = 0;
                     __syncthreads();
                 }
-                if (t + C::kHeld < t1) {
-                    look_up(t + C::kHeld);
-                    load_keys(t + C::kHeld, at);
-                }
-#pragma unroll
-                for (int sub = 0; sub < C::kSub; ++sub) {
-                    if (base0 + sub * 32 >= limit) continue;
-                    const char* const vt = stage + C::kTileBytes + (wk * C::kSub + sub) * 32 * C::kRowBytes;
-                    // the values, transposed: 4 keys of a column each read
+                // the values, transposed: 4 keys of a column each read
+                union {
+                    s16x4 h[2];
+                    x8 all;
+                } v[kBlocks][2];
+                {
+                    const char* const vt = stage + C::kTileBytes;
                     const int q4 = (lane & 15) >> 2, wide = lane >> 4 & 1;
 #pragma unroll
-                    for (int db = 0; db < kBlocks; ++db) {
+                    for (int db = 0; db < kBlocks; ++db)
 #pragma unroll
-                        for (int kb = 0; kb < 2; ++kb) {
-                            union {
-                                s16x4 h[2];
-                                x8 all;
-                            } vf;
-#pragma unroll
-                            for (int j = 0; j < 2; ++j) {
-                                const int r = 16 * kb + 8 * j + 4 * half + q4, piece = db * 4 + 2 * wide + ((lane & 3) >> 1);
-                                vf.h[j] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(vt + r * C::kRowBytes + (piece ^ turn<D>(r)) * 16 + (lane & 1) * 8));
-                            }
-                            o[db] = mfma<DT>(vf.all, weights[sub][kb], o[db]);
+                        for (int i = 0; i < 4; ++i) {
+                            const int r = 8 * i + 4 * half + q4, piece = db * 4 + 2 * wide + ((lane & 3) >> 1);
+                            v[db][i / 2].h[i % 2] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(vt + r * C::kRowBytes + (piece ^ turn<D>(r)) * 16 + (lane & 1) * 8));
                         }
-                    }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                if (t + C::kHeld < t1) load_keys(at);
+                if (some) {
+#pragma unroll
+                    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                        for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+                            for (int c = 0; c < NC; ++c) o[c][db] = mfma<DT>(v[db][kb].all, weights[c][kb], o[c][db]);
                 }
                 at = at == kAhead ? 0 : at + 1;
             }
-            l += __shfl_xor(l, 32, kWave);
+#pragma unroll
+            for (int c = 0; c < NC; ++c) l[c] += __shfl_xor(l[c], 32, kWave);
         }
         if (bad) sh_bad = 1;
         // the waves' sums over their keys to those of the first
         __syncthreads();
         float* const hand = reinterpret_cast<float*>(lds);
         if (C::WK > 1) {
-            if (half == 0) hand_ml[wk][wm * 32 + (lane & 31)] = make_float2(m, l);
-            if (wk > 0) {
-                float* const to = hand + ((wk - 1) * C::kColumns + wm * 32 + (lane & 31)) * C::kPad;
 #pragma unroll
-                for (int db = 0; db < kBlocks; ++db)
+            for (int c = 0; c < NC; ++c) {
+                if (half == 0) hand_ml[wk][place_of[c]] = make_float2(m[c], l[c]);
+                if (wk > 0) {
+                    float* const to = hand + ((wk - 1) * C::kColumns + place_of[c]) * C::kPad;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        *reinterpret_cast<f32v4*>(to + db * 32 + 8 * i + 4 * half) = f32v4{o[db][4 * i], o[db][4 * i + 1], o[db][4 * i + 2], o[db][4 * i + 3]};
+                    for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            *reinterpret_cast<f32v4*>(to + db * 32 + 8 * i + 4 * half) = f32v4{o[c][db][4 * i], o[c][db][4 * i + 1], o[c][db][4 * i + 2], o[c][db][4 * i + 3]};
+                }
             }
             __syncthreads();
         }
         if (wk == 0) {
-            if (C::WK > 1) {
-                float top = m;
-                for (int w = 1; w < C::WK; ++w) top = fmaxf(top, hand_ml[w][wm * 32 + (lane & 31)].x);
-                const float by = __builtin_amdgcn_exp2f(m - top);
-                l *= by;
-                m = top;
 #pragma unroll
-                for (int db = 0; db < kBlocks; ++db) o[db] *= by;
-                for (int w = 1; w < C::WK; ++w) {
-                    const float2 ml = hand_ml[w][wm * 32 + (lane & 31)];
-                    const float f = __builtin_amdgcn_exp2f(ml.x - m);
-                    l = fmaf(ml.y, f, l);
-                    const float* const from = hand + ((w - 1) * C::kColumns + wm * 32 + (lane & 31)) * C::kPad;
+            for (int c = 0; c < NC; ++c) {
+                if (C::WK > 1) {
+                    float top = m[c];
+                    for (int w = 1; w < C::WK; ++w) top = fmaxf(top, hand_ml[w][place_of[c]].x);
+                    const float by = __builtin_amdgcn_exp2f(m[c] - top);
+                    l[c] *= by;
+                    m[c] = top;
 #pragma unroll
-                    for (int db = 0; db < kBlocks; ++db)
+                    for (int db = 0; db < kBlocks; ++db) o[c][db] *= by;
+                    for (int w = 1; w < C::WK; ++w) {
+                        const float2 ml = hand_ml[w][place_of[c]];
+                        const float f = __builtin_amdgcn_exp2f(ml.x - m[c]);
+                        l[c] = fmaf(ml.y, f, l[c]);
+                        const float* const from = hand + ((w - 1) * C::kColumns + place_of[c]) * C::kPad;
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const f32v4 x = *reinterpret_cast<const f32v4*>(from + db * 32 + 8 * i + 4 * half);
+                        for (int db = 0; db < kBlocks; ++db)
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) o[db][4 * i + j] = fmaf(x[j], f, o[db][4 * i + j]);
-                        }
+                            for (int i = 0; i < 4; ++i) {
+                                const f32v4 x = *reinterpret_cast<const f32v4*>(from + db * 32 + 8 * i + 4 * half);
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) o[c][db][4 * i + j] = fmaf(x[j], f, o[c][db][4 * i + j]);
+                            }
+                    }
                 }
-            }
-            if (sh_bad) l = __builtin_nanf("");
-            if (valid) {
+                if (sh_bad) l[c] = __builtin_nanf("");
+                if (row[c] >= rows) continue;
                 if (whole) {
-                    const float by = 1.f / l;
-                    char* const to = a.out + 2 * (b * a.os.a + row * a.os.b + (head * a.group + of_group) * a.os.c + 4 * half);
+                    const float by = 1.f / l[c];
+                    char* const to = a.out + 2 * (b * a.os.a + row[c] * a.os.b + query[c] * a.os.c + 4 * half);
 #pragma unroll
                     for (int db = 0; db < kBlocks; ++db)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             typename H::T r[4];
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) r[j] = (typename H::T)(o[db][4 * i + j] * by);
+                            for (int j = 0; j < 4; ++j) r[j] = (typename H::T)(o[c][db][4 * i + j] * by);
                             __builtin_memcpy(__builtin_assume_aligned(to + 2 * (db * 32 + 8 * i), 8), r, 8);
                         }
                 } else {
-                    const long slot = 2l * blockIdx.x + (first_item ? 0 : 1), c = slot * C::kColumns + wm * 32 + (lane & 31);
-                    if (half == 0) a.part_ml[c] = make_float2(m, l);
-                    float* const to = a.part_o + c * D + 4 * half;
+                    const long slot = 2l * blockIdx.x + (first_item ? 0 : 1), column = slot * C::kColumns + place_of[c];
+                    if (half == 0) a.part_ml[column] = make_float2(m[c], l[c]);
+                    float* const to = a.part_o + column * D + 4 * half;
 #pragma unroll
                     for (int db = 0; db < kBlocks; ++db)
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            *reinterpret_cast<f32v4*>(to + db * 32 + 8 * i) = f32v4{o[db][4 * i], o[db][4 * i + 1], o[db][4 * i + 2], o[db][4 * i + 3]};
+                            *reinterpret_cast<f32v4*>(to + db * 32 + 8 * i) = f32v4{o[c][db][4 * i], o[c][db][4 * i + 1], o[c][db][4 * i + 2], o[c][db][4 * i + 3]};
                 }
             }
         }
@@ -620,15 +628,15 @@ template <typename F>
 auto with_shape(const ss_tree_params& p, F f) {
     const int columns = (p.nodes + 1) * (p.heads / p.kv_heads);
     if (p.head_dim == 64) {
-        if (columns <= 32) return f(Shape<64, 1, 2, 1, 4>{}, 2);
-        if (columns <= 64) return f(Shape<64, 2, 2, 1, 4>{}, 2);
-        if (columns <= 128) return f(Shape<64, 4, 2, 1, 5>{}, 1);
-        return f(Shape<64, 8, 1, 2, 5>{}, 1);
+        if (columns <= 32) return f(Shape<64, 1, 1, 8, 2>{}, 1);
+        if (columns <= 64) return f(Shape<64, 1, 2, 4, 4>{}, 1);
+        if (columns <= 128) return f(Shape<64, 1, 4, 2, 8>{}, 1);
+        return f(Shape<64, 2, 4, 2, 8>{}, 1);
     }
-    if (columns <= 32) return f(Shape<128, 1, 2, 1, 2>{}, 2);
-    if (columns <= 64) return f(Shape<128, 2, 2, 1, 2>{}, 2);
-    if (columns <= 128) return f(Shape<128, 4, 2, 1, 4>{}, 1);
-    return f(Shape<128, 8, 1, 1, 5>{}, 1);
+    if (columns <= 32) return f(Shape<128, 1, 1, 8, 1>{}, 1);
+    if (columns <= 64) return f(Shape<128, 1, 2, 4, 2>{}, 1);
+    if (columns <= 128) return f(Shape<128, 1, 4, 2, 4>{}, 1);
+    return f(Shape<128, 1, 8, 1, 8>{}, 1);
 }
 
 }  // namespace
@@ -675,6 +683,11 @@ ss_status specsteer_tree_attention(const void* q, const void* k, const void* v, 
         a.page_step = (unsigned)(2 * s.cache.a);
         a.slot_step = (unsigned)(2 * s.cache.b);
         a.head_step = 2 * s.cache.c;
+        // exact for positions below 2^31: ceil(2^(31 + s) / size) with 2^s >= size
+        int bits = 0;
+        while (1l << bits < params->page_size) ++bits;
+        a.page_mul = bits ? (unsigned)(((1ul << (31 + bits)) + params->page_size - 1) / params->page_size) : 0u;
+        a.page_shift = bits - 1;
         a.ts = s.table;
         a.B = params->batch;
         a.N = params->nodes;
