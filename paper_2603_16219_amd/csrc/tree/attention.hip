@@ -75,7 +75,7 @@ __device__ __forceinline__ float tree_sum16(const float (&p)[16]) {
 
 // Which of the 32 keys from `base` on a row sees: of the block's own rows itself and its ancestors, of the cache those there are.
 __device__ __forceinline__ unsigned seen_keys(bool own, bool tree, int base, int limit, int row, int N, const unsigned short* up) {
-    if (!own) return limit - base >= 32 ? ~0u : (1u << (limit - base)) - 1;
+    if (!own) return limit - base >= 32 ? ~0u : limit > base ? (1u << (limit - base)) - 1 : 0u;
     int j = min(row, N);
     if (!tree) return j < base ? 0u : j - base >= 31 ? ~0u : (2u << (j - base)) - 1;
     unsigned seen = base == 0 ? 1u : 0u;
@@ -99,6 +99,7 @@ struct AttnArgs {
     char* out;
     float* part_o;   // [2 * shares][columns][D]: sums of values of parts
     float2* part_ml; // [2 * shares][columns]: their references and sums of weights
+    struct Cut* cuts;  // [shares]
     Strides3 qs, ks, os;
     unsigned page_step, slot_step;  // bytes
     unsigned page_mul;              // a position's page: the upper half of its product with this, shifted; or 0 for pages of one
@@ -124,45 +125,35 @@ __device__ __forceinline__ Sequence sequence(const AttnArgs& a, int b) {
 
 // Where a unit lies: its sequence, and the units before that.
 struct Place {
-    int b;
-    long before, total;
+    int b, before, total;
 };
 // The sums over all sequences, by a workgroup; the unit asked for follows from them.
 template <int NT, typename F>
-__device__ __forceinline__ Place find_place(const AttnArgs& a, const TreeTiles& tiles, long* sh, F unit) {
+__device__ __forceinline__ Place find_place(const AttnArgs& a, const TreeTiles& tiles, int* sh, F unit) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     constexpr int kWaves = NT / kWave;
     const auto of = [&](int b) {
-        if (b >= a.B) return 0l;
+        if (b >= a.B) return 0;
         const Sequence s = sequence(a, b);
         return tree_items(tiles, s.L, s.N, s.bad, a.N).units(a.kv_heads);
     };
-    const long first = of(tid);
-    long sum = first;
+    const int first = of(tid);
+    int sum = first;
     for (int b = tid + NT; b < a.B; b += NT) sum += of(b);
-    for (int d = 1; d < kWave; d <<= 1) sum += __shfl_xor(sum, d, kWave);
-    __syncthreads();
+    sum = wave_sum_i32(sum);
     if (lane == 0) sh[wave] = sum;
     __syncthreads();
-    Place p;
-    p.total = 0;
+    Place p{0, 0, 0};
     for (int w = 0; w < kWaves; ++w) p.total += sh[w];
-    p.b = 0;
-    p.before = 0;
-    const long u = unit(p.total);
+    const int u = unit(p.total);
     if (u < 0 || u >= p.total) return p;
-    long before = 0;
+    int before = 0;
     for (int b0 = 0; b0 < a.B; b0 += NT) {
-        const long mine = b0 == 0 ? first : of(b0 + tid);
-        long incl = mine;
-        for (int d = 1; d < kWave; d <<= 1) {
-            const long o = __shfl_up(incl, d, kWave);
-            if (lane >= d) incl += o;
-        }
+        const int mine = b0 == 0 ? first : of(b0 + tid), incl = wave_incl_scan_i32(mine);
         __syncthreads();
         if (lane == 63) sh[wave] = incl;
         __syncthreads();
-        long start = before;
+        int start = before;
         for (int w = 0; w < kWaves; ++w) {
             if (w < wave) start += sh[w];
             before += sh[w];
@@ -174,20 +165,27 @@ __device__ __forceinline__ Place find_place(const AttnArgs& a, const TreeTiles& 
         if (u < before) break;
     }
     __syncthreads();
-    p.b = (int)sh[kWaves];
+    p.b = sh[kWaves];
     p.before = sh[kWaves + 1];
     return p;
 }
 
-// A workgroup of WM x WK waves: each takes NC blocks of 32 columns and 32 keys of a tile; waves of the same columns take turns at the keys.
-template <int D_, int NC_, int WM_, int WK_, int HELD_>
+// What joins the parts of an item that a share's beginning cuts, written by that share if no share before it begins inside of the item.
+struct Cut {
+    int b, head, block, parts;  // parts: 0 if there is nothing to join; the first is the share's before, in its second slot if `second`
+    int second, pad[3];
+};
+
+// A workgroup of WM x WK waves: each takes 32 columns and SUB times 32 keys of a tile; waves of the same columns take turns at the keys.
+template <int D_, int WM_, int WK_, int SUB_, int HELD_, int GROUPS_>
 struct Shape {
-    static constexpr int D = D_, NC = NC_, WM = WM_, WK = WK_;
-    static constexpr int kWaves = WM * WK, kThreads = kWaves * kWave, kColumns = 32 * NC * WM;
-    static constexpr int kTile = 32 * WK;            // keys
+    static constexpr int D = D_, WM = WM_, WK = WK_, kSub = SUB_;
+    static constexpr int kWaves = WM * WK, kThreads = kWaves * kWave, kColumns = 32 * WM;
+    static constexpr int kGroups = GROUPS_;          // workgroups a compute unit
+    static constexpr int kTile = 32 * WK * kSub;     // keys
     static constexpr int kLanes = D / 8;             // of 16 bytes each, a row
     static constexpr int kRows = kWave / kLanes;     // rows a load instruction
-    static constexpr int kLoads = 32 / (kRows * WM); // of a wave for the keys of a tile, and for its values; with one wave over the columns its own
+    static constexpr int kLoads = 32 * kSub / (kRows * WM);  // of a wave for the keys of a tile, and for its values; with one wave over the columns its own
     static constexpr int kRowBytes = 2 * D, kTileBytes = kTile * kRowBytes, kStage = 2 * kTileBytes;
     static constexpr int kHeld = HELD_;              // tiles in LDS
     static constexpr int kTable = 1024;              // entries of the table in LDS
@@ -208,40 +206,50 @@ template <int DT, typename C>
 __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 2))) void attention_kernel(const AttnArgs a) {
     using H = Half<DT>;
     using x8 = typename H::x8;
-    constexpr int D = C::D, NC = C::NC, kBlocks = D / 32, kSteps = D / 16;
+    constexpr int D = C::D, kSub = C::kSub, kBlocks = D / 32, kSteps = D / 16;
     __shared__ __attribute__((aligned(1024))) char lds[C::kBuffers];
     __shared__ float2 hand_ml[C::WK][C::kColumns];
     __shared__ unsigned short up[SS_MAX_K + 1];
     __shared__ int table[C::kTable];
-    __shared__ long sh[C::kWaves + 2];
+    __shared__ int sh[C::kWaves + 2];
     __shared__ int sh_bad;
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave % C::WM, wk = wave / C::WM;
     const TreeTiles tiles{C::kTile, C::kColumns, a.group, a.kv_heads};
 
-    if (a.tree_len) {  // rows that belong to nobody are 0
-        const int pieces = a.group * a.kv_heads * (D / 8);
-        for (long r = blockIdx.x; r < (long)a.B * (a.N + 1); r += gridDim.x) {
-            const int b = (int)(r / (a.N + 1)), row = (int)(r % (a.N + 1));
-            const Sequence s = sequence(a, b);
-            if (s.bad || row <= s.N) continue;
-            for (int i = tid; i < pieces; i += C::kThreads)
-                *reinterpret_cast<uint4*>(a.out + 2 * (b * a.os.a + row * a.os.b + (i / (D / 8)) * a.os.c) + 16 * (i % (D / 8))) = make_uint4(0, 0, 0, 0);
-        }
-    }
-
     Shares deals{};
-    const Place place = find_place<C::kThreads>(a, tiles, sh, [&](long total) {
+    const Place place = find_place<C::kThreads>(a, tiles, sh, [&](int total) {
         deals = deal(total, a.shares);
-        return (int)blockIdx.x < deals.shares ? deals.begin(blockIdx.x) : -1l;
+        return (int)blockIdx.x < deals.shares ? deals.begin(blockIdx.x) : -1;
     });
-    if ((int)blockIdx.x >= deals.shares) return;
-    long u = deals.begin(blockIdx.x);
-    const long u_end = deals.begin(blockIdx.x + 1);
-    int b = place.b;
-    long rel = u - place.before;  // within the sequence
+    int u = 0, u_end = 0;
+    if ((int)blockIdx.x < deals.shares) {
+        u = deals.begin(blockIdx.x);
+        u_end = deals.begin(blockIdx.x + 1);
+    }
+    int b = place.b, rel = u - place.before;  // within the sequence
     Sequence s = sequence(a, b);
     TreeItems items = tree_items(tiles, s.L, s.N, s.bad, a.N);
+    if (tid == 0 && blockIdx.x > 0) {
+        int parts = 0, second = 0;
+        if (u < u_end) {
+            const int nt = items.tiles(), item = rel / nt, start = u - (rel - item * nt);
+            const int before = deals.begin(blockIdx.x - 1);
+            if (start < u && before <= start) {
+                int x = blockIdx.x + 1;
+                while (x < deals.shares && deals.begin(x) < start + nt) ++x;
+                parts = x - (int)blockIdx.x + 1;
+                second = before < start ? 1 : 0;
+            }
+        }
+        Cut* const cut = a.cuts + blockIdx.x;
+        const int item = rel / max(items.tiles(), 1);
+        cut->b = b;
+        cut->head = item / items.blocks;
+        cut->block = item % items.blocks;
+        cut->parts = parts;
+        cut->second = second;
+    }
     bool first_item = true;
     while (u < u_end) {
         if (rel >= items.units(a.kv_heads)) {
@@ -251,44 +259,21 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
             items = tree_items(tiles, s.L, s.N, s.bad, a.N);
         }
         const int nt = items.tiles();
-        const int item = (int)(rel / nt), t0 = (int)(rel - (long)item * nt), t1 = (int)min((long)nt, t0 + (u_end - u));
+        const int item = rel / nt, t0 = rel - item * nt, t1 = min(nt, t0 + (u_end - u));
         const int head = item / items.blocks, block = item - head * items.blocks;
-        // this lane's columns
-        const int rows = (s.bad ? a.N : s.N) + 1;
-        int row[NC], query[NC], place_of[NC];  // a tree's row, the query head, the column of the block
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            place_of[c] = (wm * NC + c) * 32 + (lane & 31);
-            const int column = block * C::kColumns + place_of[c];
-            row[c] = column / a.group;
-            query[c] = head * a.group + column - row[c] * a.group;
-        }
+        // this lane's column: a row of the tree and a query head
+        const int place_of = wm * 32 + (lane & 31), column = block * C::kColumns + place_of;
+        const int rows = (s.bad ? a.N : s.N) + 1, row = column / a.group, query = head * a.group + column - row * a.group;
         const bool whole = t0 == 0 && t1 == nt;
         bool bad = s.bad;
 
-        f32x16 o[NC][kBlocks];
-        float m[NC], l[NC];
+        f32x16 o[kBlocks];
+        float m = -1e30f, l = 0.f;
 #pragma unroll
-        for (int c = 0; c < NC; ++c) {
-            m[c] = -1e30f;
-            l[c] = 0.f;
-#pragma unroll
-            for (int i = 0; i < kBlocks; ++i) o[c][i] = f32x16{};
-        }
+        for (int i = 0; i < kBlocks; ++i) o[i] = f32x16{};
         __syncthreads();  // the last item's hand-over is done with
         if (tid == 0) sh_bad = 0;
         if (!s.bad) {
-            x8 q[NC][kSteps];
-#pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                const char* const qp = a.q + 2 * (b * a.qs.a + min(row[c], s.N) * a.qs.b + query[c] * a.qs.c) + 16 * half;
-#pragma unroll
-                for (int i = 0; i < kSteps; ++i) {
-                    u32v4 w = *reinterpret_cast<const u32v4*>(qp + 32 * i);
-                    if (a.negative) w ^= 0x80008000u;
-                    q[c][i] = __builtin_bit_cast(x8, w);
-                }
-            }
             if (t1 > items.cached && a.parents) {
                 for (int i = tid; i < s.N; i += C::kThreads) {
                     int p = a.parents[(long)b * a.N + i];
@@ -362,92 +347,112 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
                     load_keys(i);
                     if (i < kAhead) load_values(t0 + i, i);
                 }
+            x8 q[kSteps];  // behind the first loads of keys: they are all on their way together
+            {
+                const char* const qp = a.q + 2 * (b * a.qs.a + min(row, s.N) * a.qs.b + query * a.qs.c) + 16 * half;
+#pragma unroll
+                for (int i = 0; i < kSteps; ++i) {
+                    u32v4 w = *reinterpret_cast<const u32v4*>(qp + 32 * i);
+                    if (a.negative) w ^= 0x80008000u;
+                    q[i] = __builtin_bit_cast(x8, w);
+                }
+            }
             int at = 0;  // the place of tile t
             for (int t = t0; t < t1; ++t) {
                 const bool own = t >= items.cached;  // a tile of the block's own rows, not of the cache
-                const char* const stage = lds + at * C::kStage + wk * 32 * C::kRowBytes;
-                const int limit = own ? s.N + 1 : s.L, base = (own ? t - items.cached : t) * C::kTile + wk * 32;  // of the block's rows, or of the cache
+                const char* const stage = lds + at * C::kStage + wk * kSub * 32 * C::kRowBytes;
+                const int limit = own ? s.N + 1 : s.L, base = (own ? t - items.cached : t) * C::kTile + wk * kSub * 32;  // of the block's rows, or of the cache
                 const bool some = base < limit;
                 arrived<C::kLoads, C::kHeld, kShared>(t1 - 1 - t);
                 // All reads of LDS before the first product: one by one, each waited for, they took most of a tile's time
-                x8 k[kSteps];
-                {
+                f32x16 sc[kSub];
+#pragma unroll
+                for (int sub = 0; sub < kSub; ++sub) {
+                    x8 k[kSteps];
                     const int r = lane & 31, x = half ^ turn<D>(r);
-                    const char* const kr = stage + r * C::kRowBytes;
+                    const char* const kr = stage + (sub * 32 + r) * C::kRowBytes;
 #pragma unroll
                     for (int i = 0; i < kSteps; ++i) k[i] = *reinterpret_cast<const x8*>(kr + ((2 * i) ^ x) * 16);
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (sub == 0) {
+                        if (t + kAhead < t1) load_values(t + kAhead, at > 0 ? at - 1 : kAhead);
+                        if (t + C::kHeld < t1) locate(t + C::kHeld);
+                    }
+                    sc[sub] = f32x16{};
+#pragma unroll
+                    for (int i = 0; i < kSteps; ++i) sc[sub] = mfma<DT>(k[i], q[i], sc[sub]);
                 }
-                __builtin_amdgcn_sched_barrier(0);
-                if (t + kAhead < t1) load_values(t + kAhead, at > 0 ? at - 1 : kAhead);
-                if (t + C::kHeld < t1) locate(t + C::kHeld);
-                x8 weights[NC][2];
+                x8 weights[kSub][2];
                 if (some) {
-                    f32x16 sc[NC];
+                    if (own || base + 32 * kSub > limit)
 #pragma unroll
-                    for (int c = 0; c < NC; ++c) sc[c] = f32x16{};
-#pragma unroll
-                    for (int i = 0; i < kSteps; ++i)
-#pragma unroll
-                        for (int c = 0; c < NC; ++c) sc[c] = mfma<DT>(k[i], q[c][i], sc[c]);
-                    if (own || base + 32 > limit)
-#pragma unroll
-                        for (int c = 0; c < NC; ++c) {
-                            const unsigned mine = seen_keys(own, a.parents != nullptr, base, limit, row[c], s.N, up) >> (4 * half);
+                        for (int sub = 0; sub < kSub; ++sub) {
+                            const unsigned mine = seen_keys(own, a.parents != nullptr, base + 32 * sub, limit, row, s.N, up) >> (4 * half);
 #pragma unroll
                             for (int i = 0; i < 16; ++i)
-                                if (!(mine >> (8 * (i / 4) + i % 4) & 1)) sc[c][i] = -__builtin_huge_valf();
+                                if (!(mine >> (8 * (i / 4) + i % 4) & 1)) sc[sub][i] = -__builtin_huge_valf();
                         }
+                    float top = sc[0][0];
 #pragma unroll
-                    for (int c = 0; c < NC; ++c) {
-                        float top = sc[c][0];
+                    for (int sub = 0; sub < kSub; ++sub)
 #pragma unroll
-                        for (int i = 1; i < 16; ++i) top = fmaxf(top, sc[c][i]);
-                        top = halves_max(top) * a.scale;
-                        const bool rise = top > m[c] + H::kSlack;
-                        if (__ballot(rise)) {
-                            const float to = rise ? top : m[c], by = __builtin_amdgcn_exp2f(m[c] - to);
-                            m[c] = to;
-                            l[c] *= by;
+                        for (int i = sub == 0 ? 1 : 0; i < 16; ++i) top = fmaxf(top, sc[sub][i]);
+                    // one reference for all weights of the tile, which are products only later
+                    top = halves_max(top) * a.scale;
+                    const bool rise = top > m + H::kSlack;
+                    if (__ballot(rise)) {
+                        const float to = rise ? top : m, by = __builtin_amdgcn_exp2f(m - to);
+                        m = to;
+                        l *= by;
 #pragma unroll
-                            for (int i = 0; i < kBlocks; ++i) o[c][i] *= by;
-                        }
-                        const float ref = H::kLift - m[c];
+                        for (int i = 0; i < kBlocks; ++i) o[i] *= by;
+                    }
+                    const float ref = H::kLift - m;
+#pragma unroll
+                    for (int sub = 0; sub < kSub; ++sub) {
                         float p[16];
 #pragma unroll
                         for (int i = 0; i < 16; ++i) {
-                            p[i] = __builtin_amdgcn_exp2f(fmaf(sc[c][i], a.scale, ref));
-                            weights[c][i / 8][i % 8] = (typename H::T)p[i];
+                            p[i] = __builtin_amdgcn_exp2f(fmaf(sc[sub][i], a.scale, ref));
+                            weights[sub][i / 8][i % 8] = (typename H::T)p[i];
                         }
-                        l[c] += tree_sum16(p);
+                        l += tree_sum16(p);
                     }
                 }
                 arrived<C::kLoads, C::kHeld, kShared>(t1 - 1 - t);
                 if (own) {
                     // Values of the block that are not finite count for the rows that see them alone, which have NaN; a product with a weight of 0 is none
-                    char* const vr = lds + (stage - lds) + C::kTileBytes + (lane & 31) * C::kRowBytes + half * D;
-                    bool is = false;
-                    for (int i = 0; i < D / 4; ++i) {
-                        const unsigned w = reinterpret_cast<const unsigned*>(vr)[i];
-                        is = is || (w & H::kExponent) == H::kExponent || (w >> 16 & H::kExponent) == H::kExponent;
-                    }
-                    const unsigned long long ballot = __ballot(is);
-                    const unsigned odd = (unsigned)ballot | (unsigned)(ballot >> 32);
-                    if (odd && some)
+                    unsigned odd[kSub];
 #pragma unroll
-                        for (int c = 0; c < NC; ++c)
-                            if (odd & seen_keys(true, a.parents != nullptr, base, limit, row[c], s.N, up)) l[c] = __builtin_nanf("");
+                    for (int sub = 0; sub < kSub; ++sub) {
+                        const char* const vr = stage + C::kTileBytes + (sub * 32 + (lane & 31)) * C::kRowBytes + half * D;
+                        bool is = false;
+                        for (int i = 0; i < D / 4; ++i) {
+                            const unsigned w = reinterpret_cast<const unsigned*>(vr)[i];
+                            is = is || (w & H::kExponent) == H::kExponent || (w >> 16 & H::kExponent) == H::kExponent;
+                        }
+                        const unsigned long long ballot = __ballot(is);
+                        odd[sub] = (unsigned)ballot | (unsigned)(ballot >> 32);
+                        if (odd[sub] && base + 32 * sub < limit && (odd[sub] & seen_keys(true, a.parents != nullptr, base + 32 * sub, limit, row, s.N, up)))
+                            l = __builtin_nanf("");
+                    }
                     __syncthreads();  // other waves look at the same values
-                    if (odd >> (lane & 31) & 1)
-                        for (int i = 0; i < D / 4; ++i) reinterpret_cast<unsigned*>(vr)[i] = 0;
+#pragma unroll
+                    for (int sub = 0; sub < kSub; ++sub)
+                        if (odd[sub] >> (lane & 31) & 1) {
+                            char* const vr = lds + (stage - lds) + C::kTileBytes + (sub * 32 + (lane & 31)) * C::kRowBytes + half * D;
+                            for (int i = 0; i < D / 4; ++i) reinterpret_cast<unsigned*>(vr)[i] = 0;
+                        }
                     __syncthreads();
                 }
-                // the values, transposed: 4 keys of a column each read
-                union {
-                    s16x4 h[2];
-                    x8 all;
-                } v[kBlocks][2];
-                {
-                    const char* const vt = stage + C::kTileBytes;
+#pragma unroll
+                for (int sub = 0; sub < kSub; ++sub) {
+                    // the values, transposed: 4 keys of a column each read
+                    union {
+                        s16x4 h[2];
+                        x8 all;
+                    } v[kBlocks][2];
+                    const char* const vt = stage + C::kTileBytes + sub * 32 * C::kRowBytes;
                     const int q4 = (lane & 15) >> 2, wide = lane >> 4 & 1;
 #pragma unroll
                     for (int db = 0; db < kBlocks; ++db)
@@ -456,90 +461,81 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
                             const int r = 8 * i + 4 * half + q4, piece = db * 4 + 2 * wide + ((lane & 3) >> 1);
                             v[db][i / 2].h[i % 2] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(vt + r * C::kRowBytes + (piece ^ turn<D>(r)) * 16 + (lane & 1) * 8));
                         }
-                }
-                __builtin_amdgcn_sched_barrier(0);
-                if (t + C::kHeld < t1) load_keys(at);
-                if (some) {
+                    __builtin_amdgcn_sched_barrier(0);
+                    if (sub == 0 && t + C::kHeld < t1) load_keys(at);
+                    if (some)
 #pragma unroll
-                    for (int kb = 0; kb < 2; ++kb)
+                        for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
-                        for (int db = 0; db < kBlocks; ++db)
-#pragma unroll
-                            for (int c = 0; c < NC; ++c) o[c][db] = mfma<DT>(v[db][kb].all, weights[c][kb], o[c][db]);
+                            for (int db = 0; db < kBlocks; ++db) o[db] = mfma<DT>(v[db][kb].all, weights[sub][kb], o[db]);
                 }
                 at = at == kAhead ? 0 : at + 1;
             }
-#pragma unroll
-            for (int c = 0; c < NC; ++c) l[c] += __shfl_xor(l[c], 32, kWave);
+            l += __shfl_xor(l, 32, kWave);
         }
         if (bad) sh_bad = 1;
         // the waves' sums over their keys to those of the first
         __syncthreads();
         float* const hand = reinterpret_cast<float*>(lds);
         if (C::WK > 1) {
+            if (half == 0) hand_ml[wk][place_of] = make_float2(m, l);
+            if (wk > 0) {
+                float* const to = hand + ((wk - 1) * C::kColumns + place_of) * C::kPad;
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                if (half == 0) hand_ml[wk][place_of[c]] = make_float2(m[c], l[c]);
-                if (wk > 0) {
-                    float* const to = hand + ((wk - 1) * C::kColumns + place_of[c]) * C::kPad;
+                for (int db = 0; db < kBlocks; ++db)
 #pragma unroll
-                    for (int db = 0; db < kBlocks; ++db)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            *reinterpret_cast<f32v4*>(to + db * 32 + 8 * i + 4 * half) = f32v4{o[c][db][4 * i], o[c][db][4 * i + 1], o[c][db][4 * i + 2], o[c][db][4 * i + 3]};
-                }
+                    for (int i = 0; i < 4; ++i)
+                        *reinterpret_cast<f32v4*>(to + db * 32 + 8 * i + 4 * half) = f32v4{o[db][4 * i], o[db][4 * i + 1], o[db][4 * i + 2], o[db][4 * i + 3]};
             }
             __syncthreads();
         }
         if (wk == 0) {
+            if (C::WK > 1) {
+                float top = m;
+                for (int w = 1; w < C::WK; ++w) top = fmaxf(top, hand_ml[w][place_of].x);
+                const float by = __builtin_amdgcn_exp2f(m - top);
+                l *= by;
+                m = top;
 #pragma unroll
-            for (int c = 0; c < NC; ++c) {
-                if (C::WK > 1) {
-                    float top = m[c];
-                    for (int w = 1; w < C::WK; ++w) top = fmaxf(top, hand_ml[w][place_of[c]].x);
-                    const float by = __builtin_amdgcn_exp2f(m[c] - top);
-                    l[c] *= by;
-                    m[c] = top;
+                for (int db = 0; db < kBlocks; ++db) o[db] *= by;
+                for (int w = 1; w < C::WK; ++w) {
+                    const float2 ml = hand_ml[w][place_of];
+                    const float f = __builtin_amdgcn_exp2f(ml.x - m);
+                    l = fmaf(ml.y, f, l);
+                    const float* const from = hand + ((w - 1) * C::kColumns + place_of) * C::kPad;
 #pragma unroll
-                    for (int db = 0; db < kBlocks; ++db) o[c][db] *= by;
-                    for (int w = 1; w < C::WK; ++w) {
-                        const float2 ml = hand_ml[w][place_of[c]];
-                        const float f = __builtin_amdgcn_exp2f(ml.x - m[c]);
-                        l[c] = fmaf(ml.y, f, l[c]);
-                        const float* const from = hand + ((w - 1) * C::kColumns + place_of[c]) * C::kPad;
+                    for (int db = 0; db < kBlocks; ++db)
 #pragma unroll
-                        for (int db = 0; db < kBlocks; ++db)
+                        for (int i = 0; i < 4; ++i) {
+                            const f32v4 x = *reinterpret_cast<const f32v4*>(from + db * 32 + 8 * i + 4 * half);
 #pragma unroll
-                            for (int i = 0; i < 4; ++i) {
-                                const f32v4 x = *reinterpret_cast<const f32v4*>(from + db * 32 + 8 * i + 4 * half);
-#pragma unroll
-                                for (int j = 0; j < 4; ++j) o[c][db][4 * i + j] = fmaf(x[j], f, o[c][db][4 * i + j]);
-                            }
-                    }
+                            for (int j = 0; j < 4; ++j) o[db][4 * i + j] = fmaf(x[j], f, o[db][4 * i + j]);
+                        }
                 }
-                if (sh_bad) l[c] = __builtin_nanf("");
-                if (row[c] >= rows) continue;
+            }
+            if (sh_bad) l = __builtin_nanf("");
+            if (row < rows) {
                 if (whole) {
-                    const float by = 1.f / l[c];
-                    char* const to = a.out + 2 * (b * a.os.a + row[c] * a.os.b + query[c] * a.os.c + 4 * half);
+                    const float by = 1.f / l;
+                    char* const to = a.out + 2 * (b * a.os.a + row * a.os.b + query * a.os.c + 4 * half);
 #pragma unroll
                     for (int db = 0; db < kBlocks; ++db)
 #pragma unroll
                         for (int i = 0; i < 4; ++i) {
                             typename H::T r[4];
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) r[j] = (typename H::T)(o[c][db][4 * i + j] * by);
+                            for (int j = 0; j < 4; ++j) r[j] = (typename H::T)(o[db][4 * i + j] * by);
                             __builtin_memcpy(__builtin_assume_aligned(to + 2 * (db * 32 + 8 * i), 8), r, 8);
                         }
                 } else {
-                    const long slot = 2l * blockIdx.x + (first_item ? 0 : 1), column = slot * C::kColumns + place_of[c];
-                    if (half == 0) a.part_ml[column] = make_float2(m[c], l[c]);
-                    float* const to = a.part_o + column * D + 4 * half;
+                    const long slot = 2l * blockIdx.x + (first_item ? 0 : 1), at = slot * C::kColumns + place_of;
+                    if (half == 0) a.part_ml[at] = make_float2(m, l);
+                    float* const to = a.part_o + at * D + 4 * half;
 #pragma unroll
                     for (int db = 0; db < kBlocks; ++db)
 #pragma unroll
                         for (int i = 0; i < 4; ++i)
-                            *reinterpret_cast<f32v4*>(to + db * 32 + 8 * i) = f32v4{o[c][db][4 * i], o[c][db][4 * i + 1], o[c][db][4 * i + 2], o[c][db][4 * i + 3]};
+                            *reinterpret_cast<f32v4*>(to + db * 32 + 8 * i) = f32v4{o[db][4 * i], o[db][4 * i + 1], o[db][4 * i + 2], o[db][4 * i + 3]};
                 }
             }
         }
@@ -547,80 +543,71 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
         rel += t1 - t0;
         u += t1 - t0;
     }
+    if (a.tree_len) {  // rows that belong to nobody are 0
+        const int pieces = a.group * a.kv_heads * (D / 8);
+        for (long r = blockIdx.x; r < (long)a.B * (a.N + 1); r += gridDim.x) {
+            const int b = (int)(r / (a.N + 1)), row = (int)(r % (a.N + 1));
+            const Sequence s = sequence(a, b);
+            if (s.bad || row <= s.N) continue;
+            for (int i = tid; i < pieces; i += C::kThreads)
+                *reinterpret_cast<uint4*>(a.out + 2 * (b * a.os.a + row * a.os.b + (i / (D / 8)) * a.os.c) + 16 * (i % (D / 8))) = make_uint4(0, 0, 0, 0);
+        }
+    }
 }
 
-// The parts of the item that share blockIdx.x + 1 begins inside of, if no share before it does.
-constexpr int kJoinThreads = 256, kJoinColumns = 16;
+// The parts of the items that shares' beginnings cut, a workgroup for some columns of each.
+constexpr int kJoinThreads = 256;
 template <int DT, typename C>
 __global__ __launch_bounds__(kJoinThreads) void attention_join_kernel(const AttnArgs a) {
     using H = Half<DT>;
-    constexpr int D = C::D, kLanes = D / 4, kAtOnce = kJoinThreads / kLanes;
-    __shared__ long sh[kJoinThreads / kWave + 2];
+    constexpr int D = C::D, kLanes = D / 4;
     const int w = blockIdx.x + 1, tid = threadIdx.x;
-    const TreeTiles tiles{C::kTile, C::kColumns, a.group, a.kv_heads};
-    Shares deals{};
-    const Place place = find_place<kJoinThreads>(a, tiles, sh, [&](long total) {
-        deals = deal(total, a.shares);
-        return w < deals.shares ? deals.begin(w) : -1l;
-    });
-    if (w >= deals.shares) return;
-    const long u = deals.begin(w);
-    const int b = place.b;
-    const Sequence s = sequence(a, b);
-    const TreeItems items = tree_items(tiles, s.L, s.N, s.bad, a.N);
-    const int nt = items.tiles();
-    const long rel = u - place.before;
-    const int item = (int)(rel / nt), t0 = (int)(rel - (long)item * nt);
-    const long start = u - t0, end = start + nt;
-    if (t0 == 0 || deals.begin(w - 1) > start) return;  // it is cut before this already
-    const int head = item / items.blocks, block = item - head * items.blocks;
-    const int rows = (s.bad ? a.N : s.N) + 1;
-    for (int i = tid / kLanes; i < kJoinColumns; i += kAtOnce) {
-        const int of_block = blockIdx.y * kJoinColumns + i, column = block * C::kColumns + of_block, row = column / a.group;
-        if (of_block >= C::kColumns || row >= rows) break;
-        // the share before has the item's first part, in its second slot unless it begins with the item
-        const auto at = [&](int x) { return (2l * x + (x >= w || deals.begin(x) == start ? 0 : 1)) * C::kColumns + of_block; };
-        int x_end = w;
-        while (x_end < deals.shares && deals.begin(x_end) < end) ++x_end;
-        float m = -1e30f, l = 0.f;
+    const Cut cut = a.cuts[w];
+    if (cut.parts == 0) return;
+    const Sequence s = sequence(a, cut.b);
+    const int of_block = blockIdx.y * (kJoinThreads / kLanes) + tid / kLanes, column = cut.block * C::kColumns + of_block, row = column / a.group;
+    if (row >= (s.bad ? a.N : s.N) + 1) return;
+    // the share before has the item's first part
+    const auto at = [&](int x) { return (2l * (w - 1 + x) + (x == 0 ? cut.second : 0)) * C::kColumns + of_block; };
+    float m = -1e30f, l = 0.f;
 #pragma unroll 4
-        for (int x = w - 1; x < x_end; ++x) m = fmaxf(m, a.part_ml[at(x)].x);
-        f32v4 o = {};
+    for (int x = 0; x < cut.parts; ++x) m = fmaxf(m, a.part_ml[at(x)].x);
+    f32v4 o = {};
 #pragma unroll 4
-        for (int x = w - 1; x < x_end; ++x) {
-            const float2 ml = a.part_ml[at(x)];
-            const f32v4 v = *reinterpret_cast<const f32v4*>(a.part_o + at(x) * D + 4 * (tid % kLanes));
-            const float f = __builtin_amdgcn_exp2f(ml.x - m);
-            l = fmaf(ml.y, f, l);
-            o += v * f;
-        }
-        typename H::T r[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) r[j] = (typename H::T)(o[j] / l);
-        char* const to = a.out + 2 * (b * a.os.a + row * a.os.b + (head * a.group + (column - row * a.group)) * a.os.c + 4 * (tid % kLanes));
-        __builtin_memcpy(__builtin_assume_aligned(to, 8), r, 8);
+    for (int x = 0; x < cut.parts; ++x) {
+        const float2 ml = a.part_ml[at(x)];
+        const f32v4 v = *reinterpret_cast<const f32v4*>(a.part_o + at(x) * D + 4 * (tid % kLanes));
+        const float f = __builtin_amdgcn_exp2f(ml.x - m);
+        l = fmaf(ml.y, f, l);
+        o += v * f;
     }
+    typename H::T r[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) r[j] = (typename H::T)(o[j] / l);
+    char* const to = a.out + 2 * (cut.b * a.os.a + row * a.os.b + (cut.head * a.group + (column - row * a.group)) * a.os.c + 4 * (tid % kLanes));
+    __builtin_memcpy(__builtin_assume_aligned(to, 8), r, 8);
 }
 
 // What a call takes: its shares, one a workgroup that runs at once, and no more than it may have units.
 struct AttnPlan {
-    int columns, shares;
-    size_t off_ml, bytes;
+    int shares;  // 0: more units than 32 bits count
+    size_t off_ml, off_cuts, bytes;
 };
 template <typename C>
-AttnPlan plan_for(const ss_tree_params& p, int groups_a_unit) {
+AttnPlan plan_for(const ss_tree_params& p) {
     const TreeTiles tiles{C::kTile, C::kColumns, p.heads / p.kv_heads, p.kv_heads};
     TreeItems most = tree_items(tiles, 0, p.nodes, false, p.nodes);
     most.cached = (int)(((long)p.table_width * p.page_size + C::kTile - 1) / C::kTile);
-    const double units = (double)most.units(p.kv_heads) * p.batch;
-    AttnPlan r;
-    r.columns = C::kColumns;
-    r.shares = device_cu_count() * groups_a_unit;
+    const double units = (double)most.tiles() * most.blocks * p.kv_heads * p.batch;
+    AttnPlan r{};
+    if (units >= 2147483648.0) return r;
+    r.shares = device_cu_count() * C::kGroups;
     if (r.shares > kMaxShares) r.shares = kMaxShares;
     if (units < r.shares) r.shares = units < 1 ? 1 : (int)units;
     const size_t slots = 2 * (size_t)r.shares * C::kColumns;
     r.off_ml = slots * C::D * 4;
-    r.bytes = (r.off_ml + slots * 8 + 255) / 256 * 256;
+    r.off_cuts = r.off_ml + slots * 8;
+    r.bytes = (r.off_cuts + (size_t)r.shares * sizeof(Cut) + 255) / 256 * 256;
     return r;
 }
 
@@ -628,15 +615,15 @@ template <typename F>
 auto with_shape(const ss_tree_params& p, F f) {
     const int columns = (p.nodes + 1) * (p.heads / p.kv_heads);
     if (p.head_dim == 64) {
-        if (columns <= 32) return f(Shape<64, 1, 1, 8, 2>{}, 1);
-        if (columns <= 64) return f(Shape<64, 1, 2, 4, 4>{}, 1);
-        if (columns <= 128) return f(Shape<64, 1, 4, 2, 8>{}, 1);
-        return f(Shape<64, 2, 4, 2, 8>{}, 1);
+        if (columns <= 32) return f(Shape<64, 1, 4, 1, 2, 2>{});
+        if (columns <= 64) return f(Shape<64, 2, 2, 2, 2, 2>{});
+        if (columns <= 128) return f(Shape<64, 4, 1, 2, 4, 2>{});
+        return f(Shape<64, 8, 1, 2, 8, 1>{});
     }
-    if (columns <= 32) return f(Shape<128, 1, 1, 8, 1>{}, 1);
-    if (columns <= 64) return f(Shape<128, 1, 2, 4, 2>{}, 1);
-    if (columns <= 128) return f(Shape<128, 1, 4, 2, 4>{}, 1);
-    return f(Shape<128, 1, 8, 1, 8>{}, 1);
+    if (columns <= 32) return f(Shape<128, 1, 4, 1, 1, 2>{});
+    if (columns <= 64) return f(Shape<128, 2, 2, 1, 2, 2>{});
+    if (columns <= 128) return f(Shape<128, 4, 1, 2, 2, 2>{});
+    return f(Shape<128, 8, 1, 2, 4, 1>{});
 }
 
 }  // namespace
@@ -646,7 +633,7 @@ extern "C" {
 size_t specsteer_tree_attention_workspace_bytes(const ss_tree_params* params) {
     TreeShape s;
     if (tree_shape(params, true, s) != SS_OK) return 0;
-    return with_shape(*params, [&](auto shape, int groups) { return plan_for<decltype(shape)>(*params, groups).bytes; });
+    return with_shape(*params, [&](auto shape) { return plan_for<decltype(shape)>(*params).bytes; });
 }
 
 ss_status specsteer_tree_attention(const void* q, const void* k, const void* v, const void* k_cache, const void* v_cache, const int32_t* block_table,
@@ -659,9 +646,10 @@ ss_status specsteer_tree_attention(const void* q, const void* k, const void* v, 
     const bool cached = params->pages > 0 && params->table_width > 0;
     if (!q || !k || !v || !cache_len || !out || (cached && (!k_cache || !v_cache || !block_table))) return SS_ERR_NULL;
     if (off_16(q) || off_16(k) || off_16(v) || off_16(out) || (cached && (off_16(k_cache) || off_16(v_cache)))) return SS_ERR_STRIDE;
-    return with_shape(*params, [&](auto shape, int groups) {
+    return with_shape(*params, [&](auto shape) {
         using C = decltype(shape);
-        const AttnPlan plan = plan_for<C>(*params, groups);
+        const AttnPlan plan = plan_for<C>(*params);
+        if (plan.shares == 0) return SS_ERR_SHAPE;
         if (bad_workspace(workspace, workspace_bytes, plan.bytes)) return SS_ERR_WORKSPACE;
         const auto in = [](const void* p) { return static_cast<const char*>(p); };
         AttnArgs a{};
@@ -677,6 +665,7 @@ ss_status specsteer_tree_attention(const void* q, const void* k, const void* v, 
         a.out = static_cast<char*>(out);
         a.part_o = static_cast<float*>(workspace);
         a.part_ml = reinterpret_cast<float2*>(static_cast<char*>(workspace) + plan.off_ml);
+        a.cuts = reinterpret_cast<Cut*>(static_cast<char*>(workspace) + plan.off_cuts);
         a.qs = s.q;
         a.ks = s.k;
         a.os = s.out;
@@ -705,7 +694,7 @@ ss_status specsteer_tree_attention(const void* q, const void* k, const void* v, 
         launch(bf ? attention_kernel<SS_BF16, C> : attention_kernel<SS_TREE_F16, C>, dim3((unsigned)plan.shares), dim3(C::kThreads), 0, st, (const AttnArgs)a);
         if (plan.shares > 1)
             launch(bf ? attention_join_kernel<SS_BF16, C> : attention_join_kernel<SS_TREE_F16, C>,
-                   dim3((unsigned)plan.shares - 1, (unsigned)((C::kColumns + kJoinColumns - 1) / kJoinColumns)), dim3(kJoinThreads), 0, st, (const AttnArgs)a);
+                   dim3((unsigned)plan.shares - 1, (unsigned)(C::kColumns * (C::D / 4) / kJoinThreads)), dim3(kJoinThreads), 0, st, (const AttnArgs)a);
         return tree_launched();
     });
 }

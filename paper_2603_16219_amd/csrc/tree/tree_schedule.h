@@ -8,7 +8,7 @@
 // launch joins those of the item that the share's beginning cuts, if it is the first to do so.
 #pragma once
 
-// begin() multiplies two numbers of shares in 32 bits
+// begin() multiplies two numbers of shares in 32 bits; a call has fewer than 2^31 units
 constexpr int kMaxShares = 1 << 15;
 
 #ifdef __HIPCC__
@@ -29,29 +29,28 @@ struct TreeTiles {
 struct TreeItems {
     int cached, own, blocks;
     SS_TREE_BOTH int tiles() const { return cached + own; }
-    SS_TREE_BOTH long units(int kv_heads) const { return (long)tiles() * blocks * kv_heads; }
+    SS_TREE_BOTH int units(int kv_heads) const { return tiles() * blocks * kv_heads; }
 };
 SS_TREE_BOTH TreeItems tree_items(const TreeTiles& t, int length, int nodes, bool bad, int max_nodes) {
     TreeItems r;
-    const long columns = (long)((bad ? max_nodes : nodes) + 1) * t.group;
-    r.cached = bad ? 0 : (int)(((long)length + t.tile - 1) / t.tile);
+    const int columns = ((bad ? max_nodes : nodes) + 1) * t.group;
+    r.cached = bad ? 0 : (int)(((unsigned)length + (unsigned)t.tile - 1) / (unsigned)t.tile);
     r.own = bad ? 1 : (nodes + t.tile) / t.tile;
-    r.blocks = (int)((columns + t.columns - 1) / t.columns);
+    r.blocks = (columns + t.columns - 1) / t.columns;
     return r;
 }
-// No share is empty.
-SS_TREE_BOTH int shares_of(int most, long units) { return units < most ? (int)units : most; }
+// The shares of all units: no share is empty.
 struct Shares {
-    long each;   // units of a share,
-    int more;    // and one more of these of them, spread out
+    int each;   // units of a share,
+    int more;   // and one more of these of them, spread out
     int shares;
-    SS_TREE_BOTH long begin(int w) const { return each * w + (long)((unsigned)more * (unsigned)w / (unsigned)shares); }
+    SS_TREE_BOTH int begin(int w) const { return each * w + (int)((unsigned)more * (unsigned)w / (unsigned)shares); }
 };
-SS_TREE_BOTH Shares deal(long units, int most) {
+SS_TREE_BOTH Shares deal(int units, int most) {
     Shares r;
-    r.shares = shares_of(most, units);
+    r.shares = units < most ? units : most;
     r.each = r.shares ? units / r.shares : 0;
-    r.more = (int)(units - r.each * r.shares);
+    r.more = units - r.each * r.shares;
     return r;
 }
 
