@@ -251,6 +251,9 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
         cut->second = second;
     }
     bool first_item = true;
+    // the piece of the table that is in LDS: its sequence, the column that it begins with, the tiles whose pages it has
+    int table_of = -1, table_from = 0, table_first = 0, table_until = 0;
+    bool table_bad = false;  // of its sequence this thread has met a page that is none
     while (u < u_end) {
         if (rel >= items.units(a.kv_heads)) {
             ++b;
@@ -274,33 +277,22 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
         __syncthreads();  // the last item's hand-over is done with
         if (tid == 0) sh_bad = 0;
         if (!s.bad) {
-            if (t1 > items.cached && a.parents) {
-                for (int i = tid; i < s.N; i += C::kThreads) {
-                    int p = a.parents[(long)b * a.N + i];
-                    if (p < -1 || p >= i) {
-                        bad = true;
-                        p = -1;
-                    }
-                    up[i + 1] = (unsigned short)(p + 1);
-                }
-                __syncthreads();
-            }
-
             // The rows of a tile that this wave loads are kMine from first_row on.  A lane finds where one of them lies, and those that load its pieces
             // ask for that: the arithmetic once for all rows, whatever the pages' size.  The pages come from a piece of the table in LDS.
             constexpr int kMine = C::kLoads * C::kRows;
             const int first_row = wave * kMine, my_row = first_row + lane % kMine;
             const int last = s.L > 0 ? (s.L - 1) / a.page_size : 0;
-            int table_from = 0, table_until = t0;  // the column that table[0] is, the tile up to which they are there
             const auto look_up = [&](int t) {
-                if (t >= items.cached || t < table_until) return;
+                if (t >= items.cached || (b == table_of && t >= table_first && t < table_until)) return;
                 __syncthreads();
+                if (b != table_of) table_bad = false;
+                table_of = b;
+                table_first = t;
                 table_from = (int)((long)t * C::kTile / a.page_size);
-                const int until = min(last, (int)(((long)min(t1, items.cached) * C::kTile - 1) / a.page_size));
-                for (int i = tid; i < C::kTable && table_from + i <= until; i += C::kThreads) {
+                for (int i = tid; i < C::kTable && table_from + i <= last; i += C::kThreads) {
                     int p = a.table[b * a.ts + table_from + i];
                     if (p < 0 || p >= a.pages) {
-                        bad = true;
+                        table_bad = true;
                         p = 0;
                     }
                     table[i] = p;
@@ -356,6 +348,17 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
                     if (a.negative) w ^= 0x80008000u;
                     q[i] = __builtin_bit_cast(x8, w);
                 }
+            }
+            if (t1 > items.cached && a.parents) {
+                for (int i = tid; i < s.N; i += C::kThreads) {
+                    int p = a.parents[(long)b * a.N + i];
+                    if (p < -1 || p >= i) {
+                        bad = true;
+                        p = -1;
+                    }
+                    up[i + 1] = (unsigned short)(p + 1);
+                }
+                __syncthreads();
             }
             int at = 0;  // the place of tile t
             for (int t = t0; t < t1; ++t) {
@@ -473,7 +476,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
             }
             l += __shfl_xor(l, 32, kWave);
         }
-        if (bad) sh_bad = 1;
+        if (bad || (table_bad && table_of == b)) sh_bad = 1;
         // the waves' sums over their keys to those of the first
         __syncthreads();
         float* const hand = reinterpret_cast<float*>(lds);
