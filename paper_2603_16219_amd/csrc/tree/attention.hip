@@ -115,10 +115,15 @@ struct Sequence {
     int L, N;
     bool bad;
 };
+template <bool UNIFORM>
 __device__ __forceinline__ Sequence sequence(const AttnArgs& a, int b) {
     Sequence s;
     s.L = a.cache_len[b];
     s.N = a.tree_len ? a.tree_len[b] : a.N;
+    if (UNIFORM) {  // which loads by vector instructions do not tell
+        s.L = __builtin_amdgcn_readfirstlane(s.L);
+        s.N = __builtin_amdgcn_readfirstlane(s.N);
+    }
     s.bad = s.L < 0 || s.L > (long)a.width * a.page_size || s.N < 0 || s.N > a.N;
     return s;
 }
@@ -134,7 +139,7 @@ __device__ __forceinline__ Place find_place(const AttnArgs& a, const TreeTiles& 
     constexpr int kWaves = NT / kWave;
     const auto of = [&](int b) {
         if (b >= a.B) return 0;
-        const Sequence s = sequence(a, b);
+        const Sequence s = sequence<false>(a, b);
         return tree_items(tiles, s.L, s.N, s.bad, a.N).units(a.kv_heads);
     };
     const int first = of(tid);
@@ -145,6 +150,7 @@ __device__ __forceinline__ Place find_place(const AttnArgs& a, const TreeTiles& 
     __syncthreads();
     Place p{0, 0, 0};
     for (int w = 0; w < kWaves; ++w) p.total += sh[w];
+    p.total = __builtin_amdgcn_readfirstlane(p.total);
     const int u = unit(p.total);
     if (u < 0 || u >= p.total) return p;
     int before = 0;
@@ -165,8 +171,8 @@ __device__ __forceinline__ Place find_place(const AttnArgs& a, const TreeTiles& 
         if (u < before) break;
     }
     __syncthreads();
-    p.b = sh[kWaves];
-    p.before = sh[kWaves + 1];
+    p.b = __builtin_amdgcn_readfirstlane(sh[kWaves]);
+    p.before = __builtin_amdgcn_readfirstlane(sh[kWaves + 1]);
     return p;
 }
 
@@ -228,7 +234,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
         u_end = deals.begin(blockIdx.x + 1);
     }
     int b = place.b, rel = u - place.before;  // within the sequence
-    Sequence s = sequence(a, b);
+    Sequence s = sequence<true>(a, b);
     TreeItems items = tree_items(tiles, s.L, s.N, s.bad, a.N);
     if (tid == 0 && blockIdx.x > 0) {
         int parts = 0, second = 0;
@@ -258,11 +264,11 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
         if (rel >= items.units(a.kv_heads)) {
             ++b;
             rel = 0;
-            s = sequence(a, b);
+            s = sequence<true>(a, b);
             items = tree_items(tiles, s.L, s.N, s.bad, a.N);
         }
         const int nt = items.tiles();
-        const int item = rel / nt, t0 = rel - item * nt, t1 = min(nt, t0 + (u_end - u));
+        const int item = __builtin_amdgcn_readfirstlane(rel / nt), t0 = __builtin_amdgcn_readfirstlane(rel - item * nt), t1 = __builtin_amdgcn_readfirstlane(min(nt, t0 + (u_end - u)));
         const int head = item / items.blocks, block = item - head * items.blocks;
         // this lane's column: a row of the tree and a query head
         const int place_of = wm * 32 + (lane & 31), column = block * C::kColumns + place_of;
@@ -284,13 +290,14 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
             const int last = s.L > 0 ? (s.L - 1) / a.page_size : 0;
             const auto look_up = [&](int t) {
                 if (t >= items.cached || (b == table_of && t >= table_first && t < table_until)) return;
+                const int32_t* const pages = a.table + b * a.ts;
                 __syncthreads();
                 if (b != table_of) table_bad = false;
                 table_of = b;
                 table_first = t;
                 table_from = (int)((long)t * C::kTile / a.page_size);
                 for (int i = tid; i < C::kTable && table_from + i <= last; i += C::kThreads) {
-                    int p = a.table[b * a.ts + table_from + i];
+                    int p = pages[table_from + i];
                     if (p < 0 || p >= a.pages) {
                         table_bad = true;
                         p = 0;
@@ -350,8 +357,9 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
                 }
             }
             if (t1 > items.cached && a.parents) {
+                const int32_t* const parents = a.parents + (long)b * a.N;
                 for (int i = tid; i < s.N; i += C::kThreads) {
-                    int p = a.parents[(long)b * a.N + i];
+                    int p = parents[i];
                     if (p < -1 || p >= i) {
                         bad = true;
                         p = -1;
@@ -429,12 +437,10 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
 #pragma unroll
                     for (int sub = 0; sub < kSub; ++sub) {
                         const char* const vr = stage + C::kTileBytes + (sub * 32 + (lane & 31)) * C::kRowBytes + half * D;
-                        bool is = false;
-                        for (int i = 0; i < D / 4; ++i) {
-                            const unsigned w = reinterpret_cast<const unsigned*>(vr)[i];
-                            is = is || (w & H::kExponent) == H::kExponent || (w >> 16 & H::kExponent) == H::kExponent;
-                        }
-                        const unsigned long long ballot = __ballot(is);
+                        unsigned is = 0;  // an exponent of all ones carries into the sign's bit
+#pragma unroll 4
+                        for (int i = 0; i < D / 4; ++i) is |= (reinterpret_cast<const unsigned*>(vr)[i] & 0x7FFF7FFFu) + 0x10001u * (0x8000u - H::kExponent);
+                        const unsigned long long ballot = __ballot((is & 0x80008000u) != 0);
                         odd[sub] = (unsigned)ballot | (unsigned)(ballot >> 32);
                         if (odd[sub] && base + 32 * sub < limit && (odd[sub] & seen_keys(true, a.parents != nullptr, base + 32 * sub, limit, row, s.N, up)))
                             l = __builtin_nanf("");
@@ -550,7 +556,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
         const int pieces = a.group * a.kv_heads * (D / 8);
         for (long r = blockIdx.x; r < (long)a.B * (a.N + 1); r += gridDim.x) {
             const int b = (int)(r / (a.N + 1)), row = (int)(r % (a.N + 1));
-            const Sequence s = sequence(a, b);
+            const Sequence s = sequence<true>(a, b);
             if (s.bad || row <= s.N) continue;
             for (int i = tid; i < pieces; i += C::kThreads)
                 *reinterpret_cast<uint4*>(a.out + 2 * (b * a.os.a + row * a.os.b + (i / (D / 8)) * a.os.c) + 16 * (i % (D / 8))) = make_uint4(0, 0, 0, 0);
@@ -567,7 +573,7 @@ __global__ __launch_bounds__(kJoinThreads) void attention_join_kernel(const Attn
     const int w = blockIdx.x + 1, tid = threadIdx.x;
     const Cut cut = a.cuts[w];
     if (cut.parts == 0) return;
-    const Sequence s = sequence(a, cut.b);
+    const Sequence s = sequence<true>(a, cut.b);
     const int of_block = blockIdx.y * (kJoinThreads / kLanes) + tid / kLanes, column = cut.block * C::kColumns + of_block, row = column / a.group;
     if (row >= (s.bad ? a.N : s.N) + 1) return;
     // the share before has the item's first part
