@@ -118,14 +118,17 @@ __device__ __forceinline__ int key_id(unsigned long long k) { return (int)(0xFFF
 
 constexpr int kHits = 4096, kRanked = 1024;  // tokens that reached a bound, and the last one
 struct Finder {
-    unsigned long long hits[kHits], ranked[kRanked];
+    unsigned long long ranked[kRanked];
+    int hits[kHits];  // ids
     float bound[kUnitWaves];  // of every wave
     int hit_count, ranked_count, digit, above;
 };
 
-__device__ __forceinline__ void push(Finder& f, float h, int id) {
+// Only the id, which the shortlist reads the logit of again: to pick it out of the lane's vectors here took 50 us more for
+// 1024 rows of 151936 in bf16 with n = 16.
+__device__ __forceinline__ void push(Finder& f, int id) {
     const int at = atomicAdd(&f.hit_count, 1);
-    if (at < kHits) f.hits[at] = key_of(h, id);
+    if (at < kHits) f.hits[at] = id;
 }
 // The least of the groups' largest logits, over the wave.
 __device__ __forceinline__ float wave_bound(float top, int group) {
@@ -147,7 +150,7 @@ __device__ __forceinline__ float block_bound(const Finder& f, int waves) {
 // sweeps, a row of V = 128256 bf16 in about 0.1 ms.
 template <int DT>
 __device__ __forceinline__ void find_slowly(Finder& f, const void* h, int begin, int end, int n, int threads) {
-    int* const count = reinterpret_cast<int*>(f.hits);
+    int* const count = f.hits;
     const float lowest = -__builtin_huge_valf();
     unsigned prefix = 0, fixed = 0;  // digits of the n-th largest known so far
     int above = 0;                   // tokens above all that share them
@@ -233,8 +236,7 @@ __device__ __forceinline__ SumX scan(const AltArgs& a, const void* h, const Layo
     if (TOP) {
         if (threadIdx.x == 0) f->hit_count = f->ranked_count = 0;
     }
-    bool first = true;
-    for (int i = begin; i < end || first; i += kUnroll * threads) {
+    for (int i = begin, round = 0; i < end || round == 0; i += kUnroll * threads, ++round) {
         typename Row<DT>::Raw r[kUnroll];
 #pragma unroll
         for (int u = 0; u < kUnroll; ++u) {
@@ -254,39 +256,44 @@ __device__ __forceinline__ SumX scan(const AltArgs& a, const void* h, const Layo
         for (int u = 0; u < kUnroll; ++u) add_under(sum, x[u], a.r.c);
         if (TOP) {
             top = fmaxf(top, most);
-            const float b = wave_bound(top, a.group);
-            if ((threadIdx.x & 63) == 0) reinterpret_cast<volatile float*>(f->bound)[wave] = b;
-            if (first) __syncthreads();  // without the others' first bounds there is none
-            bound = block_bound(*f, waves);
+            if ((round & (round - 1)) == 0) {  // it rises less and less; every round, 3 us more
+                const float b = wave_bound(top, a.group);
+                if ((threadIdx.x & 63) == 0) reinterpret_cast<volatile float*>(f->bound)[wave] = b;
+                if (round == 0) __syncthreads();  // without the others' first bounds there is none
+            }
+            bound = fmaxf(block_bound(*f, waves), -3.402823466e38f);  // what is masked is none
+            unsigned hit = 0;
 #pragma unroll
             for (int u = 0; u < kUnroll; ++u)
-                if (m[u] >= bound) {
-                    const int at = lay.head + (i + u * threads + (int)threadIdx.x) * kVec;
+                if (m[u] >= bound)
 #pragma unroll
-                    for (int j = 0; j < kVec; ++j)
-                        if (x[u][j] >= bound && x[u][j] > -__builtin_huge_valf()) push(*f, x[u][j], at + j);
-                }
+                    for (int j = 0; j < kVec; ++j) hit |= (x[u][j] >= bound ? 1u : 0u) << (u * kVec + j);
+            for (; hit; hit &= hit - 1) {
+                const int k = __ffs((int)hit) - 1;
+                push(*f, lay.head + (i + k / kVec * threads + (int)threadIdx.x) * kVec + k % kVec);
+            }
         }
-        first = false;
     }
     if (extra && lay.extra >= 0) {
         const float x[1] = {ld_elem<DT>(h, lay.extra)};
         raise(sum, x[0], a.r.c);
         add_under(sum, x, a.r.c);
-        if (TOP && x[0] >= bound && x[0] > -__builtin_huge_valf()) push(*f, x[0], lay.extra);
+        if (TOP && x[0] >= bound) push(*f, lay.extra);
     }
     return sum;
 }
 
 // The hits that reach `least` into f.ranked; false if there are too many of either.
-__device__ __forceinline__ bool shortlist(Finder& f, float least, int threads) {
+template <int DT>
+__device__ __forceinline__ bool shortlist(Finder& f, const void* h, float least, int threads) {
     const int n = f.hit_count;
     if (n > kHits) return false;
     for (int i = threadIdx.x; i < n; i += threads) {
-        const unsigned long long k = f.hits[i];
-        if (key_logit(k) >= least) {
+        const int id = f.hits[i];
+        const float v = ld_elem<DT>(h, id);
+        if (v >= least) {
             const int at = atomicAdd(&f.ranked_count, 1);
-            if (at < kRanked) f.ranked[at] = k;
+            if (at < kRanked) f.ranked[at] = key_of(v, id);
         }
     }
     __syncthreads();
@@ -344,9 +351,11 @@ __device__ __forceinline__ void finish(const AltArgs& a, long row, const void* h
     }
 }
 
+// Bytes bound it: 1024 rows of 151936 in bf16 take 54 us without likeliest tokens, 5.8 TB/s, and 77 with 16 of them, 4.1 TB/s; 117 with 64.  Registers
+// for four waves a SIMD hold two workgroups a unit, one of which computes while the other waits: with one it was 113 us.
 constexpr int kAltThreads = 512;
 template <int DT, bool TOP>
-__global__ __launch_bounds__(kAltThreads) void alternatives_kernel(const AltArgs a) {
+__global__ __launch_bounds__(kAltThreads) __attribute__((amdgpu_waves_per_eu(4))) void alternatives_kernel(const AltArgs a) {
     __shared__ Total<SumX> part[kAltThreads / kWave];
     __shared__ typename std::conditional<TOP, Finder, int>::type finder;
     Finder* const f = TOP ? reinterpret_cast<Finder*>(&finder) : nullptr;
@@ -365,7 +374,7 @@ __global__ __launch_bounds__(kAltThreads) void alternatives_kernel(const AltArgs
     const bool far = a.r.far || is_far(s);
     if (far) s = far_sum_x<DT>(h, a.r.V, a.r.c64, kAltThreads, part);
     if (TOP) {
-        if (!shortlist(*f, block_bound(*f, kAltThreads / kWave), kAltThreads)) find_slowly<DT>(*f, h, 0, a.r.V, a.topk, kAltThreads);
+        if (!shortlist<DT>(*f, h, block_bound(*f, kAltThreads / kWave), kAltThreads)) find_slowly<DT>(*f, h, 0, a.r.V, a.topk, kAltThreads);
     }
     finish<DT, TOP>(a, row, h, far, s, kAltThreads, f);
 }
@@ -390,7 +399,7 @@ __global__ __launch_bounds__(256) void alternatives_slice_kernel(const AltArgs a
     if (threadIdx.x == 0) a.parts[row * a.slices + slice] = s;
     if (TOP) {
         unsigned long long* const keys = a.keys + (row * a.slices + slice) * a.topk;
-        if (!shortlist(*f, block_bound(*f, kThreads / kWave), kThreads)) {
+        if (!shortlist<DT>(*f, h, block_bound(*f, kThreads / kWave), kThreads)) {
             // the first slice has the elements before and behind the vectors too: it looks through all that no other has
             constexpr int kVec = Row<DT>::kVec;
             const int lo = slice == 0 ? 0 : lay.head + begin * kVec, hi = lay.head + end * kVec;
