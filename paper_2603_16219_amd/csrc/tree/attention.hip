@@ -102,8 +102,7 @@ struct AttnArgs {
     struct Cut* cuts;  // [shares]
     Strides3 qs, ks, os;
     unsigned page_step, slot_step;  // bytes
-    unsigned page_mul;              // a position's page: the upper half of its product with this, shifted; or 0 for pages of one
-    int page_shift;
+    PageOf page_of;
     long head_step;
     long ts;
     int B, N, group, kv_heads, pages, page_size, width, shares;
@@ -314,7 +313,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
                 if (t < items.cached) {
                     look_up(t);
                     const unsigned pos = (unsigned)min(t * C::kTile + my_row, s.L - 1);  // past the end the last key again, which is masked
-                    const unsigned col = a.page_mul ? __umulhi(pos, a.page_mul) >> a.page_shift : pos, slot = pos - col * (unsigned)a.page_size;
+                    const unsigned col = a.page_of(pos), slot = pos - col * (unsigned)a.page_size;
                     of_row = (unsigned long)(unsigned)table[col - table_from] * a.page_step + ((unsigned long)slot * a.slot_step + first_key);
                 } else {
                     of_row = first_own + 2 * (min((t - items.cached) * C::kTile + my_row, s.N) * a.ks.b);
@@ -395,7 +394,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
                 }
                 x8 weights[kSub][2];
                 if (some) {
-                    if (own || base + 32 * kSub > limit)
+                    if (own || limit - base < 32 * kSub)
 #pragma unroll
                         for (int sub = 0; sub < kSub; ++sub) {
                             const unsigned mine = seen_keys(own, a.parents != nullptr, base + 32 * sub, limit, row, s.N, up) >> (4 * half);
@@ -442,7 +441,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
                         for (int i = 0; i < D / 4; ++i) is |= (reinterpret_cast<const unsigned*>(vr)[i] & 0x7FFF7FFFu) + 0x10001u * (0x8000u - H::kExponent);
                         const unsigned long long ballot = __ballot((is & 0x80008000u) != 0);
                         odd[sub] = (unsigned)ballot | (unsigned)(ballot >> 32);
-                        if (odd[sub] && base + 32 * sub < limit && (odd[sub] & seen_keys(true, a.parents != nullptr, base + 32 * sub, limit, row, s.N, up)))
+                        if (odd[sub] && limit - base > 32 * sub && (odd[sub] & seen_keys(true, a.parents != nullptr, base + 32 * sub, limit, row, s.N, up)))
                             l = __builtin_nanf("");
                     }
                     __syncthreads();  // other waves look at the same values
@@ -681,11 +680,7 @@ ss_status specsteer_tree_attention(const void* q, const void* k, const void* v, 
         a.page_step = (unsigned)(2 * s.cache.a);
         a.slot_step = (unsigned)(2 * s.cache.b);
         a.head_step = 2 * s.cache.c;
-        // exact for positions below 2^31: ceil(2^(31 + s) / size) with 2^s >= size
-        int bits = 0;
-        while (1l << bits < params->page_size) ++bits;
-        a.page_mul = bits ? (unsigned)(((1ul << (31 + bits)) + params->page_size - 1) / params->page_size) : 0u;
-        a.page_shift = bits - 1;
+        a.page_of = page_of(params->page_size);
         a.ts = s.table;
         a.B = params->batch;
         a.N = params->nodes;

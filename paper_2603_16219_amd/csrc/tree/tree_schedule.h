@@ -39,6 +39,18 @@ SS_TREE_BOTH TreeItems tree_items(const TreeTiles& t, int length, int nodes, boo
     r.blocks = (columns + t.columns - 1) / t.columns;
     return r;
 }
+// The page of a position below 2^31 without a division: the upper half of its product with ceil(2^(31 + s) / size), shifted, with s the least for which
+// 2^s >= size.  What the factor is too large by is below size <= 2^s, which 2^31 positions do not bring to a page.  A factor of 0: pages of one.
+struct PageOf {
+    unsigned mul;
+    int shift;
+    SS_TREE_BOTH unsigned operator()(unsigned position) const { return mul ? (unsigned)((unsigned long)position * mul >> 32) >> shift : position; }
+};
+inline PageOf page_of(int size) {
+    int bits = 0;
+    while (1l << bits < size) ++bits;
+    return PageOf{bits ? (unsigned)(((1ul << (31 + bits)) + (unsigned long)size - 1) / (unsigned long)size) : 0u, bits - 1};
+}
 // The shares of all units: no share is empty.
 struct Shares {
     int each;   // units of a share,

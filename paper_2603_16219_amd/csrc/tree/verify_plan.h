@@ -21,7 +21,7 @@ struct VerifyPlan {
 constexpr int kVerifyGroup = 256;                      // threads
 constexpr int kMassVecs = 4 * 64;                     // of a wave
 constexpr long kAllBytes = 160l << 20, kFirstBytes = 36l << 20;
-constexpr int kMaxParts = 16;                          // slices of a row
+constexpr int kMostSlices = 16;                        // of a row: as many as a walk reads sums of
 constexpr int kArriveBytes = 256;                      // between the counters of two sequences
 inline VerifyPlan verify_plan(const ss_params& p, int units) {
     const auto up = [](size_t n) { return (n + 255) / 256 * 256; };
@@ -47,8 +47,8 @@ inline VerifyPlan verify_plan(const ss_params& p, int units) {
     }
     // about four workgroups a unit in a stage of a few rows, eight in one of all, of 512 vectors each at least (64 trees, two rows first: 4 slices 68 us, 8 75;
     // 4 trees in one stage: 4 32, 8 29.5)
-    const long want = (long)(4.0 * units / tasks + 0.999), most = vecs / 512 > 0 ? vecs / 512 : 1;
-    r.slices = (int)(want < 1 ? 1 : want > most ? most : want > kMaxParts ? kMaxParts : want);
+    const long want = (long)(4.0 * units / tasks + 0.999), wide = vecs / 512 > 0 ? vecs / 512 : 1, most = wide < kMostSlices ? wide : kMostSlices;
+    r.slices = (int)(want < 1 ? 1 : want > most ? most : want);
     r.slice_vecs = (int)((vecs + r.slices - 1) / r.slices);
     for (int k = 0; k < r.stages; ++k) {
         const int rows = r.rows[k] < N + 1 ? r.rows[k] : (int)N + 1;

@@ -365,6 +365,19 @@ def test_walk_of_batches(tree, B):
     check_walk(tree, verify_inputs(B, 8, 3001, "bf16", B, ragged=True), lam=0.2, beta=0.5, temperature=0.8)
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("B,N,V", [(1, 2, 32000), (1, 1, 128256), (1, 7, 151936), (2, 20, 262147), (1, 3, 1 << 20)])
+def test_walk_counts_all_of_a_long_row(tree, B, N, V, dtype):
+    """Each model's mass lies in another part of the row; all of a few rows are shared by many workgroups."""
+    for seed in range(3):
+        i = verify_inputs(B, N, V, dtype, seed, "random")
+        i["G"][..., V - V // 8:] += 4
+        i["Sm"][..., :V // 8] += 4
+        i["tokens"][:] = torch.randint(0, V // 8, i["tokens"].shape, generator=gen(seed), device="cuda") + V // 2
+        i["uniforms"][:, :-1] *= 0.9
+        check_walk(tree, i, lam=0.7, beta=0.5)
+
+
 def test_walk_with_peaked_rows(tree):
     """Rows as models have them: few likely tokens, which the drafts are; long paths."""
     for B, N, V, kind in ((16, 31, 32000, "random"), (3, 12, 128256, "wide"), (40, 16, 20000, "chain")):
