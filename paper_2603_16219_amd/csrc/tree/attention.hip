@@ -343,18 +343,29 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
             const auto load_keys = [&](int stage) { load(0, lds0 + stage * C::kStage); };
             const auto load_values = [&](int t, int stage) { load(t < items.cached ? a.vc - a.kc : a.v - a.k, lds0 + stage * C::kStage + C::kTileBytes); };
 
-            // kHeld tiles are held, and half a tile is asked for as soon as its place is free: values of t + kHeld - 1 behind the products with the
-            // values of t - 1, keys of t + kHeld behind those with the keys of t.  All but one of the halves are on their way at any time.  Waves that
-            // share their keys meet at every half; others go on by themselves.
             constexpr int kAhead = C::kHeld - 1;
-            constexpr bool kShared = C::WM > 1;
+            constexpr bool kShared = C::WM > 1, kTurns = C::kWaves > 4;
+            const auto ask = [&](int t, int place) {  // values of t, whose keys were asked for last, and keys of t + 1
+                if (t >= t1) return;
+                load_values(t, place);
+                if (t + 1 >= t1) return;
+                locate(t + 1);
+                load_keys(place == kAhead ? 0 : place + 1);
+            };
+            if constexpr (kTurns) {
+                locate(t0);
+                load_keys(0);
 #pragma unroll
-            for (int i = 0; i < C::kHeld; ++i)
-                if (t0 + i < t1) {
-                    locate(t0 + i);
-                    load_keys(i);
-                    if (i < kAhead) load_values(t0 + i, i);
-                }
+                for (int i = 0; i < kAhead; ++i) ask(t0 + i, i);
+            } else {
+#pragma unroll
+                for (int i = 0; i < C::kHeld; ++i)
+                    if (t0 + i < t1) {
+                        locate(t0 + i);
+                        load_keys(i);
+                        if (i < kAhead) load_values(t0 + i, i);
+                    }
+            }
             x8 q[kSteps];  // behind the first loads of keys: they are all on their way together
             {
                 const char* const qp = a.q + 2 * (b * a.qs.a + min(row, s.N) * a.qs.b + query * a.qs.c) + 16 * half;
@@ -377,117 +388,178 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
                 }
                 __syncthreads();
             }
-            int at = 0;  // the place of tile t
-            for (int t = t0; t < t1; ++t) {
-                const bool own = t >= items.cached;  // a tile of the block's own rows, not of the cache
-                const char* const stage = lds + at * C::kStage + wk * kSub * 32 * C::kRowBytes;
-                const int limit = own ? s.N + 1 : s.L, base = (own ? t - items.cached : t) * C::kTile + wk * kSub * 32;  // of the block's rows, or of the cache
-                const bool some = base < limit;
-                arrived<C::kLoads, C::kHeld, kShared>(t1 - 1 - t);
-                // All reads of LDS before the first product: one by one, each waited for, they took most of a tile's time
-                f32x16 sc[kSub];
+            const char* const mine = lds + wk * kSub * 32 * C::kRowBytes;
+            f32x16 sc[kSub];
+            x8 weights[kSub][2];
+            // of tile t: whether it is of the block's own rows and not of the cache, the rows or positions that there are, the first of this wave's keys
+            const auto is_own = [&](int t) { return t >= items.cached; };
+            const auto limit_of = [&](int t) { return is_own(t) ? s.N + 1 : s.L; };
+            const auto base_of = [&](int t) { return (is_own(t) ? t - items.cached : t) * C::kTile + wk * kSub * 32; };
+            union Values {  // of 32 keys, transposed: 4 keys of a column each read
+                s16x4 h[2];
+                x8 all;
+            };
+            const auto read_keys = [&](int at, int sub, x8 (&k)[kSteps]) {
+                const int r = lane & 31, x = half ^ turn<D>(r);
+                const char* const kr = mine + at * C::kStage + (sub * 32 + r) * C::kRowBytes;
+#pragma unroll
+                for (int i = 0; i < kSteps; ++i) k[i] = *reinterpret_cast<const x8*>(kr + ((2 * i) ^ x) * 16);
+            };
+            const auto read_values = [&](int at, int sub, Values (&v)[kBlocks][2]) {
+                const char* const vt = mine + at * C::kStage + C::kTileBytes + sub * 32 * C::kRowBytes;
+                const int q4 = (lane & 15) >> 2, wide = lane >> 4 & 1;
+#pragma unroll
+                for (int db = 0; db < kBlocks; ++db)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = 8 * i + 4 * half + q4, piece = db * 4 + 2 * wide + ((lane & 3) >> 1);
+                        v[db][i / 2].h[i % 2] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(vt + r * C::kRowBytes + (piece ^ turn<D>(r)) * 16 + (lane & 1) * 8));
+                    }
+            };
+            const auto score = [&](int sub, const x8 (&k)[kSteps]) {
+                sc[sub] = f32x16{};
+#pragma unroll
+                for (int i = 0; i < kSteps; ++i) sc[sub] = mfma<DT>(k[i], q[i], sc[sub]);
+            };
+            const auto take = [&](int sub, const Values (&v)[kBlocks][2]) {
+#pragma unroll
+                for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+                    for (int db = 0; db < kBlocks; ++db) o[db] = mfma<DT>(v[db][kb].all, weights[sub][kb], o[db]);
+            };
+            const auto weigh = [&](int t) {
+                const bool own = is_own(t);
+                const int limit = limit_of(t), base = base_of(t);
+                if (own || limit - base < 32 * kSub)
+#pragma unroll
+                    for (int sub = 0; sub < kSub; ++sub) {
+                        const unsigned seen = seen_keys(own, a.parents != nullptr, base + 32 * sub, limit, row, s.N, up) >> (4 * half);
+#pragma unroll
+                        for (int i = 0; i < 16; ++i)
+                            if (!(seen >> (8 * (i / 4) + i % 4) & 1)) sc[sub][i] = -__builtin_huge_valf();
+                    }
+                float top = sc[0][0];
+#pragma unroll
+                for (int sub = 0; sub < kSub; ++sub)
+#pragma unroll
+                    for (int i = sub == 0 ? 1 : 0; i < 16; ++i) top = fmaxf(top, sc[sub][i]);
+                // one reference for all weights of the tile, which are products only later
+                top = halves_max(top) * a.scale;
+                const bool rise = top > m + H::kSlack;
+                if (__ballot(rise)) {
+                    const float to = rise ? top : m, by = __builtin_amdgcn_exp2f(m - to);
+                    m = to;
+                    l *= by;
+#pragma unroll
+                    for (int i = 0; i < kBlocks; ++i) o[i] *= by;
+                }
+                const float ref = H::kLift - m;
 #pragma unroll
                 for (int sub = 0; sub < kSub; ++sub) {
-                    x8 k[kSteps];
-                    const int r = lane & 31, x = half ^ turn<D>(r);
-                    const char* const kr = stage + (sub * 32 + r) * C::kRowBytes;
+                    float p[16];
 #pragma unroll
-                    for (int i = 0; i < kSteps; ++i) k[i] = *reinterpret_cast<const x8*>(kr + ((2 * i) ^ x) * 16);
-                    __builtin_amdgcn_sched_barrier(0);
-                    if (sub == 0) {
-                        if (t + kAhead < t1) load_values(t + kAhead, at > 0 ? at - 1 : kAhead);
-                        if (t + C::kHeld < t1) locate(t + C::kHeld);
+                    for (int i = 0; i < 16; ++i) {
+                        p[i] = __builtin_amdgcn_exp2f(fmaf(sc[sub][i], a.scale, ref));
+                        weights[sub][i / 8][i % 8] = (typename H::T)p[i];
                     }
-                    sc[sub] = f32x16{};
-#pragma unroll
-                    for (int i = 0; i < kSteps; ++i) sc[sub] = mfma<DT>(k[i], q[i], sc[sub]);
+                    l += tree_sum16(p);
                 }
-                x8 weights[kSub][2];
-                if (some) {
-                    if (own || limit - base < 32 * kSub)
+            };
+            // Values of the block that are not finite count for the rows that see them alone, which have NaN; a product with a weight of 0 is none
+            const auto look_at_own = [&](int t, int at) {
+                const int limit = limit_of(t), base = base_of(t);
+                unsigned odd[kSub];
 #pragma unroll
-                        for (int sub = 0; sub < kSub; ++sub) {
-                            const unsigned mine = seen_keys(own, a.parents != nullptr, base + 32 * sub, limit, row, s.N, up) >> (4 * half);
-#pragma unroll
-                            for (int i = 0; i < 16; ++i)
-                                if (!(mine >> (8 * (i / 4) + i % 4) & 1)) sc[sub][i] = -__builtin_huge_valf();
-                        }
-                    float top = sc[0][0];
-#pragma unroll
-                    for (int sub = 0; sub < kSub; ++sub)
-#pragma unroll
-                        for (int i = sub == 0 ? 1 : 0; i < 16; ++i) top = fmaxf(top, sc[sub][i]);
-                    // one reference for all weights of the tile, which are products only later
-                    top = halves_max(top) * a.scale;
-                    const bool rise = top > m + H::kSlack;
-                    if (__ballot(rise)) {
-                        const float to = rise ? top : m, by = __builtin_amdgcn_exp2f(m - to);
-                        m = to;
-                        l *= by;
-#pragma unroll
-                        for (int i = 0; i < kBlocks; ++i) o[i] *= by;
-                    }
-                    const float ref = H::kLift - m;
-#pragma unroll
-                    for (int sub = 0; sub < kSub; ++sub) {
-                        float p[16];
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) {
-                            p[i] = __builtin_amdgcn_exp2f(fmaf(sc[sub][i], a.scale, ref));
-                            weights[sub][i / 8][i % 8] = (typename H::T)p[i];
-                        }
-                        l += tree_sum16(p);
-                    }
-                }
-                arrived<C::kLoads, C::kHeld, kShared>(t1 - 1 - t);
-                if (own) {
-                    // Values of the block that are not finite count for the rows that see them alone, which have NaN; a product with a weight of 0 is none
-                    unsigned odd[kSub];
-#pragma unroll
-                    for (int sub = 0; sub < kSub; ++sub) {
-                        const char* const vr = stage + C::kTileBytes + (sub * 32 + (lane & 31)) * C::kRowBytes + half * D;
-                        unsigned is = 0;  // an exponent of all ones carries into the sign's bit
+                for (int sub = 0; sub < kSub; ++sub) {
+                    const char* const vr = mine + at * C::kStage + C::kTileBytes + (sub * 32 + (lane & 31)) * C::kRowBytes + half * D;
+                    unsigned is = 0;  // an exponent of all ones carries into the sign's bit
 #pragma unroll 4
-                        for (int i = 0; i < D / 4; ++i) is |= (reinterpret_cast<const unsigned*>(vr)[i] & 0x7FFF7FFFu) + 0x10001u * (0x8000u - H::kExponent);
-                        const unsigned long long ballot = __ballot((is & 0x80008000u) != 0);
-                        odd[sub] = (unsigned)ballot | (unsigned)(ballot >> 32);
-                        if (odd[sub] && limit - base > 32 * sub && (odd[sub] & seen_keys(true, a.parents != nullptr, base + 32 * sub, limit, row, s.N, up)))
-                            l = __builtin_nanf("");
+                    for (int i = 0; i < D / 4; ++i) is |= (reinterpret_cast<const unsigned*>(vr)[i] & 0x7FFF7FFFu) + 0x10001u * (0x8000u - H::kExponent);
+                    const unsigned long long ballot = __ballot((is & 0x80008000u) != 0);
+                    odd[sub] = (unsigned)ballot | (unsigned)(ballot >> 32);
+                    if (odd[sub] && limit - base > 32 * sub && (odd[sub] & seen_keys(true, a.parents != nullptr, base + 32 * sub, limit, row, s.N, up)))
+                        l = __builtin_nanf("");
+                }
+                __syncthreads();  // other waves look at the same values
+#pragma unroll
+                for (int sub = 0; sub < kSub; ++sub)
+                    if (odd[sub] >> (lane & 31) & 1) {
+                        char* const vr = lds + (mine - lds) + at * C::kStage + C::kTileBytes + (sub * 32 + (lane & 31)) * C::kRowBytes + half * D;
+                        for (int i = 0; i < D / 4; ++i) reinterpret_cast<unsigned*>(vr)[i] = 0;
                     }
-                    __syncthreads();  // other waves look at the same values
+                __syncthreads();
+            };
+            int at = 0;  // the place of tile t
+            if constexpr (kTurns) {
+                // Two waves a SIMD: between two barriers the first four take a tile's values, score the next one's keys and weigh them, the others weigh a
+                // tile's keys, take its values and score the next one's, so that the matrix unit has one wave's products while the other's weights
+                // are formed.  Keys of t and values of t - 1 are done with at the barrier of t, and their places asked for again.
+                const bool later = wave >= 4;
+                if (t1 - t0 >= C::kHeld) wait_loads<2 * C::kLoads * kAhead>();
+                else wait_loads<0>();
+                asm volatile("s_barrier" : : : "memory");
+                const auto score_tile = [&](int place) {
 #pragma unroll
-                    for (int sub = 0; sub < kSub; ++sub)
-                        if (odd[sub] >> (lane & 31) & 1) {
-                            char* const vr = lds + (stage - lds) + C::kTileBytes + (sub * 32 + (lane & 31)) * C::kRowBytes + half * D;
-                            for (int i = 0; i < D / 4; ++i) reinterpret_cast<unsigned*>(vr)[i] = 0;
-                        }
-                    __syncthreads();
+                    for (int sub = 0; sub < kSub; ++sub) {
+                        x8 k[kSteps];
+                        read_keys(place, sub, k);
+                        __builtin_amdgcn_sched_barrier(0);
+                        score(sub, k);
+                    }
+                };
+                score_tile(0);
+                if (!later) weigh(t0);
+                for (int t = t0; t < t1; ++t) {
+                    const int next = at == kAhead ? 0 : at + 1;
+                    if (t1 - 1 - t >= kAhead) wait_loads<2 * C::kLoads*(C::kHeld - 2)>();
+                    else wait_loads<0>();
+                    asm volatile("s_barrier" : : : "memory");
+                    if (is_own(t)) look_at_own(t, at);
+                    ask(t + kAhead, at > 0 ? at - 1 : kAhead);
+                    if (later) weigh(t);
+#pragma unroll
+                    for (int sub = 0; sub < kSub; ++sub) {
+                        Values v[kBlocks][2];
+                        read_values(at, sub, v);
+                        __builtin_amdgcn_sched_barrier(0);
+                        take(sub, v);
+                    }
+                    if (t + 1 < t1) score_tile(next);
+                    if (!later && t + 1 < t1) weigh(t + 1);
+                    at = next;
                 }
+            } else {
+                // kHeld tiles are held, and half a tile is asked for as soon as its place is free: values of t + kHeld - 1 behind the products with the
+                // values of t - 1, keys of t + kHeld behind those with the keys of t.  All but one of the halves are on their way at any time.  Waves that
+                // share their keys meet at every half; others go on by themselves.
+                for (int t = t0; t < t1; ++t) {
+                    const bool some = base_of(t) < limit_of(t);
+                    arrived<C::kLoads, C::kHeld, kShared>(t1 - 1 - t);
+                    // All reads of LDS before the first product: one by one, each waited for, they took most of a tile's time
 #pragma unroll
-                for (int sub = 0; sub < kSub; ++sub) {
-                    // the values, transposed: 4 keys of a column each read
-                    union {
-                        s16x4 h[2];
-                        x8 all;
-                    } v[kBlocks][2];
-                    const char* const vt = stage + C::kTileBytes + sub * 32 * C::kRowBytes;
-                    const int q4 = (lane & 15) >> 2, wide = lane >> 4 & 1;
-#pragma unroll
-                    for (int db = 0; db < kBlocks; ++db)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            const int r = 8 * i + 4 * half + q4, piece = db * 4 + 2 * wide + ((lane & 3) >> 1);
-                            v[db][i / 2].h[i % 2] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s16x4*)(vt + r * C::kRowBytes + (piece ^ turn<D>(r)) * 16 + (lane & 1) * 8));
+                    for (int sub = 0; sub < kSub; ++sub) {
+                        x8 k[kSteps];
+                        read_keys(at, sub, k);
+                        __builtin_amdgcn_sched_barrier(0);
+                        if (sub == 0) {
+                            if (t + kAhead < t1) load_values(t + kAhead, at > 0 ? at - 1 : kAhead);
+                            if (t + C::kHeld < t1) locate(t + C::kHeld);
                         }
-                    __builtin_amdgcn_sched_barrier(0);
-                    if (sub == 0 && t + C::kHeld < t1) load_keys(at);
-                    if (some)
+                        score(sub, k);
+                    }
+                    if (some) weigh(t);
+                    arrived<C::kLoads, C::kHeld, kShared>(t1 - 1 - t);
+                    if (is_own(t)) look_at_own(t, at);
 #pragma unroll
-                        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-                            for (int db = 0; db < kBlocks; ++db) o[db] = mfma<DT>(v[db][kb].all, weights[sub][kb], o[db]);
+                    for (int sub = 0; sub < kSub; ++sub) {
+                        Values v[kBlocks][2];
+                        read_values(at, sub, v);
+                        __builtin_amdgcn_sched_barrier(0);
+                        if (sub == 0 && t + C::kHeld < t1) load_keys(at);
+                        if (some) take(sub, v);
+                    }
+                    at = at == kAhead ? 0 : at + 1;
                 }
-                at = at == kAhead ? 0 : at + 1;
             }
             l += __shfl_xor(l, 32, kWave);
         }
