@@ -10,11 +10,13 @@
 // every row's first accepted child is found at once, and the walk follows them.
 //
 // What bounds it are the launches' beginnings, a chain of loads and two logarithms that each has to walk before it can load a row, and rows that the walk does
-// not come through in the end.  64 trees of up to 31 nodes, V = 128256 bf16: 74 us, of which the stages of rows take 23 and 25 and the draw 22; one tree of 12
+// not come through in the end.  64 trees of up to 31 nodes, V = 128256 bf16: 70 us, of which the stages of rows take 16 and 30 and the draw 22; one tree of 12
 // nodes, V = 32000 fp32, 17, of which the draw 12.
 #include "../loss/loss_rows.h"
 #include "tree_common.h"
 #include "verify_plan.h"
+
+#include <type_traits>
 
 namespace {
 
@@ -401,6 +403,10 @@ __global__ __launch_bounds__(kVerifyGroup) void rows_kernel(const VerifyArgs a, 
     const int per = groups * 2 * a.slices, b = (int)(blockIdx.x / (unsigned)per), id = (int)(blockIdx.x - (unsigned)(b * per));
     const int slice = id % a.slices, x = id / a.slices & 1, group = id / (2 * a.slices);
     const bool leader = id == 0;
+    // a small tree's tokens, a lane each, beside the walk's loads, and their logits beside the row's: behind the sums both took two round trips more
+    constexpr bool kSmallTree = std::is_same<W, SmallShared>::value;
+    const int i_mine = threadIdx.x;
+    const int token = kSmallTree && slice == 0 && i_mine < a.N ? a.tokens[(long)b * a.N + i_mine] : 0;
     const int N = reach<DT>(a, b, stage, rows_before, rows, leader, w);
     if (leader && threadIdx.x == 0) {
         a.cursors[(long)stage * a.B + b] = w.at;
@@ -413,8 +419,13 @@ __global__ __launch_bounds__(kVerifyGroup) void rows_kernel(const VerifyArgs a, 
         const void* const h = row_ptr<DT>(x ? a.Sm : a.G, b * a.sb + r * a.st);
         const Layout<DT> lay(h, a.V, threadIdx.x);
         const int begin = min(lay.vecs, slice * a.slice_vecs), end = slice + 1 == a.slices ? lay.vecs : min(lay.vecs, begin + a.slice_vecs);
+        const bool child = kSmallTree && slice == 0 && i_mine < N && w.parent[i_mine] == r - 1;
+        float child_logit = 0.f;
+        if (child) child_logit = ld_elem<DT>(h, token);
         const Sum mine = lane_sum<DT, Sum, 2, true>(h, nullptr, lay, begin + threadIdx.x, end, kVerifyGroup, slice == 0, a.c);
-        if (slice == 0)
+        asm volatile("" : "+v"(child_logit));  // not loaded later
+        if (child) reinterpret_cast<float*>(a.logits + (long)b * a.N + i_mine)[x] = child_logit;
+        if (!kSmallTree && slice == 0)
             for (int i = r + threadIdx.x; i < N; i += kVerifyGroup)  // children lie behind their parent, node r - 1
                 if (w.parent[i] == r - 1)
                     reinterpret_cast<float*>(a.logits + (long)b * a.N + i)[x] = ld_elem<DT>(h, a.tokens[(long)b * a.N + i]);

@@ -45,17 +45,18 @@ inline VerifyPlan verify_plan(const ss_params& p, int units) {
         r.rows[1] = (int)N + 1;
         tasks *= r.rows[0];
     }
-    // about four workgroups a unit in a stage of a few rows, eight in one of all, of 512 vectors each at least (64 trees, two rows first: 4 slices 68 us, 8 75;
+    // about four workgroups a unit in a stage of a few rows, of 512 vectors each at least (64 trees, two rows first: 4 slices 68 us, 8 75;
     // 4 trees in one stage: 4 32, 8 29.5)
     const long want = (long)(4.0 * units / tasks + 0.999), wide = vecs / 512 > 0 ? vecs / 512 : 1, most = wide < kMostSlices ? wide : kMostSlices;
     r.slices = (int)(want < 1 ? 1 : want > most ? most : want);
     r.slice_vecs = (int)((vecs + r.slices - 1) / r.slices);
     for (int k = 0; k < r.stages; ++k) {
         const int rows = r.rows[k] < N + 1 ? r.rows[k] : (int)N + 1;
-        // a stage of any number of rows: as many as fill the chip, the others behind them
+        // a stage of any number of rows: as many as fill the chip, the others behind them (64 trees of 31 nodes: two a slice 72 us, three 67, four 68; 256
+        // of 8: 127, 119, 126)
         long g = rows;
         if (k + 1 == r.stages) {
-            const long fill = (8l * units + 2 * B * r.slices - 1) / (2 * B * r.slices);
+            const long fill = (6l * units + 2 * B * r.slices - 1) / (2 * B * r.slices);
             g = g < fill ? g : fill;
         }
         r.groups[k] = (int)(g < 1 ? 1 : g);
