@@ -629,6 +629,46 @@ def test_calls_from_two_streams_at_once(tree):
             assert torch.equal(p, q)
 
 
+def test_calls_from_several_threads(tree):
+    """Each thread with a stream of its own, all at once, from Python threads that switch inside of the calls."""
+    import threading
+
+    from paper_2603_16219_amd import losses
+
+    made = [(make(3, 4 + 9 * n, 8, 2, 64 if n % 2 else 128, [300 * n, 64, 5], 16, seed=n), verify_inputs(3, 9 + n, 9000 + n, "bf16", n)) for n in range(4)]
+    torch.cuda.synchronize()
+
+    def block(i, v):
+        kc, vc = i["k_cache"].clone(), i["v_cache"].clone()
+        w = walk(tree, v)
+        some = dict(accepted_len=w["accepted_len"].clamp(max=i["k"].shape[1] - 1))
+        new = tree.commit(i["k"], i["v"], kc, vc, i["table"], i["cache_len"] // 2, some["accepted_len"])
+        top = losses.token_alternatives(v["G"], topk=5)
+        return [run(tree, i), new, kc, vc, *w.values(), top["top_tokens"], top["top_logprobs"], top["entropy"]]
+
+    want = [block(*m) for m in made]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(n):
+        try:
+            with torch.cuda.stream(torch.cuda.Stream()):
+                for _ in range(15):
+                    got = block(*made[n])
+                    torch.cuda.current_stream().synchronize()
+                    if not all(torch.equal(a.nan_to_num(7), b.nan_to_num(7)) for a, b in zip(got, want[n])):
+                        wrong.append(n)
+        except Exception as e:  # what ends a thread would be lost
+            wrong.append(e)
+
+    threads = [threading.Thread(target=work, args=(n,)) for n in range(4)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not wrong, wrong
+
+
 def test_a_block_of_a_small_model(tree):
     """From the specialist's alternatives to the cache of the next block: a tree grown, scored through an attention layer, walked, kept; the cached
     sequence then gives what a single pass over it gives."""
