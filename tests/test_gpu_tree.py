@@ -99,6 +99,14 @@ def test_long_caches(tree, L, B, Hq, H):
     check(tree, make(B, 0, Hq, H, 64, [L - 1111 * b for b in range(B)], 16, "f16", kind="none"))
 
 
+@pytest.mark.parametrize("N,Hq,H", [(40, 8, 2), (70, 16, 2), (130, 3, 1)])
+@pytest.mark.parametrize("page", [1, 7, 64])
+def test_wide_trees_over_long_caches(tree, N, Hq, H, page):
+    """More columns than a workgroup of four waves has; with small pages a sequence's table comes in pieces, a new one inside of a share."""
+    check(tree, make(2, N, Hq, H, 128, [5003, 1100], page, kind="random"))
+    check(tree, make(3, N, Hq, H, 64, [2500, 0, 3333], page, "f16", kind="wide", ragged=True))
+
+
 @pytest.mark.parametrize("B", [1, 2, 31, 64, 257, 600])
 def test_batches_of_any_lengths(tree, B):
     g = torch.Generator().manual_seed(B)
