@@ -327,15 +327,16 @@ __device__ __forceinline__ void write_none(const AltArgs& a, long row, int threa
         a.top_logprobs[row * a.topk + i] = -__builtin_huge_valf();
     }
 }
+// The given token and its logit, for the first thread, asked for beside other loads: behind the sums they are two round trips.
+__device__ __forceinline__ int given_token(const AltArgs& a, long row) { return a.logprobs && threadIdx.x == 0 ? a.r.tokens[row] : -1; }
+template <int DT>
+__device__ __forceinline__ float given_logit(const AltArgs& a, const void* h, int y) { return y >= 0 && y < a.r.V ? ld_elem<DT>(h, y) : 0.f; }
+
 // What is written of a row whose sums and, in f.ranked, likeliest tokens are known.
 template <int DT, bool TOP>
-__device__ __forceinline__ void finish(const AltArgs& a, long row, const void* h, bool far, const Total<SumX>& s, int threads, const Finder* f) {
+__device__ __forceinline__ void finish(const AltArgs& a, long row, int y, float hy, bool far, const Total<SumX>& s, int threads, const Finder* f) {
     if (threadIdx.x == 0) {
-        double lp = 0.0;
-        if (a.logprobs) {
-            const int y = a.r.tokens[row];
-            lp = token_logprob<1>(a.r, far, y, y >= 0 && y < a.r.V ? ld_elem<DT>(h, y) : 0.f, s.E, s.s);
-        }
+        const double lp = a.logprobs ? token_logprob<1>(a.r, far, y, hy, s.E, s.s) : 0.0;
         // the statistics are those of the whole c
         write_row(a, row, lp, entropy_of(a.r, far, s), s.E, far ? -s.s : s.s * exp2((double)s.E * a.r.rest));
     }
@@ -369,14 +370,16 @@ __global__ __launch_bounds__(kAltThreads) __attribute__((amdgpu_waves_per_eu(4))
     place(a.r, row, at, grad_at);
     const void* const h = row_ptr<DT>(a.r.logits, at);
     const Layout<DT> lay(h, a.r.V, threadIdx.x);
+    const int y = given_token(a, row);
     const SumX mine = a.keep ? scan<DT, TOP, false>(a, h, lay, 0, lay.vecs, true, kAltThreads, f) : scan<DT, TOP, true>(a, h, lay, 0, lay.vecs, true, kAltThreads, f);
+    const float hy = given_logit<DT>(a, h, y);
     Total<SumX> s = block_total(mine, kAltThreads, part);
     const bool far = a.r.far || is_far(s);
     if (far) s = far_sum_x<DT>(h, a.r.V, a.r.c64, kAltThreads, part);
     if (TOP) {
         if (!shortlist<DT>(*f, h, block_bound(*f, kAltThreads / kWave), kAltThreads)) find_slowly<DT>(*f, h, 0, a.r.V, a.topk, kAltThreads);
     }
-    finish<DT, TOP>(a, row, h, far, s, kAltThreads, f);
+    finish<DT, TOP>(a, row, y, hy, far, s, kAltThreads, f);
 }
 
 // Few rows: several workgroups each, whose sums and likeliest tokens a second launch joins.
@@ -425,10 +428,14 @@ __global__ __launch_bounds__(256) void alternatives_join_kernel(const AltArgs a)
     place(a.r, row, at, grad_at);
     const void* const h = row_ptr<DT>(a.r.logits, at);
     const int lane = threadIdx.x & 63;
+    // all that does not wait for anything is asked for at once
+    const int y = given_token(a, row), count = a.slices * a.topk;
+    const Total<SumX> sums = a.parts[row * a.slices + (lane < a.slices ? lane : 0)];
     if (TOP) {
         // each slice's q-th, q slices' worth of n: the least of them is reached by n tokens at least
         const unsigned long long* const keys = a.keys + row * a.slices * a.topk;
         const int q = (a.topk + a.slices - 1) / a.slices;
+        const unsigned long long ahead = (int)threadIdx.x < count ? keys[threadIdx.x] : 0;
         unsigned o = lane < a.slices ? (unsigned)(keys[lane * a.topk + q - 1] >> 32) : 0xFFFFFFFFu;
         for (int d = 1; d < kWave; d <<= 1) o = min(o, (unsigned)__shfl_xor((int)o, d, kWave));
         if (threadIdx.x == 0) {
@@ -436,20 +443,21 @@ __global__ __launch_bounds__(256) void alternatives_join_kernel(const AltArgs a)
             f->ranked_count = 0;
         }
         __syncthreads();
-        for (int i = threadIdx.x; i < a.slices * a.topk; i += kThreads) {
-            const unsigned long long k = keys[i];
+        for (int i = threadIdx.x; i < count; i += kThreads) {
+            const unsigned long long k = i == (int)threadIdx.x ? ahead : keys[i];
             if (k && (unsigned)(k >> 32) >= least) {
                 const int to = atomicAdd(&f->ranked_count, 1);
                 if (to < kRanked) f->ranked[to] = k;
             }
         }
-        __syncthreads();
     }
-    Total<SumX> s = join(a.parts[row * a.slices + (lane < a.slices ? lane : 0)], a.slices);
+    const float hy = given_logit<DT>(a, h, y);
+    __syncthreads();
+    Total<SumX> s = join(sums, a.slices);
     const bool far = a.r.far || is_far(s);
     if (far) s = far_sum_x<DT>(h, a.r.V, a.r.c64, kThreads, part);
     if (TOP && f->ranked_count > kRanked) find_slowly<DT>(*f, h, 0, a.r.V, a.topk, kThreads);
-    finish<DT, TOP>(a, row, h, far, s, kThreads, f);
+    finish<DT, TOP>(a, row, y, hy, far, s, kThreads, f);
 }
 
 // ------------------------------------------------------------------ gradient
