@@ -116,7 +116,7 @@ ss_status specsteer_tree_verify(const void *G, const void *S_ctx, const void *S_
  * of the cache; new_len[b] = cache_len[b] + accepted_len[b] + 1.  Other positions keep what they hold.
  *
  *   k, v              device, [B, N + 1, kv_heads, head_dim]
- *   k_cache, v_cache  device, read as described above and written; no memory of k or v
+ *   k_cache, v_cache  device, laid out as described above; no memory of k, v or each other
  *   accepted_len      device, [B] int32, 0..N
  *   path              device, [B, N] int32, or NULL: 0, 1, 2, ..., a chain's
  *   new_len           device, [B] int32 out; not cache_len itself

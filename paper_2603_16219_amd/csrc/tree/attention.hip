@@ -14,9 +14,9 @@
 //
 // Bytes: the cache once a call for up to 256 columns, whose products take 4 D flop a column for 4 D bytes a key.  Measured, main launch and join: 32 trees of 24
 // nodes over up to 4096 tokens (32 heads over 8, D = 128, bf16; 411 MB) 111 us, 3.7 TB/s; the same without loads 101 us: products, softmax and LDS in turn.
-// 8 rows (32 columns) instead of 25 over the same cache take 95 us.  4 times 64 rows over 65536 tokens (275 GFLOP) 365 us, 750 TFLOP/s; 128 chains of 8 over up to 2000 tokens (16 heads,
-// D = 64, fp16; 792 MB) 161 us, 4.9 TB/s.  One token over 1000 takes 14 us: a launch that finds its place in the batch before its first load (6 to 8 us), and
-// the join's 4.
+// 8 rows (32 columns) instead of 25 over the same cache take 95 us.  4 times 64 rows over 65536 tokens (275 GFLOP) 330 to 356 us, 770 to 830 TFLOP/s; 128
+// chains of 8 over up to 2000 tokens (16 heads, D = 64, fp16; 792 MB) 161 us, 4.9 TB/s.  One token over 1000 takes 14 us: a launch that finds its place in
+// the batch before its first load (6 to 8 us), and the join's 4.
 #include "tree_common.h"
 #include "tree_schedule.h"
 
@@ -277,7 +277,8 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
         }
         const int nt = items.tiles();
         // the same for all lanes, which the compiler does not see: vector compares and masks around every step took 4 per cent of the long cache's time
-        const int item = __builtin_amdgcn_readfirstlane(rel / nt), t0 = __builtin_amdgcn_readfirstlane(rel - item * nt), t1 = __builtin_amdgcn_readfirstlane(min(nt, t0 + (u_end - u)));
+        const int item = __builtin_amdgcn_readfirstlane(rel / nt), t0 = __builtin_amdgcn_readfirstlane(rel - item * nt);
+        const int t1 = __builtin_amdgcn_readfirstlane(min(nt, t0 + (u_end - u)));
         const int head = item / items.blocks, block = item - head * items.blocks;
         // this lane's column: a row of the tree and a query head
         const int place_of = wm * 32 + (lane & 31), column = block * C::kColumns + place_of;
@@ -493,7 +494,8 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
             if constexpr (kTurns) {
                 // Two waves a SIMD: between two barriers the first four take a tile's values, score the next one's keys and weigh them, the others weigh a
                 // tile's keys, take its values and score the next one's, so that the matrix unit has one wave's products while the other's weights
-                // are formed.  Keys of t and values of t - 1 are done with at the barrier of t, and their places asked for again.
+                // are formed: 4 times 64 rows over 65536 tokens 330 us, 365 with all waves in step.  Keys of t and values of t - 1 are done with at the
+                // barrier of t, and their places asked for again.
                 const bool later = wave >= 4;
                 if (t1 - t0 >= C::kHeld) wait_loads<2 * C::kLoads * kAhead>();
                 else wait_loads<0>();

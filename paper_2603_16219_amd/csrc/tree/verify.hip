@@ -10,7 +10,7 @@
 // every row's first accepted child is found at once, and the walk follows them.
 //
 // What bounds it are the launches' beginnings, a chain of loads and two logarithms that each has to walk before it can load a row, and rows that the walk does
-// not come through in the end.  64 trees of up to 31 nodes, V = 128256 bf16: 70 us, of which the stages of rows take 16 and 30 and the draw 22; one tree of 12
+// not come through in the end.  64 trees of up to 31 nodes, V = 128256 bf16: 69 to 74 us, of which the stages of rows take 16 and 30 and the draw 22; one tree of 12
 // nodes, V = 32000 fp32, 17, of which the draw 12.
 #include "../loss/loss_rows.h"
 #include "tree_common.h"

@@ -114,6 +114,10 @@ def test_no_sequences_need_no_arrays(tree, name):
     assert call(tree, name, batch=0, **{k: None for k in ORDER[name] if k not in ("params", "stream", "bytes")}) == OK
 
 
+def test_commit_refuses_one_cache_for_keys_and_values(tree):
+    assert call(tree, "commit", k_cache=AT, v_cache=AT) == PARAM
+
+
 def test_accepted_layouts(tree):
     """Refused for the workspace only, which is looked at last: pages of [heads, slots, dim], gaps, strides of dimensions of one element."""
     for more in (dict(cache_stride=(2048, 64, 1024)), dict(k_stride=(8192, 512, 64), q_stride=(1 << 20, 1024, 128)), dict(out_stride=(64, 1024, 128)),
