@@ -10,7 +10,7 @@
 // every row's first accepted child is found at once, and the walk follows them.
 //
 // What bounds it are the launches' beginnings, a chain of loads and two logarithms that each has to walk before it can load a row, and rows that the walk does
-// not come through in the end.  64 trees of up to 31 nodes, V = 128256 bf16: 69 to 74 us, of which the stages of rows take 16 and 30 and the draw 22; one tree of 12
+// not come through in the end.  64 trees of up to 31 nodes, V = 128256 bf16: 63 to 70 us, of which the stages of rows take 16 and 25 and the draw 22; one tree of 12
 // nodes, V = 32000 fp32, 17, of which the draw 12.
 #include "../loss/loss_rows.h"
 #include "tree_common.h"
@@ -396,6 +396,40 @@ __device__ __forceinline__ int nth_row(const SmallShared& w, int k) {
 __device__ __forceinline__ double* space_of(WalkShared& w) { return w.diff; }
 __device__ __forceinline__ double* space_of(SmallShared& w) { return w.table; }
 
+// One lane's share of a slice, some sixteen vectors: eight on their way at a time, the last ones too.  By four, and the last ones one by one, 64 trees of up to
+// 31 nodes took 67 us and not 63, 16 of 60 50 and not 46, 256 of 8 (four times the vectors a lane) 120 and not 124; four with the next four behind them 67, 47 and
+// 127, sixteen 66, 54 and 125.
+template <int DT>
+__device__ __forceinline__ Sum slice_sum(const void* h, const Layout<DT>& lay, int begin, int end, bool extra, Factor c) {
+    constexpr int kVec = Row<DT>::kVec, kUnroll = 8, kElem = DT == SS_BF16 ? 2 : 4;
+    const char* const hv = static_cast<const char*>(h) + (long)lay.head * kElem;
+    Sum a;
+    clear(a);
+    typename Row<DT>::Raw r[kUnroll];
+    const auto load = [&](int from, typename Row<DT>::Raw (&to)[kUnroll]) {
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            const int v = from + u * kVerifyGroup + (int)threadIdx.x;
+            to[u] = neg_inf_raw<DT, kVec>();
+            if (v < end) to[u] = ld_once<DT>(hv, v);
+        }
+    };
+    for (int i = begin; i < end; i += kUnroll * kVerifyGroup) {
+        load(i, r);
+#pragma unroll
+        for (int u = 0; u < kUnroll; ++u) {
+            float x[kVec];
+            unpack(r[u], x);
+            add<2>(a, x, c);
+        }
+    }
+    if (extra && lay.extra >= 0) {
+        const float x[1] = {ld_elem<DT>(h, lay.extra)};
+        add<2>(a, x, c);
+    }
+    return a;
+}
+
 // Stage `stage`: the sums of one slice of some of its rows.
 template <int DT, typename W>
 __global__ __launch_bounds__(kVerifyGroup) void rows_kernel(const VerifyArgs a, const int stage, const int rows_before, const int rows, const int groups) {
@@ -422,7 +456,7 @@ __global__ __launch_bounds__(kVerifyGroup) void rows_kernel(const VerifyArgs a, 
         const bool child = kSmallTree && slice == 0 && i_mine < N && w.parent[i_mine] == r - 1;
         float child_logit = 0.f;
         if (child) child_logit = ld_elem<DT>(h, token);
-        const Sum mine = lane_sum<DT, Sum, 2, true>(h, nullptr, lay, begin + threadIdx.x, end, kVerifyGroup, slice == 0, a.c);
+        const Sum mine = slice_sum<DT>(h, lay, begin, end, slice == 0, a.c);
         asm volatile("" : "+v"(child_logit));  // not loaded later
         if (child) reinterpret_cast<float*>(a.logits + (long)b * a.N + i_mine)[x] = child_logit;
         if (!kSmallTree && slice == 0)
