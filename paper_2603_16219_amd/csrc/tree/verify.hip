@@ -535,6 +535,15 @@ __device__ __forceinline__ void unpack_chunk(const Chunk<DT>& k, float (&g)[Row<
 #pragma unroll
     for (int i = 0; i < kVec; ++i) d[i] = sp[i] == sm[i] ? 0.f : sp[i] - sm[i];
 }
+template <typename T>
+__device__ __forceinline__ T either(bool first, const T& a, const T& b) {  // of registers
+    typedef unsigned u32v4 __attribute__((ext_vector_type(4)));
+    const u32v4 x = __builtin_bit_cast(u32v4, a), y = __builtin_bit_cast(u32v4, b);
+    u32v4 r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r[i] = first ? x[i] : y[i];
+    return __builtin_bit_cast(T, r);
+}
 constexpr int kMassSteps = kMassVecs / kWave;
 
 // What workgroups hand over inside a launch goes past the caches of one die with stores and loads at device scope; a wave has delivered when its
@@ -730,56 +739,63 @@ __global__ __launch_bounds__(kVerifyGroup) void draw_kernel(const VerifyArgs a, 
     Chunk<DT> k[kMassSteps];
 #pragma unroll
     for (int s = 0; s < kMassSteps; ++s) k[s] = load_chunk<DT>(a, row, chunk, s);
-    int token = -1, last = 0;
-    double y_token = 0.0, y_last = 0.0;
-    for (int s = 0; s < kMassSteps && token < 0; ++s) {
+    // all its steps' sums at once, the token in the step that passes the target
+    double in[kMassSteps], from[kMassSteps + 1];
+    from[0] = start;
+#pragma unroll
+    for (int s = 0; s < kMassSteps; ++s) {
+        float g[kVec], d[kVec];
+        double own = 0.0;
+        unpack_chunk<DT>(k[s], g, d);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) own += (double)exp2_hw(rec_exponent(a, g[i], d[i], cE));
+        in[s] = wave_incl_scan_f64(own * scale);
+    }
+#pragma unroll
+    for (int s = 0; s < kMassSteps; ++s) from[s + 1] = from[s] + wave_last_f64(in[s]);
+    int first = kMassSteps;
+#pragma unroll
+    for (int s = kMassSteps - 1; s >= 0; --s)
+        if (!take_last && from[s + 1] > target) first = s;
+    int token = -1;
+    double y_token = 0.0;
+    // of step s the first token that passes the target, or the last one with any mass
+    const auto look = [&](int s, bool last) {
         Chunk<DT> now = k[0];
+        double cum = from[0], incl = in[0];
 #pragma unroll
         for (int v = 1; v < kMassSteps; ++v)
-            if (s == v) now = k[v];
-        float g[kVec], d[kVec], e[kVec];
-        double own = 0.0;
+            {
+                now.g = either(s == v, k[v].g, now.g);
+                now.sp = either(s == v, k[v].sp, now.sp);
+                now.sm = either(s == v, k[v].sm, now.sm);
+                now.id = s == v ? k[v].id : now.id;
+                cum = s == v ? from[v] : cum;
+                incl = s == v ? in[v] : incl;
+            }
+        cum += wave_shift_up_f64(incl);
+        float g[kVec], d[kVec], g_hit = 0.f, d_hit = 0.f;
+        int hit = -1;
         unpack_chunk<DT>(now, g, d);
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
-            e[i] = exp2_hw(rec_exponent(a, g[i], d[i], cE));
-            own += (double)e[i];
-        }
-        const double in = wave_incl_scan_f64(own * scale);
-        double cum = start + wave_shift_up_f64(in);
-        int hit = -1, some = -1;
-        float g_hit = 0.f, g_some = 0.f, d_hit = 0.f, d_some = 0.f;
-#pragma unroll
-        for (int i = 0; i < kVec; ++i) {
-            cum += (double)e[i] * scale;
-            if (e[i] > 0.f) {
-                some = now.id + i;
-                g_some = g[i];
-                d_some = d[i];
-                if (hit < 0 && !take_last && cum > target) {
-                    hit = some;
-                    g_hit = g[i];
-                    d_hit = d[i];
-                }
+            const float e = exp2_hw(rec_exponent(a, g[i], d[i], cE));
+            cum += (double)e * scale;
+            if (e > 0.f && (last || (hit < 0 && cum > target))) {
+                hit = now.id + i;
+                g_hit = g[i];
+                d_hit = d[i];
             }
         }
-        const unsigned long long hits = __ballot(hit >= 0), somes = __ballot(some >= 0);
-        if (hits) {
-            const int L = first_lane(hits);
-            token = __shfl(hit, L, kWave);
-            y_token = rec_exponent64(a, (double)__shfl(g_hit, L, kWave), (double)__shfl(d_hit, L, kWave));
-        }
-        if (somes) {
-            const int L = 63 - __clzll((long long)somes);
-            last = __shfl(some, L, kWave);
-            y_last = rec_exponent64(a, (double)__shfl(g_some, L, kWave), (double)__shfl(d_some, L, kWave));
-        }
-        start += wave_last_f64(in);
-    }
-    if (token < 0) {
-        token = last;
-        y_token = y_last;
-    }
+        const unsigned long long hits = __ballot(hit >= 0);
+        if (!hits) return;
+        const int L = last ? 63 - __clzll((long long)hits) : first_lane(hits);
+        token = __shfl(hit, L, kWave);
+        y_token = rec_exponent64(a, (double)__shfl(g_hit, L, kWave), (double)__shfl(d_hit, L, kWave));
+    };
+    for (int s = first; s < kMassSteps && token < 0; ++s) look(s, false);
+    for (int s = kMassSteps - 1; s >= 0 && token < 0; --s) look(s, true);
+    token = max(token, 0);
     if (lane == 0) {
         a.next_token[b] = min(token, a.V - 1);
         if (a.next_logprob) a.next_logprob[b] = (float)((y_token - log2Z) * kLn2);
