@@ -117,8 +117,9 @@ __device__ __forceinline__ float key_logit(unsigned long long k) { return unorde
 __device__ __forceinline__ int key_id(unsigned long long k) { return (int)(0xFFFFFFFFu - (unsigned)k); }
 
 constexpr int kHits = 4096, kRanked = 1024;  // tokens that reached a bound, and the last one
+constexpr int kRankedAtOnce = 8;
 struct Finder {
-    unsigned long long ranked[kRanked];
+    alignas(16) unsigned long long ranked[kRanked + kRankedAtOnce];
     int hits[kHits];  // ids
     float bound[kUnitWaves];  // of every wave
     int hit_count, ranked_count, digit, above;
@@ -274,6 +275,10 @@ __device__ __forceinline__ SumX scan(const AltArgs& a, const void* h, const Layo
             }
         }
     }
+    if (TOP) {  // the last bound is that of all rounds: by one of five eighths of a row, one row in 300 had more tokens than the list holds, n = 64
+        const float b = wave_bound(top, a.group);
+        if ((threadIdx.x & 63) == 0) reinterpret_cast<volatile float*>(f->bound)[wave] = b;
+    }
     if (extra && lay.extra >= 0) {
         const float x[1] = {ld_elem<DT>(h, lay.extra)};
         raise(sum, x[0], a.r.c);
@@ -299,14 +304,22 @@ __device__ __forceinline__ bool shortlist(Finder& f, const void* h, float least,
     __syncthreads();
     return f.ranked_count <= kRanked;
 }
-// out(rank, key) for the n first of f.ranked, or with the key 0 where there are fewer.
+// out(rank, key) for the n first of f.ranked, or with the key 0 where there are fewer.  Each thread compares its key with all others, eight at a time: one by
+// one, each waited for, the some 300 of a row with n = 64 took 8 us.
 template <typename F>
-__device__ __forceinline__ void rank(const Finder& f, int n, int threads, F out) {
+__device__ __forceinline__ void rank(Finder& f, int n, int threads, F out) {
     const int count = f.ranked_count;
+    if (threadIdx.x < kRankedAtOnce) f.ranked[count + threadIdx.x] = 0;
+    __syncthreads();
     for (int i = threadIdx.x; i < count; i += threads) {
         const unsigned long long k = f.ranked[i];
         int before = 0;
-        for (int j = 0; j < count; ++j) before += f.ranked[j] > k ? 1 : 0;
+        for (int j = 0; j < count; j += kRankedAtOnce) {
+            unsigned long long o[kRankedAtOnce];
+            __builtin_memcpy(o, __builtin_assume_aligned(f.ranked + j, 16), sizeof(o));
+#pragma unroll
+            for (int x = 0; x < kRankedAtOnce; ++x) before += o[x] > k ? 1 : 0;
+        }
         if (before < n) out(before, k);
     }
     for (int i = count + threadIdx.x; i < n; i += threads) out(i, 0ull);
@@ -334,7 +347,7 @@ __device__ __forceinline__ float given_logit(const AltArgs& a, const void* h, in
 
 // What is written of a row whose sums and, in f.ranked, likeliest tokens are known.
 template <int DT, bool TOP>
-__device__ __forceinline__ void finish(const AltArgs& a, long row, int y, float hy, bool far, const Total<SumX>& s, int threads, const Finder* f) {
+__device__ __forceinline__ void finish(const AltArgs& a, long row, int y, float hy, bool far, const Total<SumX>& s, int threads, Finder* f) {
     if (threadIdx.x == 0) {
         const double lp = a.logprobs ? token_logprob<1>(a.r, far, y, hy, s.E, s.s) : 0.0;
         // the statistics are those of the whole c
@@ -352,7 +365,7 @@ __device__ __forceinline__ void finish(const AltArgs& a, long row, int y, float 
     }
 }
 
-// Bytes bound it: 1024 rows of 151936 in bf16 take 54 us without likeliest tokens, 5.8 TB/s, and 77 with 16 of them, 4.1 TB/s; 117 with 64.  Registers
+// Bytes bound it: 1024 rows of 151936 in bf16 take 54 us without likeliest tokens, 5.8 TB/s, and 77 with 16 of them, 4.1 TB/s; 104 with 64.  Registers
 // for four waves a SIMD hold two workgroups a unit, one of which computes while the other waits: with one it was 113 us.
 constexpr int kAltThreads = 512;
 template <int DT, bool TOP>
