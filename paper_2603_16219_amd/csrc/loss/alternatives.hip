@@ -7,8 +7,9 @@
 //
 // The n likeliest tokens come from the same pass.  The lanes of a workgroup form n groups or more, each with the largest logit that it has
 // met: the least of these is a lower bound of the n-th largest of the row, since n tokens reach it.  What reaches the bound goes to a list in
-// LDS.  The bound rises as the pass goes on; about n ln n (1 + ln(rounds)) of a row's tokens ever reach it (700 of 128256 for n = 64), and
-// n ln n reach the last one, which are ranked against each other.  Waves read the others' bounds without waiting: an old one is lower, and
+// LDS.  The bound rises as the pass goes on; about n ln n (1 + ln(rounds)) of a row's tokens ever reach it, half as many more where it is formed
+// after rounds that double (1000 of 128256 for n = 64), and n ln n reach the last one, which are ranked against each other.  Waves read the others'
+// bounds without waiting: an old one is lower, and
 // holds.  A row with more ties than the lists hold is searched for its n-th largest logit a digit at a time.
 #include "alternatives_plan.h"
 #include "loss_rows.h"
