@@ -147,11 +147,16 @@ __device__ __forceinline__ float block_bound(const Finder& f, int waves) {
     return v;
 }
 
-// The n likeliest of elements [begin, end) of a row into f.ranked, in no order, by a workgroup: the n-th largest logit a digit of 8 bits at a
+// The elements of a row that a search goes over, by increasing id: [begin, hole) and what lies `gap` behind it, `end` - `begin` in all.
+struct Span {
+    int begin, end, hole, gap;
+    __device__ __forceinline__ int id(int i) const { return i + (i < hole ? 0 : gap); }
+};
+// The n likeliest of a span into f.ranked, in no order, by a workgroup: the n-th largest logit a digit of 8 bits at a
 // time, then those above it and the first ones equal to it.  For rows with more ties than the lists hold (all logits the same, say): up to five
 // sweeps, a row of V = 128256 bf16 in about 0.1 ms.
 template <int DT>
-__device__ __forceinline__ void find_slowly(Finder& f, const void* h, int begin, int end, int n, int threads) {
+__device__ __forceinline__ void find_slowly(Finder& f, const void* h, Span span, int n, int threads) {
     int* const count = f.hits;
     const float lowest = -__builtin_huge_valf();
     unsigned prefix = 0, fixed = 0;  // digits of the n-th largest known so far
@@ -161,8 +166,8 @@ __device__ __forceinline__ void find_slowly(Finder& f, const void* h, int begin,
         __syncthreads();
         for (int i = threadIdx.x; i < 256; i += threads) count[i] = 0;
         __syncthreads();
-        for (int i = begin + threadIdx.x; i < end; i += threads) {
-            const float v = ld_elem<DT>(h, i);
+        for (int i = span.begin + (int)threadIdx.x; i < span.end; i += threads) {
+            const float v = ld_elem<DT>(h, span.id(i));
             const unsigned o = ordered(v);
             if (v > lowest && (o & fixed) == prefix) atomicAdd(&count[o >> shift & 255u], 1);
         }
@@ -188,9 +193,9 @@ __device__ __forceinline__ void find_slowly(Finder& f, const void* h, int begin,
     __syncthreads();
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = threads / kWave;
     int equal = 0;  // tokens equal to the n-th largest so far, the same in all lanes
-    for (int first = begin; first < end; first += threads) {
-        const int i = first + (int)threadIdx.x;
-        const float v = i < end ? ld_elem<DT>(h, i) : lowest;
+    for (int first = span.begin; first < span.end; first += threads) {
+        const int at = first + (int)threadIdx.x, i = span.id(at);
+        const float v = at < span.end ? ld_elem<DT>(h, i) : lowest;
         const unsigned o = ordered(v);
         const bool over = v > lowest && (all || o > prefix), same = !all && v > lowest && o == prefix;
         if (over) f.ranked[atomicAdd(&f.ranked_count, 1)] = key_of(v, i);
@@ -391,7 +396,7 @@ __global__ __launch_bounds__(kAltThreads) __attribute__((amdgpu_waves_per_eu(4))
     const bool far = a.r.far || is_far(s);
     if (far) s = far_sum_x<DT>(h, a.r.V, a.r.c64, kAltThreads, part);
     if (TOP) {
-        if (!shortlist<DT>(*f, h, block_bound(*f, kAltThreads / kWave), kAltThreads)) find_slowly<DT>(*f, h, 0, a.r.V, a.topk, kAltThreads);
+        if (!shortlist<DT>(*f, h, block_bound(*f, kAltThreads / kWave), kAltThreads)) find_slowly<DT>(*f, h, Span{0, a.r.V, a.r.V, 0}, a.topk, kAltThreads);
     }
     finish<DT, TOP>(a, row, y, hy, far, s, kAltThreads, f);
 }
@@ -417,10 +422,10 @@ __global__ __launch_bounds__(256) void alternatives_slice_kernel(const AltArgs a
     if (TOP) {
         unsigned long long* const keys = a.keys + (row * a.slices + slice) * a.topk;
         if (!shortlist<DT>(*f, h, block_bound(*f, kThreads / kWave), kThreads)) {
-            // the first slice has the elements before and behind the vectors too: it looks through all that no other has
+            // the first slice has the elements before and behind the vectors, as in the pass: whichever way the others go, each element is looked at once
             constexpr int kVec = Row<DT>::kVec;
-            const int lo = slice == 0 ? 0 : lay.head + begin * kVec, hi = lay.head + end * kVec;
-            find_slowly<DT>(*f, h, lo, slice + 1 == a.slices ? a.r.V : hi, a.topk, kThreads);
+            const int lo = lay.head + begin * kVec, hi = lay.head + end * kVec, tail = lay.head + lay.vecs * kVec;
+            find_slowly<DT>(*f, h, slice == 0 ? Span{0, hi + a.r.V - tail, hi, tail - hi} : Span{lo, hi, hi, 0}, a.topk, kThreads);
         }
         rank(*f, a.topk, kThreads, [&](int i, unsigned long long k) { keys[i] = k; });
     }
@@ -470,7 +475,7 @@ __global__ __launch_bounds__(256) void alternatives_join_kernel(const AltArgs a)
     Total<SumX> s = join(sums, a.slices);
     const bool far = a.r.far || is_far(s);
     if (far) s = far_sum_x<DT>(h, a.r.V, a.r.c64, kThreads, part);
-    if (TOP && f->ranked_count > kRanked) find_slowly<DT>(*f, h, 0, a.r.V, a.topk, kThreads);
+    if (TOP && f->ranked_count > kRanked) find_slowly<DT>(*f, h, Span{0, a.r.V, a.r.V, 0}, a.topk, kThreads);
     finish<DT, TOP>(a, row, y, hy, far, s, kThreads, f);
 }
 

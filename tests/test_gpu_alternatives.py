@@ -110,6 +110,26 @@ def test_orders_and_ties(losses, kind, rows, dtype):
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+@pytest.mark.parametrize("lead", [0, 1])
+@pytest.mark.parametrize("rows", [1, 5, 100])
+@pytest.mark.parametrize("tied", ["lowest", 1.25, 14.0])
+@pytest.mark.parametrize("part", ["first", "last", "middle"])
+def test_ties_in_one_part_of_a_row(losses, part, tied, rows, lead, dtype):
+    """Of rows in slices only one has more ties than its lists hold, and the elements outside of vectors are among the likeliest."""
+    V, vec, g = 50257, 8 if dtype is torch.bfloat16 else 4, gen(rows + lead)
+    each = -(-(V // vec) // min(64, -(-1024 // rows), V // vec // 512)) * vec  # elements of a slice
+    x = torch.full((1, rows, V + 7 + lead), math.nan, dtype=dtype, device="cuda")[:, :, lead:lead + V]
+    x.copy_(torch.randn(1, rows, V, generator=g, device="cuda") * 3)
+    at = {"first": 0, "middle": 3 * each, "last": V - 1 - each}[part]
+    x[:, :, at:at + each] = torch.finfo(dtype).min if tied == "lowest" else tied
+    x[:, :, [V - 1, V - 2, 1, 0]] = torch.tensor([16.0, 15.0, 15.5, 14.5], dtype=dtype, device="cuda")
+    y = torch.randint(0, V, (1, rows), generator=g, device="cuda", dtype=torch.int32)
+    y[0, 0] = V - 1
+    for topk in (1, 7, 64):
+        check(losses, x, y, topk=topk, grad=False)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
 @pytest.mark.parametrize("rows", [3, 120])
 @pytest.mark.parametrize("low", ["inf", "lowest"])
 def test_masked_tokens(losses, low, rows, dtype):
