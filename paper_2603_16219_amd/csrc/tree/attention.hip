@@ -297,7 +297,6 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
             // ask for that: the arithmetic once for all rows, whatever the pages' size.  The pages come from a piece of the table in LDS.
             constexpr int kMine = C::kLoads * C::kRows;
             const int first_row = wave * kMine, my_row = first_row + lane % kMine;
-            const int last = s.L > 0 ? (s.L - 1) / a.page_size : 0;
             const auto look_up = [&](int t) {
                 if (t >= items.cached || (b == table_of && t >= table_first && t < table_until)) return;
                 const int32_t* const pages = a.table + b * a.ts;
@@ -305,17 +304,17 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
                 if (b != table_of) table_bad = false;
                 table_of = b;
                 table_first = t;
-                table_from = (int)((long)t * C::kTile / a.page_size);
-                for (int i = tid; i < C::kTable && table_from + i <= last; i += C::kThreads) {
-                    int p = pages[table_from + i];
+                const TablePiece piece = table_piece(t, C::kTile, a.page_size, s.L, items.cached, C::kTable);
+                table_from = piece.from;
+                table_until = piece.until;
+                for (int i = tid; i < piece.entries; i += C::kThreads) {
+                    int p = pages[(long)table_from + i];
                     if (p < 0 || p >= a.pages) {
                         table_bad = true;
                         p = 0;
                     }
                     table[i] = p;
                 }
-                const long more = ((long)(table_from + C::kTable) * a.page_size - (long)t * C::kTile) / C::kTile;
-                table_until = more < items.cached ? t + (int)more : items.cached;
                 __syncthreads();
             };
             unsigned long of_row = 0;  // the address of this lane's row, of the keys of the tile that is asked for next or was last
@@ -323,7 +322,10 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
             const auto locate = [&](int t) {
                 if (t < items.cached) {
                     look_up(t);
-                    const unsigned pos = (unsigned)min(t * C::kTile + my_row, s.L - 1);  // past the end the last key again, which is masked
+                    // past the end the last key again, which is masked; the end of the last tile is a multiple of kTile up to 2^31, so that my_row < kTile
+                    // leaves the sum below it
+                    static_assert((1u << 31) % C::kTile == 0, "tiles end at 2^31");
+                    const unsigned pos = (unsigned)min(t * C::kTile + my_row, s.L - 1);
                     const unsigned col = a.page_of(pos), slot = pos - col * (unsigned)a.page_size;
                     of_row = (unsigned long)(unsigned)table[col - table_from] * a.page_step + ((unsigned long)slot * a.slot_step + first_key);
                 } else {

@@ -4,6 +4,7 @@
 // sequence, each of its threads 16 bytes at a time; every workgroup looks the whole path over first, since nothing is written of a bad one.  One path of
 // one sequence takes 5 us, a launch's least; 256 paths in trees of 24 nodes, 8 heads of 128 in bf16 (6.4 MB read and written) 6.8.
 #include "tree_common.h"
+#include "tree_schedule.h"
 
 namespace {
 
@@ -36,8 +37,9 @@ __global__ __launch_bounds__(kCommitThreads) void commit_kernel(const CommitArgs
                 const int r = a.path[(long)b * a.N + i];
                 bad = bad || r < 0 || r >= a.N;
             }
-        for (int i = L / a.page_size + tid; i <= (L + n) / a.page_size; i += kCommitThreads) {
-            const int p = a.table[b * a.ts + i];
+        const PageRange pages = pages_written(L, n, a.page_size);
+        for (int i = tid; i <= pages.more; i += kCommitThreads) {
+            const int p = a.table[b * a.ts + pages.first + i];
             bad = bad || p < 0 || p >= a.pages;
         }
         if (bad) wrong = 1;

@@ -51,6 +51,31 @@ inline PageOf page_of(int size) {
     while (1l << bits < size) ++bits;
     return PageOf{bits ? (unsigned)(((1ul << (31 + bits)) + (unsigned long)size - 1) / (unsigned long)size) : 0u, bits - 1};
 }
+// The piece of a sequence's row of the table that holds the pages of tile `t` and of as many tiles behind it as `most` entries do: entries
+// [from, from + entries), tiles before `until`.  t is below `cached`, whose last tile holds position length - 1.
+struct TablePiece {
+    int from, entries, until;
+};
+SS_TREE_BOTH TablePiece table_piece(int t, int tile, int page_size, int length, int cached, int most) {
+    TablePiece r;
+    const long first = (long)t * tile;
+    r.from = (int)(first / page_size);
+    const int left = (length - 1) / page_size - r.from;  // behind the first: no sum that may pass 32 bits where pages are of one position
+    r.entries = left < most ? left + 1 : most;
+    const long more = (((long)r.from + most) * page_size - first) / tile;
+    r.until = more < cached - t ? t + (int)more : cached;
+    return r;
+}
+// The pages that positions [length, length + rows] lie in: `more` behind the first.  length + rows is below 2^31.
+struct PageRange {
+    int first, more;
+};
+SS_TREE_BOTH PageRange pages_written(int length, int rows, int page_size) {
+    PageRange r;
+    r.first = length / page_size;
+    r.more = (length + rows) / page_size - r.first;
+    return r;
+}
 // The shares of all units: no share is empty.
 struct Shares {
     int each;   // units of a share,

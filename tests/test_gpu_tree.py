@@ -286,6 +286,35 @@ def test_offsets_past_32_bits(tree):
     check(tree, i)
 
 
+def test_positions_up_to_the_last_of_31_bits(tree):
+    """Shared pages of one position; the last 900 lie in pages of their own and weigh about a third of the row."""
+    L = 2**31 - 1
+    table = torch.zeros(1, L, dtype=torch.int32, device="cuda")
+    table[0, -900:] = 1
+    zeros = lambda *s: torch.zeros(*s, dtype=torch.bfloat16, device="cuda")
+    q, k, v, kc, vc = zeros(1, 1, 1, 64), zeros(1, 1, 1, 64), zeros(1, 1, 1, 64), zeros(5, 1, 1, 64), zeros(5, 1, 1, 64)
+    q[..., 0], kc[1, ..., 0] = 1, 14
+    v[:] = 3
+    vc[0], vc[1] = 3, -5
+    for length in (L, L - 130, L - 1000):
+        last = max(0, 900 - (L - length)) * math.exp(14)
+        rest = length - max(0, 900 - (L - length)) + 1
+        want = (3.0 * rest - 5.0 * last) / (rest + last)
+        got = tree.attention(q, k, v, kc, vc, table, torch.tensor([length], dtype=torch.int32, device="cuda"), scale=1.0).double()
+        # half a step for the weights of either value and for the output
+        assert (got - want).abs().max() <= 2.0 ** -8 * (3 + 5) + 2.0 ** -8 * abs(want), length
+    # the last three positions; the next one has no place
+    table[0, -3:] = torch.tensor([2, 3, 4], dtype=torch.int32, device="cuda")
+    rows = torch.arange(4.0, device="cuda").to(torch.bfloat16)[None, :, None, None].expand(1, 4, 1, 64).contiguous() + 1
+    at = lambda n: torch.tensor([n], dtype=torch.int32, device="cuda")
+    assert tree.commit(rows, -rows, kc, vc, table, at(L - 3), at(3)).tolist() == [-1]
+    assert torch.all(kc[2:] == 0)
+    assert tree.commit(rows, -rows, kc, vc, table, at(L - 3), at(2)).tolist() == [L]
+    assert kc[2:, 0, 0, 0].tolist() == [1, 2, 3] and vc[2:, 0, 0, 5].tolist() == [-1, -2, -3]
+    table[0, -1] = 5
+    assert tree.commit(rows, -rows, kc, vc, table, at(L - 3), at(2)).tolist() == [-1]
+
+
 def test_native_and_general_path_agree(tree, monkeypatch):
     i = make(2, 5, 8, 2, 64, [100, 37], 16, ragged=True)
     v = verify_inputs(3, 9, 1000, "f32")
