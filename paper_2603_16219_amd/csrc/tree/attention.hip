@@ -226,7 +226,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
     __shared__ unsigned short up[SS_MAX_K + 1];
     __shared__ int table[C::kTable];
     __shared__ int sh[C::kWaves + 2];
-    __shared__ int sh_bad;
+    __shared__ int sh_bad[2];  // of an item and the next one
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave % C::WM, wk = wave / C::WM;
     const TreeTiles tiles{C::kTile, C::kColumns, a.group, a.kv_heads};
@@ -265,6 +265,8 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
         cut->second = second;
     }
     bool first_item = true;
+    int turn_of = 0;
+    if (tid == 0) sh_bad[0] = 0;
     // the piece of the table that is in LDS: its sequence, the column that it begins with, the tiles whose pages it has
     int table_of = -1, table_from = 0, table_first = 0, table_until = 0;
     bool table_bad = false;  // of its sequence this thread has met a page that is none
@@ -291,7 +293,8 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
 #pragma unroll
         for (int i = 0; i < kBlocks; ++i) o[i] = f32x16{};
         __syncthreads();  // the last item's hand-over is done with
-        if (tid == 0) sh_bad = 0;
+        // Cleared a barrier before any wave may set it: where waves go on by themselves there is none between here and an item's end
+        if (tid == 0) sh_bad[turn_of ^ 1] = 0;
         if (!s.bad) {
             // The rows of a tile that this wave loads are kMine from first_row on.  A lane finds where one of them lies, and those that load its pieces
             // ask for that: the arithmetic once for all rows, whatever the pages' size.  The pages come from a piece of the table in LDS.
@@ -567,7 +570,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
             }
             l += __shfl_xor(l, 32, kWave);
         }
-        if (bad || (table_bad && table_of == b)) sh_bad = 1;
+        if (bad || (table_bad && table_of == b)) sh_bad[turn_of] = 1;
         // the waves' sums over their keys to those of the first
         __syncthreads();
         float* const hand = reinterpret_cast<float*>(lds);
@@ -607,7 +610,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
                         }
                 }
             }
-            if (sh_bad) l = __builtin_nanf("");
+            if (sh_bad[turn_of]) l = __builtin_nanf("");
             if (row < rows) {
                 if (whole) {
                     const float by = 1.f / l;
@@ -634,6 +637,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
             }
         }
         first_item = false;
+        turn_of ^= 1;
         rel += t1 - t0;
         u += t1 - t0;
     }

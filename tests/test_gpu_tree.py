@@ -248,6 +248,22 @@ def test_bad_data_marks_its_sequence_alone(tree, what):
         close(got[::2], want[::2], bound[::2], "the others")  # lengths say where all sequences' sums are cut
 
 
+@pytest.mark.parametrize("B,Hq,H", [(1, 32, 32), (7, 16, 8), (300, 4, 4)])
+def test_a_bad_page_marks_every_head(tree, B, Hq, H):
+    """Waves over their own keys, chains, heads whose pages are looked up once: the sequence's rows are NaN for each, and no other's are."""
+    i = make(B, 0, Hq, H, 64, [900 + 7 * b % 100 for b in range(B)], 64, kind="none")
+    want = run(tree, i)
+    assert not want.isnan().any()
+    for b in sorted({0, B // 2, B - 1}):
+        for at in (0, 3, 14):
+            table = i["table"].clone()
+            table[b, at] = i["k_cache"].shape[0]
+            got = run(tree, dict(i, table=table))
+            assert got[b].isnan().all()
+            others = torch.arange(B, device="cuda") != b
+            assert torch.equal(got[others], want[others])
+
+
 def test_pages_and_parents_that_are_not_needed_may_be_anything(tree):
     i = make(2, 8, 4, 2, 64, [33, 16], 16, ragged=True)
     want = run(tree, i)
