@@ -125,15 +125,26 @@ __device__ __forceinline__ void pick_rows(const VerifyArgs& a, int N, int cur, i
     __syncthreads();
 }
 
+// What is taken from the difference of a node's logits in its test: `ref`, in logits, before its product with c, and d_r less that behind it.  Of rows far
+// from zero ref is the difference of the largest logits, both of which may be beyond what h c has bits for; of others it is 0.
+struct RowDiff {
+    double ref, diff;
+};
+// The row far from zero, or one of whose tensors' is, by the whole workgroup.
 template <int DT>
-__device__ __forceinline__ double log2_sum(const VerifyArgs& a, int b, int r, int x, Total<Sum> s, WalkShared& w) {
-    const bool far = a.far || is_far(s);
-    if (far) {
+__device__ __forceinline__ RowDiff far_diff(const VerifyArgs& a, int b, int r, Total<Sum>* part) {
+    Total<Sum> s[2];
+    for (int x = 0; x < 2; ++x) {
         const void* const h = row_ptr<DT>(x ? a.Sm : a.G, b * a.sb + r * a.st);
         __syncthreads();
-        s = far_sum<DT, Sum>(h, nullptr, a.V, a.c64, kVerifyGroup, w.part);
+        s[x] = far_sum<DT, Sum>(h, nullptr, a.V, a.c64, kVerifyGroup, part);
     }
-    return (far ? (double)s.E * a.c64 : (double)s.E) + log2(s.s);
+    return RowDiff{(double)s[0].E - (double)s[1].E, log2(s[0].s) - log2(s[1].s)};
+}
+// Whether a node with logits h of G and S_noctx is accepted: masked by G never, by S_noctx alone always
+__device__ __forceinline__ bool accepts(const VerifyArgs& a, float2 h, double u, RowDiff d) {
+    const double alpha = h.x == -__builtin_huge_valf() ? -1.0 : exp2((((double)h.x - (double)h.y) - d.ref) * a.c64 - d.diff) / a.lambda;
+    return u <= 1.0 && !(u > alpha);
 }
 
 // On from w.at over the rows of w.rows, whose sums are there.
@@ -157,10 +168,16 @@ __device__ __forceinline__ void walk(const VerifyArgs& a, int b, int N, bool lea
             w.first[w.rows[k >> 1]] = kNever;
         }
     }
+    const auto test = [&](int i, int r, RowDiff d) {
+        const float2 h = a.logits[(long)b * a.N + i];
+        const double u = a.uniforms[(long)b * (a.N + 1) + i];
+        if (accepts(a, h, u, d)) atomicMin(&w.first[r], i);
+    };
+    constexpr double kTested = __builtin_huge_val();
     if (__syncthreads_or(far))
-        for (int k = 0; k < n; ++k) {  // rows far from zero, by the whole workgroup
+        for (int k = 0; k < n; ++k) {
             const int r = w.rows[k];
-            double lse[2];
+            bool of_row = a.far;
             for (int x = 0; x < 2; ++x) {
                 Total<Sum> s;
                 clear_total(s);
@@ -170,19 +187,18 @@ __device__ __forceinline__ void walk(const VerifyArgs& a, int b, int N, bool lea
                     s.s = moved(s.s, s.E, E) + moved(o.s, o.E, E);
                     s.E = E;
                 }
-                lse[x] = log2_sum<DT>(a, b, r, x, s, w);
+                of_row = of_row || is_far(s);
             }
-            if (tid == 0) w.diff[r] = lse[0] - lse[1];
+            if (!of_row) continue;
+            const RowDiff d = far_diff<DT>(a, b, r, w.part);
+            for (int i = r + tid; i < N; i += kVerifyGroup)  // children lie behind their parent
+                if (w.parent[i] == r - 1) test(i, r, d);
+            if (tid == 0) w.diff[r] = kTested;
         }
     __syncthreads();
     for (int i = tid; i < N; i += kVerifyGroup) {
         const int r = w.parent[i] + 1;
-        if (w.first[r] < 0) continue;
-        const float2 h = a.logits[(long)b * a.N + i];
-        const double u = a.uniforms[(long)b * (a.N + 1) + i];
-        // masked by G: never accepted; by S_noctx alone: always
-        const double alpha = h.x == -__builtin_huge_valf() ? -1.0 : exp2(((double)h.x - (double)h.y) * a.c64 - w.diff[r]) / a.lambda;
-        if (u <= 1.0 && !(u > alpha)) atomicMin(&w.first[r], i);
+        if (w.first[r] >= 0 && w.diff[r] != kTested) test(i, r, RowDiff{0.0, w.diff[r]});
     }
     __syncthreads();
     if (tid == 0) {
@@ -239,7 +255,7 @@ __device__ __forceinline__ int reach(const VerifyArgs& a, int b, int stage, int 
 // took 12 to 28 us and the draw 27.
 constexpr int kSmall = 63;
 struct SmallShared {
-    double diff[kSmall + 1];
+    double diff[kSmall + 1], ref[kSmall + 1];
     unsigned long long far[kVerifyGroup / kWave], inner, set, rows;
     signed char parent[kSmall + 1];
     Total<Sum> part[kVerifyGroup / kWave];
@@ -304,7 +320,10 @@ __device__ __forceinline__ int reach(const VerifyArgs& a, int b, int stage, int 
             far = far || a.far || is_far(t);
             lse[x] = (double)t.E + log2(t.s);
         }
-        if (l == 0) w.diff[r] = lse[0] - lse[1];
+        if (l == 0) {
+            w.diff[r] = lse[0] - lse[1];
+            w.ref[r] = 0.0;
+        }
         unsigned long long mask = 0;
         const unsigned long long ballot = __ballot(far && l == 0 && r <= a.N);
         for (int k = 0; k < kWave / kLanes; ++k) mask |= (ballot >> (kLanes * k) & 1) << (wave * (kWave / kLanes) + k);
@@ -334,14 +353,11 @@ __device__ __forceinline__ int reach(const VerifyArgs& a, int b, int stage, int 
         if (far) {  // rows far from zero, by the whole workgroup
             for (unsigned long long m = far; m; m &= m - 1) {
                 const int fr = first_lane(m);
-                double lse[2];
-                for (int x = 0; x < 2; ++x) {
-                    const void* const row = row_ptr<DT>(x ? a.Sm : a.G, b * a.sb + fr * a.st);
-                    __syncthreads();
-                    const Total<Sum> t = far_sum<DT, Sum>(row, nullptr, a.V, a.c64, kVerifyGroup, w.part);
-                    lse[x] = (double)t.E * a.c64 + log2(t.s);
+                const RowDiff d = far_diff<DT>(a, b, fr, w.part);
+                if (tid == 0) {
+                    w.diff[fr] = d.diff;
+                    w.ref[fr] = d.ref;
                 }
-                if (tid == 0) w.diff[fr] = lse[0] - lse[1];
             }
             __syncthreads();
         }
@@ -349,11 +365,7 @@ __device__ __forceinline__ int reach(const VerifyArgs& a, int b, int stage, int 
     if (wave == 0) {
         if (stage > 0 && !c.done) {
             bool accept = false;
-            if (parent >= -1 && (set >> (parent + 1) & 1)) {
-                // masked by G: never accepted; by S_noctx alone: always
-                const double alpha = h.x == -__builtin_huge_valf() ? -1.0 : exp2(((double)h.x - (double)h.y) * a.c64 - w.diff[parent + 1]) / a.lambda;
-                accept = u <= 1.0 && !(u > alpha);
-            }
+            if (parent >= -1 && (set >> (parent + 1) & 1)) accept = accepts(a, h, u, RowDiff{w.ref[parent + 1], w.diff[parent + 1]});
             for (;;) {
                 const int row = c.cur + 1;
                 if (!(inner >> row & 1)) c.done = 1;
