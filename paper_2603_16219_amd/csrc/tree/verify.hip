@@ -24,8 +24,9 @@ struct Cursor {
     int cur, n, done, pad;  // done: 1 at the walk's end, 2 of a sequence that is marked
 };
 struct Mass {
-    float E, s;
+    float E, s;  // s 2^E; with kByLogit for E relative to a logit that stands in `tops`
 };
+constexpr float kByLogit = __builtin_huge_valf();
 struct Best {
     double h;
     int id, pad;
@@ -42,13 +43,16 @@ struct VerifyArgs {
     Total<Sum>* sums;     // [B][N + 1][2][slices]
     float2* logits;       // [B][N]: of the nodes' tokens at their rows
     Mass* masses;         // [B][chunks]
+    double* tops;         // [B][chunks]
     Best* best;           // [B][parts]
     long sb, st;
     int B, N, V;
     Factor c;
     double c64, inv_tau, lambda, beta;
     float steer_hi, steer_lo;  // beta c in two parts
+    float steer_size, steer_most;  // |beta c|, and the difference whose product with it is kFar
     int far, greedy, plain;    // plain: beta is 0
+    int by_logit;              // all masses are
     int slices, slice_vecs, chunks, parts, part_chunks;
 };
 
@@ -488,13 +492,21 @@ struct RecoveryRow {
     const void *g, *sp, *sm;
 };
 // Eq. 8's exponent less E, in fp32: g c first, whose upper part is exact for bf16 (loss_rows.h), so that what is rounded is of the difference's size.
-// In double the masses of 64 rows of V = 128256 took 14 us, most of it arithmetic.
+// In double the masses of 64 rows of V = 128256 took 14 us, most of it arithmetic.  A term near E is off by up to 3 half steps of its steering term's
+// size, 2^-24 of it each: the sum's share of that, sum p |d beta c| / sum p, is formed beside the sum, and a chunk where it passes kSteerMean, or whose
+// exponents are far from zero, is summed again in double, by its logits' differences to their largest, which hold at any temperature.
 __device__ __forceinline__ float rec_exponent(const VerifyArgs& a, float g, float d, float E) {
     const float t = exponent<2>(g, E, a.c);
     return a.plain ? t : fmaf(d, a.steer_lo, fmaf(d, a.steer_hi, t));
 }
+constexpr double kSteerMean = 16.0;
 // and in double, for the token drawn
-__device__ __forceinline__ double rec_exponent64(const VerifyArgs& a, double g, double d) { return fma(g, a.c64, d * (a.beta * a.c64)); }
+__device__ __forceinline__ double rec_exponent64(const VerifyArgs& a, float g, float sp, float sm) { return fma((double)g, a.c64, a.plain ? 0.0 : steer(sp, sm) * (a.beta * a.c64)); }
+// Eq. 8's logit, the operations in this order
+__device__ __forceinline__ double rec_logit(const VerifyArgs& a, float g, float sp, float sm) {
+    return a.plain ? (double)g : __dadd_rn((double)g, __dmul_rn(a.beta, steer(sp, sm)));
+}
+__device__ __forceinline__ float logit_term(double h, double top, double c) { return exp2_hw((float)((h - top) * c)); }
 
 // A step of chunk `c` of a row by a wave: each lane's logits of G, -inf where there are none, and the steering term's differences; returns the
 // first one's id.  The last chunk has the elements behind the last vector, one a lane.
@@ -563,6 +575,8 @@ constexpr int kMassSteps = kMassVecs / kWave;
 __device__ __forceinline__ void put(unsigned long long* p, unsigned long long v) { __hip_atomic_store(p, v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ unsigned long long get(const unsigned long long* p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 __device__ __forceinline__ void put(Mass* p, Mass m) { put(reinterpret_cast<unsigned long long*>(p), __builtin_bit_cast(unsigned long long, m)); }
+__device__ __forceinline__ void put(double* p, double v) { put(reinterpret_cast<unsigned long long*>(p), __builtin_bit_cast(unsigned long long, v)); }
+__device__ __forceinline__ double get(const double* p) { return __builtin_bit_cast(double, get(reinterpret_cast<const unsigned long long*>(p))); }
 __device__ __forceinline__ Mass get(const Mass* p) { return __builtin_bit_cast(Mass, get(reinterpret_cast<const unsigned long long*>(p))); }
 __device__ __forceinline__ void put(Best* p, Best v) {
     unsigned long long* const q = reinterpret_cast<unsigned long long*>(p);
@@ -577,6 +591,88 @@ __device__ __forceinline__ void delivered() {
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_waitcnt(0);
     asm volatile("" ::: "memory");
+}
+
+// Chunks by their logits: seldom, so that each step is loaded again where it is needed and no registers are held for it.
+template <int DT>
+__device__ __forceinline__ void chunk_logits(const VerifyArgs& a, const Chunk<DT>& k, double (&h)[Row<DT>::kVec]) {
+    constexpr int kVec = Row<DT>::kVec;
+    float g[kVec], sp[kVec], sm[kVec];
+    unpack(k.g, g);
+    unpack(k.sp, sp);
+    unpack(k.sm, sm);
+#pragma unroll
+    for (int i = 0; i < kVec; ++i) h[i] = rec_logit(a, g[i], sp[i], sm[i]);
+}
+// A chunk's largest logit of Eq. 8, -inf of masked tokens alone, and the sum of its terms relative to that, by a wave.
+template <int DT>
+__device__ __forceinline__ double chunk_by_logit(const VerifyArgs& a, const RecoveryRow<DT>& row, int c, double& sum) {
+    constexpr int kVec = Row<DT>::kVec;
+    double top = -__builtin_huge_val(), h[kVec];
+#pragma unroll 1
+    for (int s = 0; s < kMassSteps; ++s) {
+        chunk_logits<DT>(a, load_chunk<DT>(a, row, c, s), h);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) top = fmax(top, h[i]);
+    }
+    for (int d = 1; d < kWave; d <<= 1) top = fmax(top, __shfl_xor(top, d, kWave));
+    sum = 0.0;
+    if (!(top > -__builtin_huge_val())) return top;
+#pragma unroll 1
+    for (int s = 0; s < kMassSteps; ++s) {
+        chunk_logits<DT>(a, load_chunk<DT>(a, row, c, s), h);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) sum += (double)logit_term(h[i], top, a.c64);
+    }
+    sum = wave_sum_f64(sum);
+    return top;
+}
+// The token of such a chunk, by a wave: the first that brings the sum from `cum` on past the target, or the last one with any mass; and its logit.
+template <int DT>
+__device__ __forceinline__ int token_by_logit(const VerifyArgs& a, const RecoveryRow<DT>& row, int c, double top, double scale, double cum, double target, bool last,
+                                              double& logit) {
+    constexpr int kVec = Row<DT>::kVec;
+    int token = -1;
+    logit = top;
+#pragma unroll 1
+    for (int s = 0; s < kMassSteps; ++s) {
+        const Chunk<DT> k = load_chunk<DT>(a, row, c, s);
+        double h[kVec], own = 0.0, mine = 0.0, tail = 0.0;
+        float e[kVec];
+        int hit = -1, end = -1;
+        chunk_logits<DT>(a, k, h);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+            e[i] = logit_term(h[i], top, a.c64);
+            own += (double)e[i];
+        }
+        const double incl = wave_incl_scan_f64(own * scale);
+        double at = cum + wave_shift_up_f64(incl);
+#pragma unroll
+        for (int i = 0; i < kVec; ++i) {
+            at += (double)e[i] * scale;
+            if (e[i] > 0.f) {
+                end = k.id + i;
+                tail = h[i];
+                if (!last && hit < 0 && at > target) {
+                    hit = k.id + i;
+                    mine = h[i];
+                }
+            }
+        }
+        const unsigned long long hits = __ballot(hit >= 0), ends = __ballot(end >= 0);
+        if (hits) {
+            logit = __shfl(mine, first_lane(hits), kWave);
+            return __shfl(hit, first_lane(hits), kWave);
+        }
+        if (ends) {
+            const int L = 63 - __clzll((long long)ends);
+            token = __shfl(end, L, kWave);
+            logit = __shfl(tail, L, kWave);
+        }
+        cum += wave_last_f64(incl);
+    }
+    return token;
 }
 
 template <int DT, typename W>
@@ -605,26 +701,30 @@ __global__ __launch_bounds__(kVerifyGroup) void draw_kernel(const VerifyArgs a, 
     const long off = b * a.sb + (at.cur + 1) * a.st;
     const RecoveryRow<DT> row{row_ptr<DT>(a.G, off), row_ptr<DT>(a.Sp, off), row_ptr<DT>(a.Sm, off)};
     Mass* const masses = a.masses + (long)b * a.chunks;
+    double* const tops = a.tops + (long)b * a.chunks;
     Best top{-__builtin_huge_val(), kNever, 0};
     const int c1 = min(a.chunks, (part + 1) * a.part_chunks);
     for (int c = part * a.part_chunks + wave; c < c1; c += kWaves) {
         Chunk<DT> k[kMassSteps];
 #pragma unroll
         for (int s = 0; s < kMassSteps; ++s) k[s] = load_chunk<DT>(a, row, c, s);
-        float most = -__builtin_huge_valf();
+        float most = -__builtin_huge_valf(), apart = 0.f;
 #pragma unroll
         for (int s = 0; s < kMassSteps; ++s) {
             float g[kVec], d[kVec];
             unpack_chunk<DT>(k[s], g, d);
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) most = fmaxf(most, rec_exponent(a, g[i], d[i], 0.f));
+            for (int i = 0; i < kVec; ++i) {
+                most = fmaxf(most, rec_exponent(a, g[i], d[i], 0.f));
+                apart = fmaxf(apart, fabsf(d[i]));
+            }
             if (a.greedy) {
                 float sp[kVec], sm[kVec];
                 unpack(k[s].sp, sp);
                 unpack(k[s].sm, sm);
 #pragma unroll
                 for (int i = 0; i < kVec; ++i) {
-                    const double h = a.plain ? (double)g[i] : __dadd_rn((double)g[i], __dmul_rn(a.beta, steer(sp[i], sm[i])));
+                    const double h = rec_logit(a, g[i], sp[i], sm[i]);
                     if (h > top.h) top = Best{h, k[s].id + i, 0};
                 }
             }
@@ -632,17 +732,42 @@ __global__ __launch_bounds__(kVerifyGroup) void draw_kernel(const VerifyArgs a, 
         for (int d = 1; d < kWave; d <<= 1) most = fmaxf(most, __shfl_xor(most, d, kWave));
         // a reference near the largest exponent; a chunk of masked tokens has any
         const float E = fmaxf(fminf(ceilf(most), 3e38f), -3e38f);
-        float s = 0.f;
+        float s = 0.f, steered = 0.f;
 #pragma unroll
         for (int u = 0; u < kMassSteps; ++u) {
             float g[kVec], d[kVec], e[kVec];
             unpack_chunk<DT>(k[u], g, d);
 #pragma unroll
-            for (int i = 0; i < kVec; ++i) e[i] = exp2_hw(rec_exponent(a, g[i], d[i], E));
+            for (int i = 0; i < kVec; ++i) {
+                e[i] = exp2_hw(rec_exponent(a, g[i], d[i], E));
+                steered = fmaf(e[i], fabsf(d[i]), steered);
+            }
             s += tree_sum(e);
         }
-        const double all = wave_sum_f64((double)s);
-        if (lane == 0) put(masses + c, Mass{E, (float)all});
+        const double all = wave_sum_f64((double)s), share = (double)wave_sum_f32(steered) * (double)a.steer_size;
+        // the largest term is at least a half and no sum infinite, or the exponents are not what they are taken for
+        const bool holds = !a.by_logit && fabsf(E) <= kFar && all >= 0.25 && all < 1e6 && share <= kSteerMean * all && !__ballot(!(apart <= a.steer_most));
+        Mass m{E, (float)all};
+        bool none = false;
+        if (__builtin_expect(!holds && most == -__builtin_huge_valf(), 0)) {  // masked tokens alone, or none, as behind the last vector; or logits beyond what fp32 holds
+            float g_most = most;
+#pragma unroll
+            for (int u = 0; u < kMassSteps; ++u) {
+                float g[kVec];
+                unpack(k[u].g, g);
+                g_most = fmaxf(g_most, largest(g));
+            }
+            none = !__ballot(g_most > most);
+        }
+        if (none) {
+            m = Mass{0.f, 0.f};
+        } else if (__builtin_expect(!holds, 0)) {
+            double sum;
+            const double h = chunk_by_logit<DT>(a, row, c, sum);
+            m = h > -__builtin_huge_val() ? Mass{kByLogit, (float)sum} : Mass{0.f, 0.f};
+            if (lane == 0) put(tops + c, h);
+        }
+        if (lane == 0) put(masses + c, m);
     }
     if (a.greedy) {
         for (int d = 1; d < kWave; d <<= 1) {
@@ -678,7 +803,25 @@ __global__ __launch_bounds__(kVerifyGroup) void draw_kernel(const VerifyArgs a, 
     if (lane == 0) sum[wave] = (double)E;
     __syncthreads();
     for (int v = 0; v < kWaves; ++v) E = fmaxf(E, (float)sum[v]);
-    const auto mass = [&](Mass m) { return m.s > 0.f ? moved((double)m.s, m.E, E) : 0.0; };
+    // Of a row some of whose chunks are relative to logits all of them are moved to the largest logit, in double.
+    const bool by_logit = E == kByLogit;
+    double high = -__builtin_huge_val();
+    const auto logit_of = [&](Mass m, int c) { return m.E == kByLogit ? get(tops + c) : (double)m.E / a.c64; };
+    if (__builtin_expect(by_logit, 0)) {
+        for (int c = tid; c < a.chunks; c += kVerifyGroup)
+            if (table[c].s > 0.f) high = fmax(high, logit_of(table[c], c));
+        for (int d = 1; d < kWave; d <<= 1) high = fmax(high, __shfl_xor(high, d, kWave));
+        __syncthreads();
+        if (lane == 0) sum[wave] = high;
+        __syncthreads();
+        for (int v = 0; v < kWaves; ++v) high = fmax(high, sum[v]);
+        for (int c = tid; c < a.chunks; c += kVerifyGroup) {
+            const Mass m = table[c];
+            table[c] = __builtin_bit_cast(Mass, m.s > 0.f ? (double)m.s * exp2((logit_of(m, c) - high) * a.c64) : 0.0);
+        }
+        __syncthreads();
+    }
+    const auto mass = [&](Mass m) { return by_logit ? __builtin_bit_cast(double, m) : m.s > 0.f ? moved((double)m.s, m.E, E) : 0.0; };
     // a lane's chunks lie next to each other, so that the lanes' sums are in order
     const int each = (a.chunks + kVerifyGroup - 1) / kVerifyGroup, lo = min(a.chunks, tid * each), hi = min(a.chunks, lo + each);
     double mine = 0.0;
@@ -693,7 +836,7 @@ __global__ __launch_bounds__(kVerifyGroup) void draw_kernel(const VerifyArgs a, 
         if (v < wave) before += sum[v];
         Z += sum[v];
     }
-    const double log2Z = (double)E + log2(Z);
+    const double log2Z = (by_logit ? 0.0 : (double)E) + log2(Z);  // relative to `high`, or whole
     if (a.greedy) {
         if (tid == 0) {
             Best t = get(a.best + (long)b * a.parts);
@@ -702,7 +845,7 @@ __global__ __launch_bounds__(kVerifyGroup) void draw_kernel(const VerifyArgs a, 
                 if (o.h > t.h || (o.h == t.h && o.id < t.id)) t = o;
             }
             a.next_token[b] = min(t.id, a.V - 1);
-            if (a.next_logprob) a.next_logprob[b] = (float)((t.h * a.c64 - log2Z) * kLn2);
+            if (a.next_logprob) a.next_logprob[b] = (float)(((by_logit ? t.h - high : t.h) * a.c64 - log2Z) * kLn2);
         }
         return;
     }
@@ -746,8 +889,18 @@ __global__ __launch_bounds__(kVerifyGroup) void draw_kernel(const VerifyArgs a, 
     if (take_last) chunk = last_chunk;
     if (wave != 0) return;
     // wave 0 goes over the chunk again, in the order of its tokens
-    const float cE = table[chunk].E;
-    const double scale = moved(1.0, cE, E);
+    const Mass of_chunk = by_logit ? get(masses + chunk) : table[chunk];
+    const float cE = of_chunk.E;
+    const double c_top = by_logit ? logit_of(of_chunk, chunk) : 0.0, scale = by_logit ? exp2((c_top - high) * a.c64) : moved(1.0, cE, E);
+    if (__builtin_expect(cE == kByLogit, 0)) {
+        double h;
+        const int token = token_by_logit<DT>(a, row, chunk, c_top, scale, start, target, take_last, h);
+        if (lane == 0) {
+            a.next_token[b] = min(max(token, 0), a.V - 1);
+            if (a.next_logprob) a.next_logprob[b] = (float)(((h - high) * a.c64 - log2Z) * kLn2);
+        }
+        return;
+    }
     Chunk<DT> k[kMassSteps];
 #pragma unroll
     for (int s = 0; s < kMassSteps; ++s) k[s] = load_chunk<DT>(a, row, chunk, s);
@@ -786,9 +939,11 @@ __global__ __launch_bounds__(kVerifyGroup) void draw_kernel(const VerifyArgs a, 
                 incl = s == v ? in[v] : incl;
             }
         cum += wave_shift_up_f64(incl);
-        float g[kVec], d[kVec], g_hit = 0.f, d_hit = 0.f;
+        float g[kVec], d[kVec], sp[kVec], sm[kVec], g_hit = 0.f, sp_hit = 0.f, sm_hit = 0.f;
         int hit = -1;
         unpack_chunk<DT>(now, g, d);
+        unpack(now.sp, sp);
+        unpack(now.sm, sm);
 #pragma unroll
         for (int i = 0; i < kVec; ++i) {
             const float e = exp2_hw(rec_exponent(a, g[i], d[i], cE));
@@ -796,14 +951,15 @@ __global__ __launch_bounds__(kVerifyGroup) void draw_kernel(const VerifyArgs a, 
             if (e > 0.f && (last || (hit < 0 && cum > target))) {
                 hit = now.id + i;
                 g_hit = g[i];
-                d_hit = d[i];
+                sp_hit = sp[i];
+                sm_hit = sm[i];
             }
         }
         const unsigned long long hits = __ballot(hit >= 0);
         if (!hits) return;
         const int L = last ? 63 - __clzll((long long)hits) : first_lane(hits);
         token = __shfl(hit, L, kWave);
-        y_token = rec_exponent64(a, (double)__shfl(g_hit, L, kWave), (double)__shfl(d_hit, L, kWave));
+        y_token = __shfl(by_logit ? (rec_logit(a, g_hit, sp_hit, sm_hit) - high) * a.c64 : rec_exponent64(a, g_hit, sp_hit, sm_hit), L, kWave);
     };
     for (int s = first; s < kMassSteps && token < 0; ++s) look(s, false);
     for (int s = kMassSteps - 1; s >= 0 && token < 0; --s) look(s, true);
@@ -861,6 +1017,7 @@ ss_status specsteer_tree_verify(const void* G, const void* S_ctx, const void* S_
     a.sums = reinterpret_cast<Total<Sum>*>(ws + p.off_sums);
     a.logits = reinterpret_cast<float2*>(ws + p.off_logits);
     a.masses = reinterpret_cast<Mass*>(ws + p.off_masses);
+    a.tops = reinterpret_cast<double*>(ws + p.off_masses) + (long)params->batch * p.chunks;
     a.best = reinterpret_cast<Best*>(ws + p.off_best);
     a.sb = sb;
     a.st = st;
@@ -874,7 +1031,12 @@ ss_status specsteer_tree_verify(const void* G, const void* S_ctx, const void* S_
     a.beta = (double)params->beta;
     a.steer_hi = (float)(a.beta * a.c64);
     a.steer_lo = (float)(a.beta * a.c64 - (double)a.steer_hi);
+    const double steer_size = std::fabs(a.beta * a.c64);
+    a.steer_size = (float)steer_size;
+    a.steer_most = params->beta == 0.f ? __builtin_huge_valf() : (float)std::fmin((double)kFar / steer_size, 3e38);
     a.far = r.far;
+    // factors that fp32 does not hold
+    a.by_logit = r.far || (params->beta != 0.f && !(steer_size > 1e-30 && steer_size < 1e30));
     a.greedy = (params->flags & SS_FLAG_GREEDY) ? 1 : 0;
     a.plain = params->beta == 0.f ? 1 : 0;
     a.slices = p.slices;

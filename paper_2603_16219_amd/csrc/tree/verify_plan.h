@@ -77,7 +77,7 @@ inline VerifyPlan verify_plan(const ss_params& p, int units) {
     r.off_logits = at;
     at += up((size_t)B * N * 8);
     r.off_masses = at;
-    at += up((size_t)B * r.chunks * 8);
+    at += up((size_t)B * r.chunks * 16);  // and the logits that some of them are relative to
     r.off_best = at;
     at += up((size_t)B * r.parts * 16);
     r.bytes = at + 256;

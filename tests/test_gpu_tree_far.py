@@ -1,5 +1,9 @@
 """GPU tests of the walk down a tree where exponents h / T are large or far apart: low and high temperatures, rows far from zero, steering terms that
-cancel, the type's lowest value.  Against the definitions in 64 bits, from differences of logits, which are exact there."""
+cancel, the type's lowest value.  Against the definitions in 64 bits, from differences of logits, which are exact there.
+
+u = 2^-24, z a term's distance to the row's largest in powers of two.  A term formed in double is off by 1.4 z u (its exponent as one fp32 number) and 2 u; one
+formed in fp32 by up to 3 u ln 2 times its steering term in powers of two, whose mean is at most 16 there.  Cumulated probabilities are off by
+(2.1 E[z] + 2 + 34) u, 2.8e-6 for E[z] = 5, a log-prob by as much and half a step of its own."""
 import math
 
 import pytest
@@ -10,6 +14,7 @@ from test_gpu_losses import gen
 from test_gpu_tree import DTYPES, tree, verify_inputs, walk  # noqa: F401
 
 pytestmark = pytest.mark.gpu
+TOL = 4e-6
 
 
 def reference(i, lam, beta, temperature, greedy):
@@ -62,8 +67,14 @@ def check(tree, i, lam=0.5, beta=0.5, temperature=1.0, greedy=False):
     want = reference(i, lam, beta, temperature, greedy)
     sure = torch.tensor([n > 1e-6 for n in want["near"]])
     assert sure.float().mean() >= 0.7
-    for k in ("accepted_len", "path"):
+    for k in ("accepted_len", "path") + (("next_token",) if greedy else ()):
         assert torch.equal(got[k].cpu()[sure], torch.tensor(want[k], dtype=torch.int32).view(got[k].shape)[sure]), k
+    tokens, lps = got["next_token"].tolist(), got["next_token_logprob"].tolist()
+    for b in sure.nonzero()[:, 0].tolist():
+        lp, cdf, u = want["rows"][b]
+        t = tokens[b]
+        assert greedy or (cdf[t] > u - TOL and (t == 0 or cdf[t - 1] <= u + TOL) and lp[t].exp() > 0), (b, t, want["next_token"][b])
+        assert abs(lps[b] - float(lp[t])) <= TOL + abs(float(lp[t])) * 2.0 ** -24, (b, t, lps[b], float(lp[t]))
     return want
 
 
@@ -124,3 +135,32 @@ def test_the_type_s_lowest_value(tree, low, N, V, dtype):
                 i[t][:, :, dead] = v
         for greedy in (False, True):
             check(tree, i, greedy=greedy)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("V", [3001, 40003])
+def test_large_steering_terms_in_a_few_places(tree, V, dtype):
+    """One token alone, in its own chunk of the row, has a steering term that cancels its logit; others are ordinary."""
+    for seed, size in ((0, 40.0), (1, 3e3), (2, 2e5), (3, 1e9), (4, 1e12)):
+        i = verify_inputs(6, 0, V, dtype, seed)
+        at = torch.randint(0, V, (6,), generator=gen(seed), device="cuda")
+        b = torch.arange(6, device="cuda")
+        i["G"][b, 0, at] = -size
+        i["Sp"][b, 0, at] = 2 * size  # in bf16 with what its 8 bits leave out of the cancelling
+        i["Sm"][b, 0, at] = 0.0
+        for beta in (0.5, 0.25):
+            check(tree, i, beta=beta)
+            check(tree, i, beta=beta, greedy=True)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("temperature", [0.05, 0.01, 1e-3])
+def test_a_chain_is_the_block_at_low_temperatures(tree, temperature, dtype):
+    from paper_2603_16219_amd import binding
+
+    for B, K, V, beta in ((1, 4, 32000, 0.7), (9, 16, 5003, -0.7), (70, 8, 2000, 0.0), (4, 0, 1000, 1.0)):
+        i = likely_drafts(verify_inputs(B, K, V, dtype, 4, "none"), gen(1), 0.9)
+        a = binding.verify_block(i["G"], i["Sp"], i["Sm"], i["tokens"], i["uniforms"], lam=0.3, beta=beta, temperature=temperature)
+        got = walk(tree, i, lam=0.3, beta=beta, temperature=temperature)
+        assert torch.equal(got["accepted_len"], a["accepted_len"]) and torch.equal(got["next_token"], a["next_token"])
+        torch.testing.assert_close(got["next_token_logprob"], a["next_token_logprob"], rtol=2.0 ** -23, atol=1e-5)
