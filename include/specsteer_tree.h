@@ -16,6 +16,8 @@
  * nothing is allocated, owned or waited for, argument errors return before anything is enqueued and leave every output
  * untouched.  All calls may be captured into a graph.  Sums are formed in a fixed order: the same call gives the same bits.
  * Data errors that only the GPU can see mark their sequence alone, as each call says; no out-of-range address is formed.
+ * No output shares memory with an input or another output: workgroups read the one while others write the other
+ * (SS_ERR_PARAM where two of the small arrays are one).
  *
  * Cache.  Keys and values lie in pages of page_size positions, [pages, page_size, kv_heads, head_dim] each; position t of
  * sequence b is slot t % page_size of page block_table[b][t / page_size].  Pages may be shared between sequences.
@@ -119,7 +121,7 @@ ss_status specsteer_tree_verify(const void *G, const void *S_ctx, const void *S_
  *   k_cache, v_cache  device, laid out as described above; no memory of k, v or each other
  *   accepted_len      device, [B] int32, 0..N
  *   path              device, [B, N] int32, or NULL: 0, 1, 2, ..., a chain's
- *   new_len           device, [B] int32 out; not cache_len itself
+ *   new_len           device, [B] int32 out; neither cache_len nor accepted_len itself
  *
  * A sequence whose accepted_len, cache_len, path or pages are out of range, or whose positions pass table_width * page_size,
  * has -1 in new_len, and nothing of it is written.  Sequences that would write the same slot of the same page race.

@@ -71,7 +71,7 @@ extern "C" ss_status specsteer_tree_commit(const void* k, const void* v, void* k
     if (params->batch == 0) return SS_OK;
     const bool cached = params->pages > 0 && params->table_width > 0;
     if (!k || !v || !cache_len || !accepted_len || !new_len || (cached && (!k_cache || !v_cache || !block_table))) return SS_ERR_NULL;
-    if (new_len == cache_len) return SS_ERR_PARAM;
+    if (shared({new_len}, {cache_len, accepted_len, path, block_table})) return SS_ERR_PARAM;
     if (off_16(k) || off_16(v) || (cached && (off_16(k_cache) || off_16(v_cache)))) return SS_ERR_STRIDE;
     if (cached && k_cache == v_cache) return SS_ERR_PARAM;  // keys and values would race for their places
     const CommitArgs a{static_cast<const char*>(k), static_cast<const char*>(v), static_cast<char*>(k_cache), static_cast<char*>(v_cache), block_table,

@@ -993,6 +993,7 @@ ss_status specsteer_tree_verify(const void* G, const void* S_ctx, const void* S_
     if (params->batch == 0) return SS_OK;
     const bool nodes = params->k_max > 0;
     if (!G || !S_ctx || !S_noctx || !uniforms || !accepted_len || !next_token || (nodes && (!tokens || !path))) return SS_ERR_NULL;
+    if (shared({accepted_len, next_token, next_token_logprob, nodes ? path : nullptr}, {tree_len, uniforms, nodes ? tokens : nullptr, nodes ? parents : nullptr})) return SS_ERR_PARAM;
     const uintptr_t elem = params->dtype == SS_BF16 ? 1 : 3;
     if ((reinterpret_cast<uintptr_t>(G) | reinterpret_cast<uintptr_t>(S_ctx) | reinterpret_cast<uintptr_t>(S_noctx)) & elem) return SS_ERR_STRIDE;
     const VerifyPlan p = verify_plan(*params, device_cu_count());

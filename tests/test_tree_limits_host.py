@@ -1,8 +1,11 @@
-"""CPU checks of positions and pages at the ends of 32 bits, with the headers that the kernels share, compiled for the host with its checks of overflows."""
+"""CPU checks of positions and pages at the ends of 32 bits, with the headers that the kernels share, compiled for the host with its checks of overflows;
+and of the refusal of outputs that are inputs."""
 import os
 import subprocess
 
 import pytest
+
+from test_tree_host import AT, PARAM, call, tree  # noqa: F401
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 SOURCE = r"""
@@ -53,3 +56,11 @@ def test_pages_that_a_commit_writes(program, page):
         for rows in (0, 1, 255, 256, 1024):
             if length + rows + 1 <= LAST:
                 assert program(length, rows, page) == [length // page, (length + rows) // page - length // page]
+
+
+@pytest.mark.parametrize("name,arrays", [
+    *[("commit", ("new_len", k)) for k in ("cache_len", "accepted_len", "path", "block_table")],
+    *[("verify", (o, i)) for o in ("accepted_len", "path", "next_token", "next_token_logprob") for i in ("tokens", "parents", "tree_len", "uniforms")],
+    ("verify", ("accepted_len", "next_token")), ("verify", ("path", "accepted_len")), ("verify", ("next_token_logprob", "next_token"))])
+def test_no_output_is_an_input_or_another_output(tree, name, arrays):
+    assert call(tree, name, **{k: AT for k in arrays}) == PARAM
