@@ -66,7 +66,6 @@ template <int LOADS, int HELD, bool SHARED>
 __device__ __forceinline__ void arrived(int later) {
     static_assert(2 * LOADS * (HELD - 1) < 64, "what the counter counts");
     if (later >= HELD - 1) wait_loads<2 * LOADS*(HELD - 1)>();
-    else if (HELD > 4 && later >= 3) wait_loads<2 * LOADS * 3>();
     else if (HELD > 3 && later >= 2) wait_loads<2 * LOADS * 2>();
     else if (HELD > 2 && later >= 1) wait_loads<2 * LOADS>();
     else wait_loads<0>();
@@ -264,8 +263,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
         cut->parts = parts;
         cut->second = second;
     }
-    bool first_item = true;
-    int turn_of = 0;
+    int done = 0;  // items
     if (tid == 0) sh_bad[0] = 0;
     // the piece of the table that is in LDS: its sequence, the column that it begins with, the tiles whose pages it has
     int table_of = -1, table_from = 0, table_first = 0, table_until = 0;
@@ -294,7 +292,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
         for (int i = 0; i < kBlocks; ++i) o[i] = f32x16{};
         __syncthreads();  // the last item's hand-over is done with
         // Cleared a barrier before any wave may set it: where waves go on by themselves there is none between here and an item's end
-        if (tid == 0) sh_bad[turn_of ^ 1] = 0;
+        if (tid == 0) sh_bad[~done & 1] = 0;
         if (!s.bad) {
             // The rows of a tile that this wave loads are kMine from first_row on.  A lane finds where one of them lies, and those that load its pieces
             // ask for that: the arithmetic once for all rows, whatever the pages' size.  The pages come from a piece of the table in LDS.
@@ -307,11 +305,11 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
                 if (b != table_of) table_bad = false;
                 table_of = b;
                 table_first = t;
-                const TablePiece piece = table_piece(t, C::kTile, a.page_size, s.L, items.cached, C::kTable);
+                const TablePiece piece = table_piece(t, C::kTile, a.page_of, a.page_size, s.L, items.cached, C::kTable);
                 table_from = piece.from;
                 table_until = piece.until;
                 for (int i = tid; i < piece.entries; i += C::kThreads) {
-                    int p = pages[(long)table_from + i];
+                    int p = pages[table_from + i];
                     if (p < 0 || p >= a.pages) {
                         table_bad = true;
                         p = 0;
@@ -570,7 +568,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
             }
             l += __shfl_xor(l, 32, kWave);
         }
-        if (bad || (table_bad && table_of == b)) sh_bad[turn_of] = 1;
+        if (bad || (table_bad && table_of == b)) sh_bad[done & 1] = 1;
         // the waves' sums over their keys to those of the first
         __syncthreads();
         float* const hand = reinterpret_cast<float*>(lds);
@@ -610,7 +608,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
                         }
                 }
             }
-            if (sh_bad[turn_of]) l = __builtin_nanf("");
+            if (sh_bad[done & 1]) l = __builtin_nanf("");
             if (row < rows) {
                 if (whole) {
                     const float by = 1.f / l;
@@ -625,7 +623,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
                             __builtin_memcpy(__builtin_assume_aligned(to + 2 * (db * 32 + 8 * i), 8), r, 8);
                         }
                 } else {
-                    const long slot = 2l * blockIdx.x + (first_item ? 0 : 1), at = slot * C::kColumns + place_of;
+                    const long slot = 2l * blockIdx.x + (done == 0 ? 0 : 1), at = slot * C::kColumns + place_of;
                     if (half == 0) a.part_ml[at] = make_float2(m, l);
                     float* const to = a.part_o + at * D + 4 * half;
 #pragma unroll
@@ -636,8 +634,7 @@ __global__ __launch_bounds__(C::kThreads) __attribute__((amdgpu_waves_per_eu(2, 
                 }
             }
         }
-        first_item = false;
-        turn_of ^= 1;
+        ++done;
         rel += t1 - t0;
         u += t1 - t0;
     }

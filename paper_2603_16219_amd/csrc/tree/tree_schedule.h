@@ -56,11 +56,11 @@ inline PageOf page_of(int size) {
 struct TablePiece {
     int from, entries, until;
 };
-SS_TREE_BOTH TablePiece table_piece(int t, int tile, int page_size, int length, int cached, int most) {
+SS_TREE_BOTH TablePiece table_piece(int t, int tile, PageOf page_of, int page_size, int length, int cached, int most) {
     TablePiece r;
-    const long first = (long)t * tile;
-    r.from = (int)(first / page_size);
-    const int left = (length - 1) / page_size - r.from;  // behind the first: no sum that may pass 32 bits where pages are of one position
+    const int first = t * tile;
+    r.from = (int)page_of((unsigned)first);
+    const int left = (int)page_of((unsigned)length - 1) - r.from;  // behind the first: no sum that may pass 32 bits where pages are of one position
     r.entries = left < most ? left + 1 : most;
     const long more = (((long)r.from + most) * page_size - first) / tile;
     r.until = more < cached - t ? t + (int)more : cached;

@@ -48,7 +48,7 @@ struct VerifyArgs {
     long sb, st;
     int B, N, V;
     Factor c;
-    double c64, inv_tau, lambda, beta;
+    double c64, lambda, beta;
     float steer_hi, steer_lo;  // beta c in two parts
     float steer_size, steer_most;  // |beta c|, and the difference whose product with it is kFar
     int far, greedy, plain;    // plain: beta is 0
@@ -681,8 +681,7 @@ __global__ __launch_bounds__(kVerifyGroup) void draw_kernel(const VerifyArgs a, 
     __shared__ W w;
     __shared__ Best best[kWaves];
     __shared__ double sum[kWaves];
-    __shared__ int pick[4];
-    __shared__ Mass held[kVerifyGroup];
+    __shared__ int before_us, last_of[kWaves];
     const int b = (int)(blockIdx.x / (unsigned)a.parts), part = (int)(blockIdx.x - (unsigned)(b * a.parts));
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const bool leader = part == 0;
@@ -786,9 +785,9 @@ __global__ __launch_bounds__(kVerifyGroup) void draw_kernel(const VerifyArgs a, 
     delivered();
     __syncthreads();
     if (a.parts > 1) {  // the last of the sequence's workgroups goes on
-        if (tid == 0) pick[0] = atomicAdd(reinterpret_cast<int*>(a.arrive + (long)b * kArriveBytes), 1);
+        if (tid == 0) before_us = atomicAdd(reinterpret_cast<int*>(a.arrive + (long)b * kArriveBytes), 1);
         __syncthreads();
-        if (pick[0] + 1 < a.parts) return;
+        if (before_us + 1 < a.parts) return;
     }
     // all masses at the largest reference
     static_assert(sizeof(Mass) <= sizeof(double) && SS_MAX_VOCAB / 4 / kMassVecs + 1 <= SS_MAX_K + 1, "space for a row's masses");
@@ -829,7 +828,6 @@ __global__ __launch_bounds__(kVerifyGroup) void draw_kernel(const VerifyArgs a, 
     const double incl = wave_incl_scan_f64(mine);
     __syncthreads();
     if (lane == 63) sum[wave] = incl;
-    if (tid == 0) pick[1] = pick[2] = -1;
     __syncthreads();
     double Z = 0.0, before = incl - mine;
     for (int v = 0; v < kWaves; ++v) {
@@ -873,7 +871,7 @@ __global__ __launch_bounds__(kVerifyGroup) void draw_kernel(const VerifyArgs a, 
         if (lane == 0) {
             w.scan[wave] = found;
             sum[wave] = start;
-            held[wave] = Mass{0.f, __int_as_float(last)};
+            last_of[wave] = last;
         }
         __syncthreads();
     }
@@ -884,7 +882,7 @@ __global__ __launch_bounds__(kVerifyGroup) void draw_kernel(const VerifyArgs a, 
             chunk = w.scan[v];
             start = sum[v];
         }
-    for (int v = 0; v < kWaves; ++v) last_chunk = max(last_chunk, __float_as_int(held[v].s));
+    for (int v = 0; v < kWaves; ++v) last_chunk = max(last_chunk, last_of[v]);
     const bool take_last = chunk == kNever;
     if (take_last) chunk = last_chunk;
     if (wave != 0) return;
@@ -1027,7 +1025,6 @@ ss_status specsteer_tree_verify(const void* G, const void* S_ctx, const void* S_
     a.V = params->vocab;
     a.c = r.c;
     a.c64 = r.c64;
-    a.inv_tau = r.inv_tau;
     a.lambda = (double)params->lambda;
     a.beta = (double)params->beta;
     a.steer_hi = (float)(a.beta * a.c64);

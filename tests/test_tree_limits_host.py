@@ -15,7 +15,7 @@ SOURCE = r"""
 int main(int argc, char** argv) {
     const auto arg = [&](int i) { return (int)std::atol(argv[i]); };
     if (argc == 7) {
-        const TablePiece r = table_piece(arg(1), arg(2), arg(3), arg(4), arg(5), arg(6));
+        const TablePiece r = table_piece(arg(1), arg(2), page_of(arg(3)), arg(3), arg(4), arg(5), arg(6));
         std::printf("%d %d %d", r.from, r.entries, r.until);
     } else {
         const PageRange r = pages_written(arg(1), arg(2), arg(3));
