@@ -134,8 +134,8 @@ def _ints(t: Optional[torch.Tensor], what: str, shape: tuple, device: torch.devi
         raise TypeError(f"{what} must be integers, got {t.dtype}")
     if tuple(t.shape) != shape:
         raise ValueError(f"{what} must be {list(shape)}, got {list(t.shape)}")
-    if t.dtype is torch.int64:  # a number beyond 32 bits must not come out as another, valid one
-        t = t.clamp(-2**31, 2**31 - 1)
+    if t.dtype is torch.int64:  # a number beyond 32 bits must not come out as another, valid one: the least is none, the largest may be a length
+        t = torch.where((t < 2**31) & (t >= -2**31), t, -2**31)
     return _ready(t, device, torch.int32)
 
 

@@ -4,6 +4,7 @@ import os
 import subprocess
 
 import pytest
+import torch
 
 from test_tree_host import AT, PARAM, call, tree  # noqa: F401
 
@@ -64,3 +65,9 @@ def test_pages_that_a_commit_writes(program, page):
     ("verify", ("accepted_len", "next_token")), ("verify", ("path", "accepted_len")), ("verify", ("next_token_logprob", "next_token"))])
 def test_no_output_is_an_input_or_another_output(tree, name, arrays):
     assert call(tree, name, **{k: AT for k in arrays}) == PARAM
+
+
+def test_numbers_beyond_32_bits_are_out_of_range(tree):
+    t = torch.tensor([0, -1, 5, 2**31 - 1, 1 - 2**31, -2**31, 2**31, 2**32 + 5, -2**32 + 5, 2**63 - 1, -2**63])
+    low = -2**31
+    assert tree._ints(t, "t", (11,), t.device).tolist() == [0, -1, 5, 2**31 - 1, 1 - 2**31, low, low, low, low, low, low]
