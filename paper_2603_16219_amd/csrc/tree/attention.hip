@@ -777,8 +777,8 @@ ss_status specsteer_tree_attention(const void* q, const void* k, const void* v, 
         a.page_size = params->page_size;
         a.width = cached ? params->table_width : 0;
         a.shares = plan.shares;
-        // a factor of 0 would make masked scores NaN; under this one all that can be told apart is the mask
-        a.scale = std::fmax(std::fabs(params->scale) * 1.4426950408889634f, 1e-30f);
+        // a factor of 0 would make masked scores NaN, and an infinite one scores of 0; the least normal number tells scores apart beyond 1e37 only
+        a.scale = (float)std::fmin(std::fmax(std::fabs((double)params->scale) * 1.4426950408889634, 1.1754944e-38), 3.4028234e38);
         a.negative = params->scale < 0.f;
         hipStream_t st = static_cast<hipStream_t>(stream);
         const bool bf = params->dtype == SS_BF16;

@@ -141,6 +141,13 @@ def test_scores_of_any_size(tree, dtype):
     assert torch.equal(run(tree, i), torch.full_like(i["q"], 3))
 
 
+@pytest.mark.parametrize("scale,q,k", [(0.0, 1e15, 1e13), (1e-36, 1e18, 1e17), (-2e-38, 1e18, 3e18), (1e30, 1e-15, 1e-15), (-3.4e38, 0.0, 1.0), (3.4e38, 0.0, 1.0)])
+def test_scales_at_the_ends_of_their_type(tree, scale, q, k):
+    i = make(2, 10, 8, 2, 128, [400, 77], 16)
+    i["q"], i["k"], i["k_cache"] = (i["q"].float() * q).to(torch.bfloat16), (i["k"].float() * k).to(torch.bfloat16), (i["k_cache"].float() * k).to(torch.bfloat16)
+    check(tree, i, scale=scale)
+
+
 def test_rising_and_falling_scores(tree):
     for sign in (1, -1):
         i = make(1, 3, 4, 1, 64, 3000, 16, "bf16")
