@@ -75,8 +75,9 @@ size_t specsteer_tree_attention_workspace_bytes(const ss_tree_params *params);
  *
  * A sequence whose cache_len or tree_len is out of range, or a parent or a page that is needed, has NaN in all its rows.  A
  * row never takes anything from positions that it does not see, whatever they hold.  What it sees is expected to be finite,
- * the sums q . k to be numbers of fp32 and scale * q . k below 2^30 in size: a row that sees other values has NaN, or what they make of it.  A call whose work may
- * reach 2^31 tiles (keys times heads times rows, by 64 keys times 32 to 256 rows) is refused with SS_ERR_SHAPE.
+ * the sums q . k to be numbers of fp32, and scale * q . k to be below 2^30 in size: a row that sees other values has NaN, or
+ * what they make of it.  A call whose work may reach 2^31 tiles (keys times heads times rows, by 64 keys times 32 to 256 rows)
+ * is refused with SS_ERR_SHAPE.
  */
 ss_status specsteer_tree_attention(const void *q, const void *k, const void *v, const void *k_cache, const void *v_cache,
                                    const int32_t *block_table, const int32_t *cache_len, const int32_t *parents,

@@ -371,7 +371,7 @@ __device__ __forceinline__ void finish(const AltArgs& a, long row, int y, float 
     }
 }
 
-// Bytes bound it: 1024 rows of 151936 in bf16 take 54 us without likeliest tokens, 5.8 TB/s, and 77 with 16 of them, 4.1 TB/s; 104 with 64.  Registers
+// Bytes bound it: 1024 rows of 151936 in bf16 take 56 us without likeliest tokens, 5.6 TB/s, and 73 with 16 of them, 4.25 TB/s; 104 with 64.  Registers
 // for four waves a SIMD hold two workgroups a unit, one of which computes while the other waits: with one it was 113 us.
 constexpr int kAltThreads = 512;
 template <int DT, bool TOP>

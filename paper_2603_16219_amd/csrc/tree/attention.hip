@@ -13,8 +13,8 @@
 // spreads both the keys' reads and the values' transposed ones over the banks.
 //
 // Bytes: the cache once a call for up to 256 columns, whose products take 4 D flop a column for 4 D bytes a key.  Measured, main launch and join: 32 trees of 24
-// nodes over up to 4096 tokens (32 heads over 8, D = 128, bf16; 411 MB) 111 us, 3.7 TB/s; the same without loads 101 us: products, softmax and LDS in turn.
-// 8 rows (32 columns) instead of 25 over the same cache take 95 us.  4 times 64 rows over 65536 tokens (275 GFLOP) 330 to 356 us, 770 to 830 TFLOP/s; 128
+// nodes over up to 4096 tokens (32 heads over 8, D = 128, bf16; 411 MB) 112 us, 3.7 TB/s; the same without loads 101 us: products, softmax and LDS in turn.
+// 8 rows (32 columns) instead of 25 over the same cache take 95 us.  4 times 64 rows over 65536 tokens (275 GFLOP) 333 to 344 us, 800 to 825 TFLOP/s; 128
 // chains of 8 over up to 2000 tokens (16 heads, D = 64, fp16; 792 MB) 161 us, 4.9 TB/s.  One token over 1000 takes 14 us: a launch that finds its place in
 // the batch before its first load (6 to 8 us), and the join's 4.
 #include "tree_common.h"
